@@ -539,6 +539,143 @@ sbc_status sbc_event_stream_step_decays(const int32_t *px, const int32_t *py, co
                                         hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * 11. Layer norm over the channels of a row:
+ *     y = (x - mean) rstd w + b,  rstd = 1 / sqrt(var + eps),
+ * var the mean squared difference from the mean, all in float32.
+ *   x, y, dy, dx     [n, C] float32 or bf16 (dtype), rows *_stride elements
+ *                    apart (>= C); outputs are rounded once, to the same type
+ *   weight, bias     [C] float32, or NULL (1 and 0); C <= 2^24
+ *   mean, rstd       [n] float32 output of the forward (NULL: not wanted),
+ *                    input of the backward
+ * The backward gives the gradients of <y, dy>: dx, dweight [C] and dbias [C]
+ * (float32); each may be NULL.  With neither dweight nor dbias it needs no
+ * workspace.  Sums over rows are taken in a fixed order.  No output may overlap
+ * an input; no pointer needs more than its elements' alignment.
+ * ------------------------------------------------------------------------ */
+sbc_status sbc_layer_norm_forward(const void *x, int64_t x_stride, const float *weight,
+                                  const float *bias, sbc_dtype dtype, int32_t n, int32_t C,
+                                  float eps, void *y, int64_t y_stride, float *mean, float *rstd,
+                                  hipStream_t stream);
+size_t sbc_layer_norm_workspace_size(int32_t n, int32_t C);
+sbc_status sbc_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
+                                   int64_t x_stride, const float *weight, const float *mean,
+                                   const float *rstd, sbc_dtype dtype, int32_t n, int32_t C,
+                                   void *dx, int64_t dx_stride, float *dweight, float *dbias,
+                                   void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The heads of n tokens: element c of head h of token i is
+ * data[i * token_stride + h * head_stride + c] (strides in elements, the last
+ * axis dense).  Strides of inputs may be 0 (the same for all); the elements of
+ * an output must be distinct.  data needs its elements' alignment. */
+typedef struct {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} sbc_heads;
+
+/* ------------------------------------------------------------------------
+ * 12. Rotary positions with several axes (time and pixel of events, coordinates
+ * of points).  The channels of a head hold pairs (a, b): channels p and
+ * p + pairs, or with `interleaved` 2 p and 2 p + 1, p < pairs = the sum of
+ * sections.  Pair p belongs to the axis whose section it lies in and turns by
+ * angle = positions[i, axis] * freqs[p]:
+ *     (a, b) -> (a cos - b sin, b cos + a sin),
+ * with backward != 0 by the opposite angle (the gradient).  Channels past
+ * 2 * pairs are copied.  The angle is reduced in float64, so large positions
+ * lose nothing.
+ *   q, k     [n, q_heads, d] and [n, k_heads, d] (either may have 0 heads and be
+ *            NULL), float32 or bf16; q_out and k_out alike: they may be q and k
+ *            themselves, and overlap nothing else
+ * ------------------------------------------------------------------------ */
+#define SBC_MAX_AXES 8
+typedef struct {
+    const void *positions;     /* [n, n_axes] float32 or int32, device           */
+    int64_t position_stride;   /* elements from token to token, >= n_axes        */
+    int32_t float_positions;   /* 1: float32, 0: int32                           */
+    const float *freqs;        /* [pairs] radians per unit, device               */
+    int32_t n_axes;            /* 1 .. SBC_MAX_AXES                              */
+    int32_t sections[SBC_MAX_AXES]; /* pairs of each axis, >= 0; 2 * sum <= d    */
+    int32_t interleaved;
+} sbc_rotary_plan;
+sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q, int32_t q_heads,
+                      const sbc_heads *k, int32_t k_heads, sbc_dtype dtype, int32_t n, int32_t d,
+                      int32_t backward, const sbc_heads *q_out, const sbc_heads *k_out,
+                      hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * 13. Linear attention with a decay for each head.  For token i of a sequence
+ * and head h (rate lambda = rates[h]):
+ *     o_i = scale * sum over j <= i of exp(-lambda (t_i - t_j)) (q_i . k_j) v_j,
+ * the sequence counterpart of the event kernel's decay (Section 3.2, Eq. 12).
+ * It is a recursion on a state S [dk, dv]:
+ *     S_i = exp(-lambda (t_i - t_{i-1})) S_{i-1} + k_i v_i^T,  o_i = scale q_i S_i,
+ * which starts from zero, or from a kept state and its time.  The forward takes
+ * whole sequences in chunks, the step one token of each.
+ *   t          [n] int32 times, non-decreasing within a sequence, or NULL: the
+ *              position (a kept state then lies one position before the first
+ *              token).  Elapsed times are taken modulo 2^32, so a clock may
+ *              wrap; where t decreases the results are unspecified (finite for
+ *              finite inputs).
+ *   splits     [n_batch + 1] int32, 0 .. n: sequence b owns the tokens
+ *              splits[b] .. splits[b+1]-1, perhaps none; NULL: one sequence
+ *   rates      [heads] float32, >= 0 and finite
+ *   q, k       [n, heads, dk], v, o [n, heads, dv]: float32 or bf16 (dtype),
+ *              1 <= dk, dv <= 128
+ *   state_in   [n_batch, heads, dk, dv] float32, or NULL: zero; with t,
+ *              state_time [n_batch] int32 its time
+ *   state_out  the same after each sequence's last token, or NULL; with t,
+ *              time_out [n_batch] its time (both NULL or none; of an empty
+ *              sequence those of state_in, zero without one)
+ * Products are taken on the matrix cores with operands split into bf16 parts
+ * (float32: three; of bf16 inputs only what is computed from them: two, and
+ * three for the state) and summed in float32; o is rounded once.
+ * No output may overlap an input.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    int32_t n, n_batch, heads, dk, dv;
+    sbc_dtype dtype;
+    float scale;
+    const float *rates;
+    const int32_t *splits;
+    const int32_t *t;
+} sbc_attention;
+size_t sbc_linear_attention_workspace_size(int32_t n, int32_t heads, int32_t dk, int32_t dv);
+sbc_status sbc_linear_attention_forward(const sbc_attention *a, const sbc_heads *q,
+                                        const sbc_heads *k, const sbc_heads *v,
+                                        const float *state_in, const int32_t *state_time,
+                                        const sbc_heads *o, float *state_out, int32_t *time_out,
+                                        void *workspace, size_t workspace_bytes,
+                                        hipStream_t stream);
+
+/* The gradients of <o, dO> for sequences that start from zero: with D_ij the
+ * decay,
+ *     dq_i = scale * sum over j <= i of D_ij (dO_i . v_j) k_j,
+ *     dk_j = scale * sum over i >= j of D_ij (dO_i . v_j) q_i,
+ *     dv_j = scale * sum over i >= j of D_ij (q_i . k_j) dO_i,
+ *     drates[h] = -scale * sum of (t_i - t_j) D_ij (q_i . k_j) (dO_i . v_j).
+ *   dO [n, heads, dv]; dq, dk [n, heads, dk], dv [n, heads, dv]: of dtype
+ *   drates [heads] float32, or NULL: not wanted */
+size_t sbc_linear_attention_backward_workspace_size(int32_t n, int32_t heads, int32_t dk,
+                                                    int32_t dv);
+sbc_status sbc_linear_attention_backward(const sbc_attention *a, const sbc_heads *dO,
+                                         const sbc_heads *q, const sbc_heads *k,
+                                         const sbc_heads *v, const sbc_heads *dq,
+                                         const sbc_heads *dk, const sbc_heads *dv, float *drates,
+                                         void *workspace, size_t workspace_bytes,
+                                         hipStream_t stream);
+
+/* One token for each of n streams (n_batch and splits are not read): token i is
+ * stream i's next.  Arguments as above with state_in and state_out [n, heads, dk,
+ * dv] given (and with t state_time and time_out); without t every step is one
+ * position.  state_out may be state_in itself; time_out must not overlap
+ * state_time or t.  No workspace. */
+sbc_status sbc_linear_attention_step(const sbc_attention *a, const sbc_heads *q,
+                                     const sbc_heads *k, const sbc_heads *v,
+                                     const float *state_in, const int32_t *state_time,
+                                     const sbc_heads *o, float *state_out, int32_t *time_out,
+                                     hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Tracing, for measurement tools.  After sbc_trace_kernel(name, start, stop)
  * every launch of the kernel called `name` made by the calling thread records
  * `start` immediately before and `stop` immediately after itself on its

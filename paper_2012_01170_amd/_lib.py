@@ -36,6 +36,10 @@ EXPORTS = [
     "sbc_event_stream_workspace_size", "sbc_event_stream_step",
     "sbc_event_stream_decays_workspace_size", "sbc_event_stream_step_decays",
     "sbc_conv_forward_noalloc_max_bytes", "sbc_conv_forward_noalloc",
+    "sbc_layer_norm_forward", "sbc_layer_norm_workspace_size", "sbc_layer_norm_backward",
+    "sbc_rotary", "sbc_linear_attention_workspace_size", "sbc_linear_attention_forward",
+    "sbc_linear_attention_backward_workspace_size", "sbc_linear_attention_backward",
+    "sbc_linear_attention_step",
 ]
 
 
@@ -62,6 +66,28 @@ class SbcConvPlan(ctypes.Structure):
                 ("forward_fused", ctypes.c_int32), ("backward_fused", ctypes.c_int32)]
 
 
+SBC_MAX_AXES = 8
+
+
+class SbcHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class SbcRotaryPlan(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("position_stride", ctypes.c_int64),
+                ("float_positions", ctypes.c_int32), ("freqs", ctypes.c_void_p),
+                ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * SBC_MAX_AXES),
+                ("interleaved", ctypes.c_int32)]
+
+
+class SbcAttention(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("n_batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("dk", ctypes.c_int32), ("dv", ctypes.c_int32), ("dtype", ctypes.c_int),
+                ("scale", ctypes.c_float), ("rates", ctypes.c_void_p),
+                ("splits", ctypes.c_void_p), ("t", ctypes.c_void_p)]
+
+
 class SbcError(RuntimeError):
     def __init__(self, status: int, message: str):
         self.status = status
@@ -76,6 +102,8 @@ _csr_p = ctypes.POINTER(SbcCsr)
 _csc_p = ctypes.POINTER(SbcCsc)
 _geo_p = ctypes.POINTER(SbcGeometry)
 _i64_p = ctypes.POINTER(ctypes.c_int64)
+_heads_p = ctypes.POINTER(SbcHeads)
+_attn_p = ctypes.POINTER(SbcAttention)
 
 _SIGS = {
     "sbc_last_error": (ctypes.c_char_p, []),
@@ -132,6 +160,21 @@ _SIGS = {
     "sbc_kernel_names": (ctypes.c_char_p, []),
     "sbc_conv_plan": (ctypes.c_int, [_i32, _i32, _i64, _i32, _i32, _i32, ctypes.c_int, ctypes.c_int,
                                      ctypes.POINTER(SbcConvPlan)]),
+    "sbc_layer_norm_forward": (ctypes.c_int, [_vp, _i64, _vp, _vp, ctypes.c_int, _i32, _i32, _f32,
+                                              _vp, _i64, _vp, _vp, _vp]),
+    "sbc_layer_norm_workspace_size": (_sz, [_i32, _i32]),
+    "sbc_layer_norm_backward": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, ctypes.c_int,
+                                               _i32, _i32, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "sbc_rotary": (ctypes.c_int, [ctypes.POINTER(SbcRotaryPlan), _heads_p, _i32, _heads_p, _i32,
+                                  ctypes.c_int, _i32, _i32, _i32, _heads_p, _heads_p, _vp]),
+    "sbc_linear_attention_workspace_size": (_sz, [_i32, _i32, _i32, _i32]),
+    "sbc_linear_attention_forward": (ctypes.c_int, [_attn_p, _heads_p, _heads_p, _heads_p, _vp,
+                                                    _vp, _heads_p, _vp, _vp, _vp, _sz, _vp]),
+    "sbc_linear_attention_backward_workspace_size": (_sz, [_i32, _i32, _i32, _i32]),
+    "sbc_linear_attention_backward": (ctypes.c_int, [_attn_p] + [_heads_p] * 7 +
+                                      [_vp, _vp, _sz, _vp]),
+    "sbc_linear_attention_step": (ctypes.c_int, [_attn_p, _heads_p, _heads_p, _heads_p, _vp, _vp,
+                                                 _heads_p, _vp, _vp, _vp]),
 }
 
 

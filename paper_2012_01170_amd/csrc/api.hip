@@ -18,7 +18,8 @@ const char *kKernelNames =
     "bwd_tile_df,bwd_tile_dw,decay_tile_dw,"
     "featureless_fwd,featureless_rowsum,featureless_dphi,decay_basis,decay_spmm,decay_gemm,"
     "decay_dot,decay_fused,decay_dw_reduce,sample_count,sample,lif_sort,lif_cells,lif_emit,stream_lists,stream_gather,stream_gemm,"
-    "stream_update";
+    "stream_update,norm_fwd,norm_bwd,norm_reduce,rotary,attn_state,attn_scan,attn_fwd,attn_bwd_state,"
+    "attn_bwd,attn_rates,attn_step";
 }  // namespace
 
 void trace_before(const char *name, hipStream_t stream) {

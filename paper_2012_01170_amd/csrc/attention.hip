@@ -1,0 +1,116 @@
+// Linear attention with decays, forward over whole sequences (attention.hpp).
+#include "attention_host.hpp"
+#include "attention_kernels.hpp"
+
+namespace sbc {
+namespace {
+
+constexpr int kFwdPerCu = 2;
+
+void forward_segments(int32_t n, int32_t heads, int32_t dv, int32_t *seg_len, int32_t *n_seg) {
+    attn_segments(n, (int64_t)heads * attn_tiles(dv), kFwdPerCu, seg_len, n_seg);
+}
+
+template <typename T> sbc_status forward(const AttnPass &p, hipStream_t stream) {
+    constexpr int NS = sizeof(T) == 4 ? 3 : 2;
+    pass_dispatch(p.da, attn_tile(p.dc), [&](auto da, auto dct) {
+        constexpr int DA = decltype(da)::value, DCT = decltype(dct)::value;
+        if (p.n_seg > 1) {
+            trace_before("attn_state", stream);
+            hipLaunchKernelGGL((attn_state_kernel<T, DA, DCT, false>), pass_grid(p),
+                               dim3(kAttnThreads), 0, stream, p);
+            trace_after("attn_state", stream);
+            trace_before("attn_scan", stream);
+            hipLaunchKernelGGL(attn_scan_kernel<false>,
+                               dim3((unsigned)grid_for(p.state_stride, 64), (unsigned)p.heads),
+                               dim3(256), 0, stream, p.carry, p.factor, p.n_seg, p.heads,
+                               p.state_stride);
+            trace_after("attn_scan", stream);
+        }
+        trace_before("attn_fwd", stream);
+        hipLaunchKernelGGL((attn_pass_kernel<T, DA, DCT, false, NS>), pass_grid(p),
+                           dim3(kAttnThreads), 0, stream, p);
+        trace_after("attn_fwd", stream);
+    });
+    SBC_LAUNCH_CHECK();
+    return SBC_OK;
+}
+
+}  // namespace
+}  // namespace sbc
+
+using namespace sbc;
+
+extern "C" size_t sbc_linear_attention_workspace_size(int32_t n, int32_t heads, int32_t dk,
+                                                      int32_t dv) {
+    if (n < 0 || heads <= 0 || dk <= 0 || dv <= 0 || dk > 128 || dv > 128) return 0;
+    int32_t seg_len, n_seg;
+    forward_segments(n, heads, dv, &seg_len, &n_seg);
+    Carver c(nullptr);
+    c.take<float>((size_t)n_seg * heads * state_stride(dk, dv));
+    c.take<float>((size_t)n_seg * heads);
+    return c.used;
+}
+
+extern "C" sbc_status sbc_linear_attention_forward(const sbc_attention *a, const sbc_heads *q,
+                                                   const sbc_heads *k, const sbc_heads *v,
+                                                   const float *state_in,
+                                                   const int32_t *state_time, const sbc_heads *o,
+                                                   float *state_out, int32_t *time_out,
+                                                   void *workspace, size_t workspace_bytes,
+                                                   hipStream_t stream) {
+    clear_error();
+    SBC_TRY(check_sequences(a));
+    const int32_t n = a->n, H = a->heads;
+    SBC_TRY(check_heads(q, H, n, a->dk, a->dtype, "q"));
+    SBC_TRY(check_heads(k, H, n, a->dk, a->dtype, "k"));
+    SBC_TRY(check_heads(v, H, n, a->dv, a->dtype, "v"));
+    SBC_TRY(check_out_heads(o, H, n, a->dv, a->dtype, "o"));
+    if (a->t && state_in && !state_time)
+        return fail(SBC_ERR_INVALID_ARG, "a state needs its time (state_time) where t is given");
+    if (a->t && (state_out != nullptr) != (time_out != nullptr))
+        return fail(SBC_ERR_INVALID_ARG, "with t, state_out and time_out go together");
+    if (n == 0 && (a->n_batch == 0 || !state_out)) return SBC_OK;
+    const size_t state_bytes = (size_t)a->n_batch * H * a->dk * a->dv * 4;
+    if (overlap(state_in, state_bytes, state_out, state_bytes))
+        return fail(SBC_ERR_INVALID_ARG, "state_out overlaps state_in");
+    if (overlap(state_time, (size_t)a->n_batch * 4, time_out, (size_t)a->n_batch * 4))
+        return fail(SBC_ERR_INVALID_ARG, "time_out overlaps state_time");
+    if (n > 0 && (heads_overlap(*o, H, a->dv, *q, H, a->dk, n, a->dtype) ||
+                  heads_overlap(*o, H, a->dv, *k, H, a->dk, n, a->dtype) ||
+                  heads_overlap(*o, H, a->dv, *v, H, a->dv, n, a->dtype)))
+        return fail(SBC_ERR_INVALID_ARG, "o overlaps an input");
+    if (!a->rates) return fail(SBC_ERR_INVALID_ARG, "rates is null");
+    if (!workspace || workspace_bytes < sbc_linear_attention_workspace_size(n, H, a->dk, a->dv))
+        return fail(SBC_ERR_WORKSPACE,
+                    "workspace smaller than sbc_linear_attention_workspace_size()");
+    AttnPass p{};
+    p.n = n;
+    p.n_batch = a->n_batch;
+    p.heads = H;
+    p.da = a->dk;
+    p.dc = a->dv;
+    forward_segments(n, H, a->dv, &p.seg_len, &p.n_seg);
+    p.tiles = attn_tiles(a->dv);
+    p.scale = a->scale;
+    p.rates = a->rates;
+    p.splits = a->splits;
+    p.t = a->t;
+    if (n > 0) {
+        p.a = *q;
+        p.b = *k;
+        p.c = *v;
+        p.y = *o;
+    }
+    Carver c(workspace);
+    p.state_stride = state_stride(a->dk, a->dv);
+    p.carry = c.take<float>((size_t)p.n_seg * H * p.state_stride);
+    p.factor = c.take<float>((size_t)p.n_seg * H);
+    p.carry_i = a->dv;
+    p.carry_j = 1;
+    p.state_in = state_in;
+    p.state_time = state_time;
+    p.state_out = state_out;
+    p.time_out = a->t ? time_out : nullptr;
+    return a->dtype == SBC_F32 ? forward<float>(p, stream) : forward<bf16_t>(p, stream);
+}

@@ -1,0 +1,198 @@
+// Rotary positions with several axes (time and pixel of an event, coordinates
+// of a point), forward and backward.
+//
+// Pair p of a head's channels turns by the angle positions[i, axis(p)] freqs[p]:
+//   (a, b) -> (a cos - b sin, b cos + a sin),
+// the gradient by the opposite angle.  Every value is moved twice and turned with
+// four products, so memory bounds it as long as the angle's sine and cosine are
+// not made for every head: a lane makes those of kVec pairs of a token once and
+// then takes the token's heads in turn, of both arrays.
+//
+// The angle is taken in revolutions in float64, where the product of two float32
+// is exact and 1 / 2 pi costs 2^-53 of it, and reduced before sine and cosine in
+// float32: angles of 1e6 (timestamps) are as good as small ones.
+#include "common.hpp"
+#include "seq.hpp"
+
+namespace sbc {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct RotaryArgs {
+    sbc_heads in[2], out[2];
+    int32_t heads[2];
+    int32_t n, d, pairs, units;  // units: lanes that a token takes
+    const void *positions;
+    int64_t pos_stride;
+    const float *freqs;
+    int32_t n_axes;
+    int32_t upto[SBC_MAX_AXES];  // pairs of the axes so far
+    float sign;
+};
+
+template <typename T, typename P, bool kInterleaved>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
+    constexpr int V = kVec<T>;
+    const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t i = at / a.units;
+    if (i >= a.n) return;
+    const int unit = (int)(at - i * a.units);
+    const int turning = (a.pairs + V - 1) / V;
+    if (unit >= turning) {  // channels past the last pair are copied
+        const int c = 2 * a.pairs + (unit - turning) * V;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const T *src = static_cast<const T *>(a.in[w].data) + i * a.in[w].token_stride + c;
+            T *dst = static_cast<T *>(a.out[w].data) + i * a.out[w].token_stride + c;
+            for (int h = 0; h < a.heads[w]; ++h) {
+                float v[V];
+                load_vec<T>(src + h * a.in[w].head_stride, a.d - c, v);
+                store_vec<T>(dst + h * a.out[w].head_stride, a.d - c, v);
+            }
+        }
+        return;
+    }
+    const int p0 = unit * V;
+    const int have = a.pairs - p0;  // pairs of this lane, if fewer than V
+    float cs[V], sn[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        cs[k] = 1.f;
+        sn[k] = 0.f;
+        if (k < have) {
+            int axis = 0;
+            for (int x = 0; x + 1 < a.n_axes; ++x) axis += p0 + k >= a.upto[x];
+            const double pos = (double)static_cast<const P *>(a.positions)[i * a.pos_stride + axis];
+            double rev = pos * (double)a.freqs[p0 + k] * 0.15915494309189533577;
+            rev -= rint(rev);
+            float s, c;
+            sincospif((float)(2.0 * rev), &s, &c);
+            cs[k] = c;
+            sn[k] = a.sign * s;
+        }
+    }
+    // the lane's two vectors: the pairs' first and second halves, or the pairs themselves
+    const int c0 = kInterleaved ? 2 * p0 : p0;
+    const int c1 = kInterleaved ? 2 * p0 + V : a.pairs + p0;
+    const int have0 = kInterleaved ? 2 * have : have;
+    const int have1 = kInterleaved ? 2 * have - V : have;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const T *src = static_cast<const T *>(a.in[w].data) + i * a.in[w].token_stride;
+        T *dst = static_cast<T *>(a.out[w].data) + i * a.out[w].token_stride;
+        for (int h = 0; h < a.heads[w]; ++h) {
+            float x[2 * V], lo[V], hi[V];
+            load_vec<T>(src + h * a.in[w].head_stride + c0, have0, lo);
+            load_vec<T>(src + h * a.in[w].head_stride + c1, have1, hi);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                x[k] = lo[k];
+                x[V + k] = hi[k];
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int u = kInterleaved ? 2 * k : k, v = kInterleaved ? 2 * k + 1 : V + k;
+                const float s = x[u] * cs[k] - x[v] * sn[k];
+                x[v] = x[v] * cs[k] + x[u] * sn[k];
+                x[u] = s;
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                lo[k] = x[k];
+                hi[k] = x[V + k];
+            }
+            store_vec<T>(dst + h * a.out[w].head_stride + c0, have0, lo);
+            store_vec<T>(dst + h * a.out[w].head_stride + c1, have1, hi);
+        }
+    }
+}
+
+template <typename T> void launch(const RotaryArgs &a, bool float_pos, bool interleaved,
+                                  hipStream_t stream) {
+    const dim3 grid((unsigned)grid_for((int64_t)a.n * a.units, kThreads)), block(kThreads);
+#define SBC_ROTARY(P, I) hipLaunchKernelGGL((rotary_kernel<T, P, I>), grid, block, 0, stream, a)
+    if (float_pos && interleaved)
+        SBC_ROTARY(float, true);
+    else if (float_pos)
+        SBC_ROTARY(float, false);
+    else if (interleaved)
+        SBC_ROTARY(int32_t, true);
+    else
+        SBC_ROTARY(int32_t, false);
+#undef SBC_ROTARY
+}
+
+}  // namespace
+}  // namespace sbc
+
+using namespace sbc;
+
+extern "C" sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q, int32_t q_heads,
+                                 const sbc_heads *k, int32_t k_heads, sbc_dtype dtype, int32_t n,
+                                 int32_t d, int32_t backward, const sbc_heads *q_out,
+                                 const sbc_heads *k_out, hipStream_t stream) {
+    clear_error();
+    if (!plan) return fail(SBC_ERR_INVALID_ARG, "plan is null");
+    if (n < 0 || d <= 0) return fail(SBC_ERR_INVALID_ARG, "n must be >= 0 and d > 0");
+    if (!known_dtype(dtype)) return fail(SBC_ERR_INVALID_ARG, "unknown dtype");
+    if (plan->n_axes < 1 || plan->n_axes > SBC_MAX_AXES)
+        return fail(SBC_ERR_INVALID_ARG, "n_axes must be 1 .. SBC_MAX_AXES");
+    RotaryArgs a{};
+    int64_t pairs = 0;
+    for (int x = 0; x < plan->n_axes; ++x) {
+        if (plan->sections[x] < 0) return fail(SBC_ERR_INVALID_ARG, "a section is negative");
+        pairs += plan->sections[x];
+        a.upto[x] = (int32_t)(pairs <= d ? pairs : d);
+    }
+    if (pairs < 1 || 2 * pairs > d)
+        return fail(SBC_ERR_INVALID_ARG, "the sections must sum to 1 .. d / 2 pairs");
+    if (plan->position_stride < plan->n_axes)
+        return fail(SBC_ERR_INVALID_ARG, "position_stride is smaller than n_axes");
+    if (q_heads < 0 || k_heads < 0) return fail(SBC_ERR_INVALID_ARG, "negative number of heads");
+    if (n == 0 || (q_heads == 0 && k_heads == 0)) return SBC_OK;
+    if (!plan->positions || !plan->freqs)
+        return fail(SBC_ERR_INVALID_ARG, "positions or freqs is null");
+    SBC_TRY(check_heads(q, q_heads, n, d, dtype, "q"));
+    SBC_TRY(check_heads(k, k_heads, n, d, dtype, "k"));
+    SBC_TRY(check_out_heads(q_out, q_heads, n, d, dtype, "q_out"));
+    SBC_TRY(check_out_heads(k_out, k_heads, n, d, dtype, "k_out"));
+    const sbc_heads none{};
+    const sbc_heads *in[2] = {q_heads ? q : &none, k_heads ? k : &none};
+    const sbc_heads *out[2] = {q_heads ? q_out : &none, k_heads ? k_out : &none};
+    const int32_t heads[2] = {q_heads, k_heads};
+    for (int w = 0; w < 2; ++w) {
+        for (int u = 0; u < 2; ++u) {
+            const bool same = w == u && in[u]->data == out[w]->data &&
+                              in[u]->token_stride == out[w]->token_stride &&
+                              in[u]->head_stride == out[w]->head_stride;
+            if (!same && heads_overlap(*out[w], heads[w], d, *in[u], heads[u], d, n, dtype))
+                return fail(SBC_ERR_INVALID_ARG, "an output overlaps an input that is not its own");
+        }
+        a.in[w] = *in[w];
+        a.out[w] = *out[w];
+        a.heads[w] = heads[w];
+    }
+    if (heads_overlap(*out[0], heads[0], d, *out[1], heads[1], d, n, dtype))
+        return fail(SBC_ERR_INVALID_ARG, "q_out and k_out overlap");
+    const int V = dtype == SBC_F32 ? 4 : 8;
+    a.n = n;
+    a.d = d;
+    a.pairs = (int32_t)pairs;
+    a.units = (int32_t)((pairs + V - 1) / V + (d - 2 * pairs + V - 1) / V);
+    a.positions = plan->positions;
+    a.pos_stride = plan->position_stride;
+    a.freqs = plan->freqs;
+    a.n_axes = plan->n_axes;
+    a.sign = backward ? -1.f : 1.f;
+    if ((int64_t)n * a.units > (int64_t)1 << 31)
+        return fail(SBC_ERR_UNSUPPORTED, "n and d need more than 2^31 lanes");
+    trace_before("rotary", stream);
+    if (dtype == SBC_F32)
+        launch<float>(a, plan->float_positions, plan->interleaved, stream);
+    else
+        launch<bf16_t>(a, plan->float_positions, plan->interleaved, stream);
+    SBC_LAUNCH_CHECK();
+    trace_after("rotary", stream);
+    return SBC_OK;
+}

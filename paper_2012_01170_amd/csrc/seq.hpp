@@ -1,0 +1,145 @@
+// What the sequence operators (layer norm, rotary positions, linear attention)
+// share: element types, vectors of 16 bytes, sums over groups of lanes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <cstring>
+
+#include "common.hpp"
+
+namespace sbc {
+
+// Element types: float, and bf16 as its bits.
+typedef uint16_t bf16_t;
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(bf16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+// float32 -> element, to nearest even (outputs are rounded here, once)
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float x) {
+    return __builtin_bit_cast(bf16_t, (__bf16)x);
+}
+
+template <typename T> constexpr int kVec = 16 / sizeof(T);  // elements of 16 bytes
+
+// kVec<T> elements at p as float32, of which the first `have` exist (the others
+// read as 0 and are not touched).  p needs an element's alignment only: global
+// memory takes 16-byte accesses at any address, and one that is not aligned
+// costs a second cache line at most, less than accesses by elements.
+template <typename T>
+__device__ __forceinline__ void load_vec(const T *p, int have, float (&out)[kVec<T>]) {
+    T raw[kVec<T>];
+    if (have >= kVec<T>) {
+        __builtin_memcpy(raw, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) raw[i] = i < have ? p[i] : T(0);
+    }
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) out[i] = to_f32(raw[i]);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(T *p, int have, const float (&in)[kVec<T>]) {
+    T raw[kVec<T>];
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) raw[i] = from_f32<T>(in[i]);
+    if (have >= kVec<T>) {
+        __builtin_memcpy(p, raw, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i)
+            if (i < have) p[i] = raw[i];
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void load_f32(const float *p, int have, float (&out)[N]) {
+    if (have >= N) {
+        __builtin_memcpy(out, p, N * 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = i < have ? p[i] : 0.f;
+    }
+}
+
+// Sum over groups of G consecutive lanes (G a power of two up to 64), in every
+// lane.  Up to 16 lanes by moves within the vector ALU.
+template <int G> __device__ __forceinline__ float group_sum(float x) {
+#define SBC_STEP(ctrl) \
+    x += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), ctrl, 0xf, 0xf, true))
+    if constexpr (G > 1) SBC_STEP(0xB1);    // quad_perm [1, 0, 3, 2]
+    if constexpr (G > 2) SBC_STEP(0x4E);    // quad_perm [2, 3, 0, 1]
+    if constexpr (G > 4) SBC_STEP(0x141);   // row_half_mirror
+    if constexpr (G > 8) SBC_STEP(0x140);   // row_mirror
+#undef SBC_STEP
+    if constexpr (G > 16) x += __shfl_xor(x, 16);
+    if constexpr (G > 32) x += __shfl_xor(x, 32);
+    return x;
+}
+
+// Whether [a, a + na) and [b, b + nb) bytes share any.
+inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+inline bool known_dtype(sbc_dtype d) { return d == SBC_F32 || d == SBC_BF16; }
+inline size_t dtype_bytes(sbc_dtype d) { return d == SBC_F32 ? 4 : 2; }
+
+// ---------------------------------------------------------------- sbc_heads
+// Bytes from the first element of n tokens' heads to past their last one.
+inline size_t heads_bytes(const sbc_heads &x, int32_t heads, int32_t n, int32_t d, sbc_dtype dt) {
+    if (!x.data || heads <= 0 || n <= 0) return 0;
+    return ((size_t)(n - 1) * (size_t)x.token_stride + (size_t)(heads - 1) * (size_t)x.head_stride +
+            (size_t)d) * dtype_bytes(dt);
+}
+
+// An input: any strides that do not go backwards (0: the same for all).
+inline sbc_status check_heads(const sbc_heads *x, int32_t heads, int32_t n, int32_t d,
+                              sbc_dtype dt, const char *name) {
+    if (heads == 0 || n == 0) return SBC_OK;
+    if (!x || !x->data) return fail(SBC_ERR_INVALID_ARG, std::string(name) + " is null");
+    if (x->token_stride < 0 || x->head_stride < 0)
+        return fail(SBC_ERR_INVALID_ARG, std::string(name) + " has a negative stride");
+    if (((uintptr_t)x->data) % dtype_bytes(dt))
+        return fail(SBC_ERR_INVALID_ARG, std::string(name) + " is not aligned to its elements");
+    return SBC_OK;
+}
+
+// An output: besides, no two of its elements in one place.
+inline sbc_status check_out_heads(const sbc_heads *x, int32_t heads, int32_t n, int32_t d,
+                                  sbc_dtype dt, const char *name) {
+    SBC_TRY(check_heads(x, heads, n, d, dt, name));
+    if (heads == 0 || n == 0) return SBC_OK;
+    const int64_t ts = x->token_stride, hs = x->head_stride;
+    const bool tokens_outside = (heads == 1 || hs >= d) && (n == 1 || ts >= (heads - 1) * hs + d);
+    const bool heads_outside = (n == 1 || ts >= d) && (heads == 1 || hs >= (n - 1) * ts + d);
+    if (!tokens_outside && !heads_outside)
+        return fail(SBC_ERR_INVALID_ARG, std::string(name) + "'s elements overlap");
+    return SBC_OK;
+}
+
+// Whether two such arrays may share elements.  Heads of different arrays in the
+// same rows (parts of one projection) do not, where the rows' strides are equal.
+inline bool heads_overlap(const sbc_heads &a, int32_t a_heads, int32_t a_d, const sbc_heads &b,
+                          int32_t b_heads, int32_t b_d, int32_t n, sbc_dtype dt) {
+    if (!overlap(a.data, heads_bytes(a, a_heads, n, a_d, dt), b.data,
+                 heads_bytes(b, b_heads, n, b_d, dt)))
+        return false;
+    const int64_t ts = a.token_stride;
+    if (ts != b.token_stride || ts <= 0) return true;
+    const int64_t e = (int64_t)dtype_bytes(dt);
+    const int64_t off = (int64_t)((uintptr_t)b.data - (uintptr_t)a.data);
+    const int64_t span_a = (a_heads - 1) * a.head_stride + a_d;
+    const int64_t span_b = (b_heads - 1) * b.head_stride + b_d;
+    int64_t m = off % (ts * e);
+    if (m < 0) m += ts * e;
+    return !(m >= span_a * e && m + span_b * e <= ts * e);
+}
+
+}  // namespace sbc
