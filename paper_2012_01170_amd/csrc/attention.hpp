@@ -53,9 +53,13 @@ struct AttnPass {
     const int32_t *state_time;
     float *state_out;
     int32_t *time_out;
-    // x . y of every token, if wanted: x [n, heads, dc], dots [tiles, heads, n]
+    // The derivative by the rate (kSlope): with z_i = -d y_i / d rate, the sums of
+    // x_i . z_i over a workgroup's tokens and columns, [tiles, n_seg, heads]; carry1
+    // holds the states' own derivatives, gap [n_seg] the time over which `factor`
+    // decays
     sbc_heads x;
-    float *dots;
+    float *carry1, *gap;
+    double *slope;
 };
 
 __device__ __forceinline__ int32_t split_at(const AttnPass &p, int32_t b) {
@@ -166,8 +170,8 @@ template <int N> __device__ __forceinline__ void join8(const bf16x8 (&in)[N], fl
 // pieces of a row are permuted by its number, so that the same piece of rows in
 // turn lies in other banks.
 template <int D> __device__ __forceinline__ int tile_at(int row, int col) {
-    constexpr int kMask = D / 8 - 1;
-    return row * D + ((((col >> 3) ^ row) & kMask) << 3) + (col & 7);
+    constexpr int kMask = ((D / 8) & -(D / 8)) - 1;  // (as many low bits as stay inside the row)
+    return row * D + (((col >> 3) ^ (row & kMask)) << 3) + (col & 7);
 }
 // 8 columns of a row
 template <int D, int N>
@@ -200,86 +204,168 @@ __device__ __forceinline__ void frag_col(const bf16_t *tile, int plane, int row0
     }
 }
 
+// x, of which the compiler knows nothing: what is computed from it inside a loop
+// stays there.  (Comparisons of lanes with sizes, kept in scalar registers across the
+// chunks, took all of those and spilled.)
+__device__ __forceinline__ int in_loop(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // ---------------------------------------------------------------- loads
 // The tokens of a chunk in the pass' order: the first is `first`, `count` exist.
 template <bool kRev> __device__ __forceinline__ int64_t token_of(int32_t first, int l) {
     return kRev ? (int64_t)first - l : (int64_t)first + l;
 }
 
-// 16 bytes of a row at column col, zero past `d` and without a token
+// Loads of 16-byte pieces of rows.  Where the channels fill whole pieces (kWhole),
+// one that does not exist (past the channels, or of no token) is read from the
+// first row's start and zeroed on its way to LDS, so that no branch lies between the
+// loads, and a lane keeps its pieces' places in a full chunk; else pieces are read
+// by elements.
 template <typename T>
-__device__ __forceinline__ u32x4v load_raw(const T *row, int col, int d, bool there) {
-    u32x4v r{0, 0, 0, 0};
-    if (!there) return r;
-    if (col + kVec<T> <= d) {
-        __builtin_memcpy(&r, row + col, 16);
-    } else {
-        T raw[kVec<T>];
+__device__ __forceinline__ u32x4v load_elements(const T *row, int col, int d, bool there) {
+    T raw[kVec<T>];
 #pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) raw[i] = col + i < d ? row[col + i] : T(0);
-        __builtin_memcpy(&r, raw, 16);
-    }
+    for (int i = 0; i < kVec<T>; ++i) raw[i] = there && col + i < d ? row[col + i] : T(0);
+    u32x4v r;
+    __builtin_memcpy(&r, raw, 16);
     return r;
 }
 
-// A chunk of 64 rows x D columns on its way to LDS, kSteps 16-byte pieces a lane
-template <typename T, int D> struct Staged {
-    static constexpr int kPerRow = D / kVec<T>;
-    static constexpr int kRows = kAttnThreads / kPerRow;
-    static constexpr int kSteps = kChunk / kRows;
-    u32x4v raw[kSteps];
+// One head's rows of an array, from the lowest token of a chunk on: row l of the
+// pass' order is `rows - 1 - l` (kRev) or l tokens above it.
+template <typename T> struct Rows {
+    const T *base;
+    int64_t stride;
+    __device__ __forceinline__ Rows(const sbc_heads &x, int32_t head, int32_t col0)
+        : base(static_cast<const T *>(x.data) + (int64_t)head * x.head_stride + col0),
+          stride(x.token_stride) {}
+};
 
-    template <bool kRev>
-    __device__ __forceinline__ void load(const sbc_heads &x, int32_t head, int32_t first,
-                                         int count, int col0, int d) {
-        const T *base = static_cast<const T *>(x.data) + (int64_t)head * x.head_stride + col0;
-        const int col = (threadIdx.x % kPerRow) * kVec<T>;
+// A chunk of 64 rows x D columns on its way to LDS, kSteps 16-byte pieces a lane
+template <typename T, int D, bool kWhole, bool kRev> struct Staged {
+    static constexpr int kPerRow = D / kVec<T>;
+    static constexpr int kSteps = kChunk * kPerRow / kAttnThreads;
+    static_assert(kChunk * kPerRow % kAttnThreads == 0, "pieces");
+    u32x4v raw[kSteps];
+    uint32_t off[kSteps];  // the pieces' bytes in a full chunk (kWhole: strides below 2^22)
+
+    __device__ __forceinline__ static int row_of(int s, int tid) {
+        return (s * kAttnThreads + tid) / kPerRow;
+    }
+    __device__ __forceinline__ static int col_of(int s, int tid) {
+        return (s * kAttnThreads + tid) % kPerRow * kVec<T>;
+    }
+    __device__ __forceinline__ Staged(const Rows<T> &x, int width) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const int l = s * kRows + threadIdx.x / kPerRow;
-            raw[s] = load_raw<T>(base + token_of<kRev>(first, l) * x.token_stride, col, d - col0,
-                                 l < count);
+            const int l = row_of(s, threadIdx.x), col = col_of(s, threadIdx.x);
+            off[s] = ((kRev ? kChunk - 1 - l : l) * (uint32_t)x.stride + (col < width ? col : 0)) *
+                     (uint32_t)sizeof(T);
         }
     }
-    __device__ __forceinline__ void store(bf16_t *tile) const {
-        const int col = (threadIdx.x % kPerRow) * kVec<T>;
+    // the chunk of `count` tokens from token `lowest` on; `width` columns exist
+    __device__ __forceinline__ void load(const Rows<T> &x, int32_t lowest, int count, int width) {
+        const T *base = x.base + (int64_t)lowest * x.stride;
+        if (kWhole && count == kChunk) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+                __builtin_memcpy(&raw[s], reinterpret_cast<const char *>(base) + off[s], 16);
+        } else {
+            const int tid = in_loop(threadIdx.x);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int l = row_of(s, tid), col = col_of(s, tid);
+                const T *row = base + (int64_t)(kRev ? count - 1 - l : l) * x.stride;
+                if constexpr (kWhole)
+                    __builtin_memcpy(&raw[s], l < count && col < width ? row + col : base, 16);
+                else
+                    raw[s] = load_elements<T>(row, col, width, l < count);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(bf16_t *tile, int count, int width) {
+        if (kWhole && (count < kChunk || width < D)) {
+            const int tid = in_loop(threadIdx.x);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const bool ok = row_of(s, tid) < count && col_of(s, tid) < width;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[s][i] = ok ? raw[s][i] : 0u;
+            }
+        }
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const int at = tile_at<D>(s * kRows + threadIdx.x / kPerRow, col);
+            const int at = tile_at<D>(row_of(s, threadIdx.x), col_of(s, threadIdx.x));
             if constexpr (sizeof(T) == 2) {
                 *reinterpret_cast<u32x4v *>(tile + at) = raw[s];
             } else {
-                uint32_t h[2], m[2], l[2];
+                uint32_t h[2], m[2], lo[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    split2(__uint_as_float(raw[s][2 * i]), __uint_as_float(raw[s][2 * i + 1]), h[i],
-                           m[i], l[i]);
+                    split2(__uint_as_float(raw[s][2 * i]), __uint_as_float(raw[s][2 * i + 1]),
+                           h[i], m[i], lo[i]);
                 constexpr int kPlane = kChunk * D;
                 *reinterpret_cast<uint2 *>(tile + at) = uint2{h[0], h[1]};
                 *reinterpret_cast<uint2 *>(tile + kPlane + at) = uint2{m[0], m[1]};
-                *reinterpret_cast<uint2 *>(tile + 2 * kPlane + at) = uint2{l[0], l[1]};
+                *reinterpret_cast<uint2 *>(tile + 2 * kPlane + at) = uint2{lo[0], lo[1]};
             }
         }
     }
 };
 
-// 8 columns of a row in global memory as an operand's parts
-template <typename T>
-__device__ __forceinline__ void frag_global(const T *row, int col, int d, bool there,
-                                            bf16x8 (&out)[kParts<T>]) {
-    if constexpr (sizeof(T) == 2) {
-        out[0] = __builtin_bit_cast(bf16x8, load_raw<T>(row, col, d, there));
-    } else {
-        const u32x4v lo = load_raw<T>(row, col, d, there), hi = load_raw<T>(row, col + 4, d, there);
-        float x[8];
+// Each lane's own row (token `mine` of the chunk) as an operand of D columns:
+// columns 32 k + 8 g .. + 7 of k-step k
+template <typename T, int D, bool kWhole, bool kRev> struct RowFrag {
+    static constexpr int kRaw = 8 / kVec<T>;
+    u32x4v raw[D / 32][kRaw];
+
+    __device__ __forceinline__ void load(const Rows<T> &x, int32_t lowest, int count, int width,
+                                         int mine) {
+        const T *base = x.base + (int64_t)lowest * x.stride;
+        const int g = (threadIdx.x & 63) >> 4;
+        const bool there = mine < count;
+        const int up = kRev ? count - 1 - mine : mine;
+        const T *row = kWhole ? base + (uint32_t)((there ? up : 0) * (uint32_t)x.stride + 8 * g)
+                              : base + (int64_t)(there ? up : 0) * x.stride + 8 * g;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = __uint_as_float(lo[i]);
-            x[4 + i] = __uint_as_float(hi[i]);
-        }
-        split8<3>(x, out);
+        for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+            for (int i = 0; i < kRaw; ++i) {
+                const int col = 32 * k + i * kVec<T>;
+                if constexpr (kWhole)
+                    __builtin_memcpy(&raw[k][i], col + 8 * g < width ? row + col : base, 16);
+                else
+                    raw[k][i] = load_elements<T>(row, col, width - 8 * g, there);
+            }
     }
-}
+    __device__ __forceinline__ void parts(bf16x8 (&out)[D / 32][kParts<T>], int count, int width,
+                                          int mine) {
+        if (kWhole && (count < kChunk || width < D)) {
+            const int g = in_loop((threadIdx.x & 63) >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+                for (int i = 0; i < kRaw; ++i) {
+                    const bool ok = mine < count && 32 * k + 8 * g + i * kVec<T> < width;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) raw[k][i][e] = ok ? raw[k][i][e] : 0u;
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            if constexpr (sizeof(T) == 2) {
+                out[k][0] = __builtin_bit_cast(bf16x8, raw[k][0]);
+            } else {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw[k][i / 4][i % 4]);
+                split8<3>(x, out[k]);
+            }
+        }
+    }
+};
 
 // ---------------------------------------------------------------- state
 // The state's tiles [DA x DCT] over the four waves: a wave has 16 columns and
@@ -296,31 +382,67 @@ template <int DA, int DCT> struct StateTiles {
     __device__ __forceinline__ static int row(int u) { return row0(u) + 4 * ((threadIdx.x & 63) >> 4); }
 };
 
-// acc += sum over the chunk's tokens of w_j b_j c_j^T
-template <typename T, int DA, int DCT>
+// acc += sum over the chunk's tokens of w_j b_j c_j^T, with kSlope also acc1 += .. w1_j ..
+template <typename T, int DA, int DCT, bool kSlope>
 __device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct, const float *w,
-                                          floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
+                                          const float *w1,
+                                          floatx4 (&acc)[StateTiles<DA, DCT>::kTiles],
+                                          floatx4 (&acc1)[StateTiles<DA, DCT>::kTiles]) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int s = 0; s < kChunk / 32; ++s) {
-        bf16x8 raw[NP], cw[3];
+        bf16x8 raw[NP], cw[3], cw1[3];
         frag_col<DCT, NP>(ct, kChunk * DCT, 32 * s, S::col0(), raw);
-        float x[8];
+        float x[8], y[8];
         join8<NP>(raw, x);
+        auto weigh = [&](const float *weights, bf16x8(&out)[3]) {
+            const floatx4 lo = *reinterpret_cast<const floatx4 *>(weights + 32 * s + 4 * g);
+            const floatx4 hi = *reinterpret_cast<const floatx4 *>(weights + 32 * s + 16 + 4 * g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] *= w[32 * s + 4 * g + e];
-            x[4 + e] *= w[32 * s + 16 + 4 * g + e];
-        }
-        split8<3>(x, cw);
+            for (int e = 0; e < 4; ++e) {
+                y[e] = x[e] * lo[e];
+                y[4 + e] = x[4 + e] * hi[e];
+            }
+            split8<3>(y, out);
+        };
+        weigh(w, cw);
+        if constexpr (kSlope) weigh(w1, cw1);
 #pragma unroll
         for (int u = 0; u < S::kTiles; ++u) {
             bf16x8 b[NP];
             frag_col<DA, NP>(bt, kChunk * DA, 32 * s, S::row0(u), b);
             mma<NP, 3>(b, cw, acc[u]);
+            if constexpr (kSlope) mma<NP, 3>(b, cw1, acc1[u]);
         }
+    }
+}
+
+// The state in LDS as parts, column after column of c, its rows (the channels of a)
+// the contraction's axis
+template <int DA, int DCT, int NS>
+__device__ __forceinline__ void store_state(bf16_t *st,
+                                            const floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
+    using S = StateTiles<DA, DCT>;
+#pragma unroll
+    for (int u = 0; u < S::kTiles; ++u) {
+        const int o = tile_at<DA>(S::col(), S::row(u));
+        uint32_t w[3][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float x = acc[u][2 * i], z = acc[u][2 * i + 1];
+            if constexpr (NS == 3) {
+                split2(x, z, w[0][i], w[1][i], w[2][i]);
+            } else {
+                w[0][i] = pack_bf16(x, z);
+                w[1][i] = pack_bf16(x - __uint_as_float(w[0][i] << 16),
+                                    z - __uint_as_float(w[0][i] & 0xFFFF0000u));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            *reinterpret_cast<uint2 *>(st + i * DCT * DA + o) = uint2{w[i][0], w[i][1]};
     }
 }
 

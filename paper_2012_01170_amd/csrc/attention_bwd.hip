@@ -2,19 +2,10 @@
 //
 //   dq: (dO, v, k) along the sequence       dk: (v, dO, q) back along it
 //   dv: (k, q, dO) back along it
-//
-// The rates' gradient.  With P_ij the term of a pair (its decay, both products
-// and the scale), drate = - sum of (t_i - t_j) P_ij.  The sum of P_ij over the
-// pairs that cross a point between two tokens is a flow: it grows by
-// k_j . dk_j = sum over i of P_ij behind token j and falls by q_i . dq_i = sum
-// over j of P_ij behind token i, so that
-//   sum of (t_i - t_j) P_ij = sum over gaps of gap * flow
-//     = X (t_end - t_before) + sum over m of (k_m . dk_m - q_m . dq_m) (t_end - t_m)
-// for a segment's tokens m of one sequence, t_end the last one's time, with the
-// flow X into the segment, the product of the states that meet there (the sum
-// of k v^T from before it and of q dO^T from behind).  The passes leave the
-// products of a token; starting anew from X in each segment keeps their rounding
-// from adding up along the sequence.
+// and the rates' gradient beside dk: drate = - sum of (t_i - t_j) times the terms of
+// y = dk summed over j against k_j, the pass' kSlope.  (From the products k . dk and
+// q . dq of the tokens alone, as a flow that each token adds to and takes from, it
+// would lose what the flow's rounding gains over a segment: 4e-6 to 1e-5.)
 #include "attention_host.hpp"
 #include "attention_kernels.hpp"
 
@@ -23,72 +14,24 @@ namespace {
 
 constexpr int kBwdPerCu = 2;
 
-struct RatesArgs {
-    AttnPass p;                  // the sequences, times and segments
-    const float *before, *behind;  // states that come into segments along and back
-    int32_t elements;            // of a state
-    const float *dot_q, *dot_k;  // [tiles, heads, n]
-    int32_t tiles;
-    double *part;                // [n_seg, heads]
-};
-
-// Sum over a workgroup of 256 in its first thread.
-__device__ __forceinline__ double block_sum(double x, double *buf) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return (buf[0] + buf[1]) + (buf[2] + buf[3]);
-}
-
-__global__ __launch_bounds__(256) void attn_rates_kernel(RatesArgs r) {
-    __shared__ double buf[4];
-    const AttnPass &p = r.p;
-    const int head = blockIdx.x % p.heads, seg = blockIdx.x / p.heads;
-    const int32_t g0 = seg * p.seg_len;
-    const int32_t g1 = seg == p.n_seg - 1 ? p.n : g0 + p.seg_len;
-    const int32_t b_new = first_from(p, g0);
-    const bool came_in = b_new > 0 && split_at(p, b_new) > g0;
-    const float rate2 = p.rates[head] * kLog2E;
-    double x = 0.0;
-    if (came_in) {
-        const float *f = r.before + ((int64_t)seg * p.heads + head) * p.state_stride;
-        const float *d = r.behind + ((int64_t)(seg - 1) * p.heads + head) * p.state_stride;
-        for (int i = threadIdx.x; i < r.elements; i += 256) x += (double)f[i] * (double)d[i];
-        x = block_sum(x, buf) *
-            (double)(p.scale * decay(rate2, elapsed<false>(time_at(p, g0), time_at(p, g0 - 1))));
-    }
-    double sum = 0.0;
-    for (int32_t b = came_in ? b_new - 1 : b_new; b < p.n_batch; ++b) {
-        const int32_t s = split_at(p, b), e = split_at(p, b + 1);
-        if (b >= b_new && s >= g1) break;
-        const int32_t lo = s > g0 ? s : g0, hi = e < g1 ? e : g1;
-        if (lo >= hi) continue;
-        const int32_t t_end = time_at(p, hi - 1);
-        if (b < b_new && threadIdx.x == 0)
-            sum += x * (double)elapsed<false>(t_end, time_at(p, g0 - 1));
-        for (int32_t m = lo + (int32_t)threadIdx.x; m < hi; m += 256) {
-            float c = 0.f;
-            for (int ti = 0; ti < r.tiles; ++ti) {
-                const int64_t at = ((int64_t)ti * p.heads + head) * p.n + m;
-                c += r.dot_k[at] - r.dot_q[at];
-            }
-            sum += (double)c * (double)elapsed<false>(t_end, time_at(p, m));
-        }
-    }
-    sum = block_sum(sum, buf);
-    if (threadIdx.x == 0) r.part[(int64_t)seg * p.heads + head] = sum;
-}
-
-__global__ __launch_bounds__(256) void attn_rates_sum_kernel(const double *__restrict__ part,
-                                                             int32_t n_seg, int32_t heads,
-                                                             float *__restrict__ drates) {
+// drates[h] = - the sum of the workgroups' parts [parts, heads], in order
+__global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restrict__ part,
+                                                         int32_t parts, int32_t heads,
+                                                         float *__restrict__ drates) {
     __shared__ double buf[4];
     double s = 0.0;
-    for (int g = threadIdx.x; g < n_seg; g += 256) s += part[(int64_t)g * heads + blockIdx.x];
-    s = block_sum(s, buf);
-    if (threadIdx.x == 0) drates[blockIdx.x] = (float)-s;
+    for (int i = threadIdx.x; i < parts; i += 256) s += part[(int64_t)i * heads + blockIdx.x];
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) s += __shfl_xor(s, m);
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) drates[blockIdx.x] = (float)-((buf[0] + buf[1]) + (buf[2] + buf[3]));
+}
+
+// Columns of a tile: of float32 and 128 channels, a state and its derivative leave
+// LDS room for 32.
+int bwd_tile(int32_t da, int32_t dc, bool slope, sbc_dtype dtype) {
+    return slope && dtype == SBC_F32 && da > 96 ? 32 : attn_tile(dc);
 }
 
 void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, int32_t *seg_len,
@@ -98,8 +41,8 @@ void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, int32_t
 }
 
 struct BwdSpace {
-    float *before, *behind, *f_before, *f_behind, *dot_q, *dot_k;
-    double *part;
+    float *before, *behind, *behind1, *f_before, *f_behind, *gap;
+    double *slope;
     size_t bytes;
 };
 BwdSpace carve(void *ws, int32_t n, int32_t heads, int32_t dk, int32_t dv, int32_t n_seg) {
@@ -108,30 +51,37 @@ BwdSpace carve(void *ws, int32_t n, int32_t heads, int32_t dk, int32_t dv, int32
     const size_t states = (size_t)n_seg * heads * state_stride(dk, dv);
     s.before = c.take<float>(states);
     s.behind = c.take<float>(states);
+    s.behind1 = c.take<float>(states);
     s.f_before = c.take<float>((size_t)n_seg * heads);
     s.f_behind = c.take<float>((size_t)n_seg * heads);
-    s.dot_q = c.take<float>((size_t)attn_tiles(dk) * heads * n);
-    s.dot_k = c.take<float>((size_t)attn_tiles(dk) * heads * n);
-    s.part = c.take<double>((size_t)n_seg * heads);
+    s.gap = c.take<float>(n_seg);
+    s.slope = c.take<double>((size_t)((dk + 31) / 32) * n_seg * heads);
     s.bytes = c.used;
     return s;
 }
 
-template <typename T, bool kRev> void states(const AttnPass &p, hipStream_t stream) {
-    pass_dispatch(p.da, attn_tile(p.dc), [&](auto da, auto dct) {
-        hipLaunchKernelGGL((attn_state_kernel<T, decltype(da)::value, decltype(dct)::value, kRev>),
+template <typename T, bool kRev, bool kSlope>
+void states(AttnPass p, bool whole_rows, hipStream_t stream) {
+    p.tiles = attn_tiles(p.dc);
+    pass_dispatch<T>(p.da, attn_tile(p.dc), whole_rows, [&](auto da, auto dct, auto whole) {
+        hipLaunchKernelGGL((attn_state_kernel<T, decltype(da)::value, decltype(dct)::value,
+                                              decltype(whole)::value, kRev, kSlope>),
                            pass_grid(p), dim3(kAttnThreads), 0, stream, p);
     });
-    hipLaunchKernelGGL(attn_scan_kernel<kRev>,
-                       dim3((unsigned)grid_for(p.state_stride, 64), (unsigned)p.heads), dim3(256),
-                       0, stream, p.carry, p.factor, p.n_seg, p.heads, p.state_stride);
+    hipLaunchKernelGGL((attn_scan_kernel<kRev, kSlope>), scan_grid(p), dim3(256), 0, stream, p);
 }
 
-template <typename T, bool kRev> void pass(const AttnPass &p, hipStream_t stream) {
-    pass_dispatch(p.da, attn_tile(p.dc), [&](auto da, auto dct) {
-        hipLaunchKernelGGL(
-            (attn_pass_kernel<T, decltype(da)::value, decltype(dct)::value, kRev, 3>),
-            pass_grid(p), dim3(kAttnThreads), 0, stream, p);
+// (dk takes three parts also without the rates' gradient, which must not change it)
+template <typename T, bool kRev, int NS, bool kSlope>
+void pass(AttnPass p, bool whole_rows, hipStream_t stream) {
+    const int dct = bwd_tile(p.da, p.dc, kSlope, sizeof(T) == 4 ? SBC_F32 : SBC_BF16);
+    p.tiles = (p.dc + dct - 1) / dct;
+    pass_dispatch<T>(p.da, dct, whole_rows, [&](auto da, auto dct, auto whole) {
+        constexpr int DA = decltype(da)::value, DCT = decltype(dct)::value;
+        if constexpr (!(kSlope && sizeof(T) == 4 && DA > 96 && DCT > 32))
+            hipLaunchKernelGGL(
+                (attn_pass_kernel<T, DA, DCT, decltype(whole)::value, kRev, NS, kSlope>),
+                pass_grid(p), dim3(kAttnThreads), 0, stream, p);
     });
 }
 
@@ -151,6 +101,7 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     base.state_stride = state_stride(a->dk, a->dv);
     backward_segments(a->n, a->heads, a->dk, a->dv, &base.seg_len, &base.n_seg);
     const BwdSpace s = carve(workspace, a->n, a->heads, a->dk, a->dv, base.n_seg);
+    const bool whole = whole_rows(a, {&dO, &q, &k, &v});
 
     auto make = [&](const sbc_heads &x, const sbc_heads &y, const sbc_heads &z,
                     const sbc_heads &out, bool keys, bool back) {
@@ -162,9 +113,10 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
         p.y = out;
         p.da = keys ? a->dk : a->dv;
         p.dc = keys ? a->dv : a->dk;
-        p.tiles = attn_tiles(p.dc);
         p.carry = back ? s.behind : s.before;
+        p.carry1 = s.behind1;
         p.factor = back ? s.f_behind : s.f_before;
+        p.gap = s.gap;
         // states lie as [dk, dv]
         p.carry_i = keys ? a->dv : 1;
         p.carry_j = keys ? 1 : a->dv;
@@ -172,31 +124,32 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     };
     if (base.n_seg > 1) {
         trace_before("attn_bwd_state", stream);
-        states<T, false>(make(q, k, v, q, true, false), stream);
-        states<T, true>(make(k, q, dO, k, true, true), stream);
+        states<T, false, false>(make(q, k, v, q, true, false), whole, stream);
+        const AttnPass back = make(k, q, dO, k, true, true);
+        if (drates)
+            states<T, true, true>(back, whole, stream);
+        else
+            states<T, true, false>(back, whole, stream);
         trace_after("attn_bwd_state", stream);
     }
-    AttnPass pq = make(dO, v, k, dq, false, false);
-    AttnPass pk = make(v, dO, q, dk, false, true);
-    AttnPass pv = make(k, q, dO, dv, true, true);
-    if (drates) {
-        pq.x = q;
-        pq.dots = s.dot_q;
-        pk.x = k;
-        pk.dots = s.dot_k;
-    }
+    constexpr int NS = sizeof(T) == 4 ? 3 : 2;
     trace_before("attn_bwd", stream);
-    pass<T, false>(pq, stream);
-    pass<T, true>(pk, stream);
-    pass<T, true>(pv, stream);
+    pass<T, false, NS, false>(make(dO, v, k, dq, false, false), whole, stream);
+    pass<T, true, NS, false>(make(k, q, dO, dv, true, true), whole, stream);
+    AttnPass pk = make(v, dO, q, dk, false, true);
+    if (drates) {
+        pk.x = k;
+        pk.slope = s.slope;
+        pass<T, true, 3, true>(pk, whole, stream);
+    } else {
+        pass<T, true, 3, false>(pk, whole, stream);
+    }
     trace_after("attn_bwd", stream);
     if (drates) {
         trace_before("attn_rates", stream);
-        RatesArgs r{base, s.before, s.behind, a->dk * a->dv, s.dot_q, s.dot_k, pq.tiles, s.part};
-        hipLaunchKernelGGL(attn_rates_kernel, dim3((unsigned)(base.n_seg * base.heads)), dim3(256),
-                           0, stream, r);
-        hipLaunchKernelGGL(attn_rates_sum_kernel, dim3((unsigned)base.heads), dim3(256), 0, stream,
-                           s.part, base.n_seg, base.heads, drates);
+        const int dct = bwd_tile(a->dv, a->dk, true, a->dtype);
+        hipLaunchKernelGGL(attn_rates_kernel, dim3((unsigned)base.heads), dim3(256), 0, stream,
+                           s.slope, (a->dk + dct - 1) / dct * base.n_seg, base.heads, drates);
         trace_after("attn_rates", stream);
     }
     SBC_LAUNCH_CHECK();

@@ -2,6 +2,8 @@
 // token axis.
 #pragma once
 
+#include <initializer_list>
+
 #include "attention.hpp"
 
 namespace sbc {
@@ -32,9 +34,18 @@ inline sbc_status check_sequences(const sbc_attention *a) {
 inline int attn_tile(int32_t dc) { return dc <= 32 ? 32 : 64; }
 inline int32_t attn_tiles(int32_t dc) { return (dc + attn_tile(dc) - 1) / attn_tile(dc); }
 
+// Whether rows are read in whole 16-byte pieces at 32-bit offsets within a chunk.
+inline bool whole_rows(const sbc_attention *a, std::initializer_list<const sbc_heads *> arrays) {
+    const int v = a->dtype == SBC_F32 ? 4 : 8;
+    if (a->dk % v || a->dv % v) return false;
+    for (const sbc_heads *x : arrays)
+        if (x->token_stride >= 1 << 22) return false;
+    return true;
+}
+
 // Segments of the token axis: as many as give every CU `per_cu` workgroups, of no
 // fewer than kLeastSeg tokens.
-constexpr int32_t kLeastSeg = 256;
+constexpr int32_t kLeastSeg = 128;
 inline void attn_segments(int32_t n, int64_t blocks_a_segment, int per_cu, int32_t *seg_len,
                           int32_t *n_seg) {
     const int64_t want = ((int64_t)per_cu * device_cus() + blocks_a_segment - 1) / blocks_a_segment;

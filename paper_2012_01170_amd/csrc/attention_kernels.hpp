@@ -3,7 +3,7 @@
 
 #include <type_traits>
 
-#include "attention.hpp"
+#include "attention_host.hpp"
 
 namespace sbc {
 namespace {
@@ -13,13 +13,13 @@ namespace {
 // the time of the last of them.  Grid: segments x heads x column tiles.  A
 // sequence's tokens are taken from the end back, and no further than their decay
 // lasts: the weights of earlier ones are exactly 0.
-template <typename T, int DA, int DCT, bool kRev>
+template <typename T, int DA, int DCT, bool kWhole, bool kRev, bool kSlope>
 __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     __shared__ alignas(16) bf16_t bt[NP * kChunk * DA];
     __shared__ alignas(16) bf16_t ct[NP * kChunk * DCT];
-    __shared__ float wj[kChunk];
+    __shared__ alignas(16) float wj[kChunk], wj1[kSlope ? kChunk : 4];
     __shared__ float last_w;
     const int tile = blockIdx.x % p.tiles;
     const int head = (blockIdx.x / p.tiles) % p.heads;
@@ -54,40 +54,50 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
         return;
     }
     const int32_t end = time_at(p, kRev ? g0 : g1 - 1);  // the time of the sum
-    if (first)
-        *factor = !passes ? kFresh
-                          : step_factor(rate, elapsed<kRev>(end, time_at(p, kRev ? g1 : g0 - 1)));
+    if (first) {
+        const float dt = passes ? elapsed<kRev>(end, time_at(p, kRev ? g1 : g0 - 1)) : 0.f;
+        *factor = passes ? step_factor(rate, dt) : kFresh;
+        if (kSlope && head == 0) p.gap[seg] = dt;
+    }
 
-    floatx4 acc[S::kTiles];
+    floatx4 acc[S::kTiles], acc1[S::kTiles];
 #pragma unroll
-    for (int u = 0; u < S::kTiles; ++u) acc[u] = floatx4{0.f, 0.f, 0.f, 0.f};
-    Staged<T, DA> sb;
-    Staged<T, DCT> sc;
-    // chunks from the end of the sum: the last in the pass' order, from its last token
-    for (int32_t done = 0; done < hi - lo; done += kChunk) {
-        const int32_t left = hi - lo - done;
+    for (int u = 0; u < S::kTiles; ++u) acc[u] = acc1[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // row l of a chunk is l tokens before the chunk's last in the pass' order
+    const Rows<T> rb(p.b, head, 0), rc(p.c, head, dc0);
+    Staged<T, DA, kWhole, !kRev> sb(rb, p.da);
+    Staged<T, DCT, kWhole, !kRev> sc(rc, p.dc - dc0);
+    int32_t t_next = 0;
+    auto fetch = [&](int32_t at) {  // the chunk whose last token lies `at` before the end
+        const int32_t left = hi - lo - at;
         const int count = left < kChunk ? left : kChunk;
-        const int32_t newest = kRev ? lo + done : hi - 1 - done;
-        // (token l of the chunk is l tokens before the newest in the pass' order)
-        sb.template load<!kRev>(p.b, head, newest, count, 0, p.da);
-        sc.template load<!kRev>(p.c, head, newest, count, dc0, p.dc);
+        const int32_t lowest = kRev ? lo + at : hi - at - count;
+        sb.load(rb, lowest, count, p.da);
+        sc.load(rc, lowest, count, p.dc - dc0);
+        if ((int)threadIdx.x < count)
+            t_next = time_at(p, kRev ? lowest + threadIdx.x : lowest + count - 1 - threadIdx.x);
+    };
+    fetch(0);
+    for (int32_t at = 0; at < hi - lo; at += kChunk) {
+        const int count = hi - lo - at < kChunk ? hi - lo - at : kChunk;
         if (threadIdx.x < kChunk) {
             const int l = threadIdx.x;
-            float w = 0.f;
-            if (l < count)
-                w = decay(rate2, elapsed<kRev>(end, time_at(p, (int32_t)token_of<!kRev>(newest, l))));
+            const float dt = elapsed<kRev>(end, t_next);
+            const float w = l < count ? decay(rate2, dt) : 0.f;
             wj[l] = w;
+            if constexpr (kSlope) wj1[l] = w * dt;
             if (l == count - 1) last_w = w;
         }
-        sb.store(bt);
-        sc.store(ct);
+        sb.store(bt, count, p.da);
+        sc.store(ct, count, p.dc - dc0);
         __syncthreads();
         const bool spent = last_w == 0.f;
-        add_chunk<T, DA, DCT>(bt, ct, wj, acc);
+        if (at + kChunk < hi - lo && !spent) fetch(at + kChunk);
+        add_chunk<T, DA, DCT, kSlope>(bt, ct, wj, wj1, acc, acc1);
         __syncthreads();
         if (spent) break;
     }
-    float *out = p.carry + ((int64_t)seg * p.heads + head) * p.state_stride;
+    const int64_t place = ((int64_t)seg * p.heads + head) * p.state_stride;
     const int col = dc0 + S::col();
     const float *s0 = nullptr;
     float kept = 0.f;
@@ -104,7 +114,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
                 if (row < p.da) {
                     float v = acc[u][r];
                     if (s0) v += kept * s0[(int64_t)row * p.dc + col];
-                    out[(int64_t)row * p.carry_i + (int64_t)col * p.carry_j] = v;
+                    const int64_t e = (int64_t)row * p.carry_i + (int64_t)col * p.carry_j;
+                    p.carry[place + e] = v;
+                    if constexpr (kSlope) p.carry1[place + e] = acc1[u][r];
                 }
             }
     }
@@ -112,70 +124,85 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
 
 // The states that segments start from, from the sums that they hand on, in place:
 // carry[next] = sum[g] + carry[g] decayed by factor[g], the first term alone where
-// a sequence starts in g.  16 groups of 16 lanes share the segments of 4 x 16
-// values: each joins its run of segments, the runs are joined in LDS, and each
-// run is gone through again from what comes in.  (A place that nothing hands on
-// to holds whatever its sum's place held; nothing starts from it.)
-template <bool kRev>
-__global__ __launch_bounds__(256) void attn_scan_kernel(float *__restrict__ carry,
-                                                        const float *__restrict__ factor,
-                                                        int32_t n_seg, int32_t heads,
-                                                        int64_t state_stride) {
-    __shared__ floatx4 sums[16][16];
-    __shared__ float through[16][16];
+// a sequence starts in g (and of their derivatives, carry1[next] = sum1[g] +
+// (carry1[g] + gap[g] carry[g]) decayed).  16 groups of 16 lanes share the segments
+// of 4 x 16 values: each joins its run of segments, the runs are joined in LDS, and
+// each run is gone through again from what comes in.  (A place that nothing hands
+// on to holds whatever its sum's place held; nothing starts from it.)
+template <bool kRev, bool kSlope>
+__global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass p) {
+    __shared__ floatx4 sums[kSlope ? 2 : 1][16][16];
+    __shared__ float through[2][16];
     const int lane = threadIdx.x % 16, run = threadIdx.x / 16;
     const int head = blockIdx.y;
     const int64_t e = ((int64_t)blockIdx.x * 16 + lane) * 4;
-    const bool there = e < state_stride;
-    const int per = (n_seg + 15) / 16;
-    const int s0 = run * per, s1 = s0 + per < n_seg ? s0 + per : n_seg;
-    auto place = [&](int s) { return (int64_t)(kRev ? n_seg - 1 - s : s) * heads + head; };
-    auto step = [](floatx4 c, floatx4 sum, float f) {
+    const bool there = e < p.state_stride;
+    const int per = (p.n_seg + 15) / 16;
+    const int s0 = run * per, s1 = s0 + per < p.n_seg ? s0 + per : p.n_seg;
+    struct State {
+        floatx4 c, c1;
+    };
+    auto seg_of = [&](int s) { return kRev ? p.n_seg - 1 - s : s; };
+    auto at = [&](float *x, int s) {
+        return reinterpret_cast<floatx4 *>(
+            x + ((int64_t)seg_of(s) * p.heads + head) * p.state_stride + e);
+    };
+    auto step = [](const State &x, const State &sum, float f, float gap) {
+        State y = sum;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += apply_factor(f, c[i]);
-        return sum;
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kSlope) y.c1[i] += apply_factor(f, fmaf(gap, x.c[i], x.c1[i]));
+            y.c[i] += apply_factor(f, x.c[i]);
+        }
+        return y;
     };
     constexpr int kAhead = 8;
-    floatx4 c{0.f, 0.f, 0.f, 0.f};
-    float f_run = 0.f;  // the run's decay
+    State v[kAhead];
+    float f[kAhead], gap[kAhead];
+    auto fetch = [&](int s) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (s + k < s1) {
+                v[k].c = *at(p.carry, s + k);
+                if constexpr (kSlope) v[k].c1 = *at(p.carry1, s + k);
+                f[k] = p.factor[(int64_t)seg_of(s + k) * p.heads + head];
+                gap[k] = kSlope ? p.gap[seg_of(s + k)] : 0.f;
+            }
+    };
+    State x{};
+    float f_run = 0.f, gap_run = 0.f;  // the run's decay and time
     if (there) {
         for (int s = s0; s < s1; s += kAhead) {
-            floatx4 v[kAhead];
-            float f[kAhead];
+            fetch(s);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
                 if (s + k < s1) {
-                    v[k] = *reinterpret_cast<const floatx4 *>(carry + place(s + k) * state_stride + e);
-                    f[k] = factor[place(s + k)];
-                }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (s + k < s1) {
-                    c = step(c, v[k], f[k]);
+                    x = step(x, v[k], f[k], gap[k]);
                     f_run = join_factors(f_run, f[k]);
+                    gap_run += gap[k];
                 }
         }
-        sums[run][lane] = c;
-        through[run][lane] = f_run;
+        sums[0][run][lane] = x.c;
+        if constexpr (kSlope) sums[1][run][lane] = x.c1;
+        through[0][run] = f_run;
+        through[1][run] = gap_run;
     }
     __syncthreads();
     if (!there) return;
-    c = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int r = 0; r < run; ++r) c = step(c, sums[r][lane], through[r][lane]);
+    x = State{};
+    for (int r = 0; r < run; ++r) {
+        State sum{sums[0][r][lane], floatx4{}};
+        if constexpr (kSlope) sum.c1 = sums[1][r][lane];
+        x = step(x, sum, through[0][r], through[1][r]);
+    }
     for (int s = s0; s < s1; s += kAhead) {
-        floatx4 v[kAhead];
-        float f[kAhead];
+        fetch(s);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
             if (s + k < s1) {
-                v[k] = *reinterpret_cast<const floatx4 *>(carry + place(s + k) * state_stride + e);
-                f[k] = factor[place(s + k)];
-            }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (s + k < s1) {
-                *reinterpret_cast<floatx4 *>(carry + place(s + k) * state_stride + e) = c;
-                c = step(c, v[k], f[k]);
+                *at(p.carry, s + k) = x.c;
+                if constexpr (kSlope) *at(p.carry1, s + k) = x.c1;
+                x = step(x, v[k], f[k], gap[k]);
             }
     }
 }
@@ -187,15 +214,21 @@ __global__ __launch_bounds__(256) void attn_scan_kernel(float *__restrict__ carr
 // without LDS), and its tiles of the state.  NS: parts that P and S are split
 // into, two where they only reach bf16 outputs (2^-17 of them, beside the
 // output's rounding of 2^-8).
-template <typename T, int DA, int DCT, bool kRev, int NS>
+//
+// kSlope: z_i = -d y_i / d rate = scale (sum over the chunk of (t_i - t_j) P_ij c_j
+// + D(i, last) ((t_i - t_last) a_i S + a_i S1)), S1 = -dS / d rate = the sum of
+// (t_last - t_j) D b c^T.  All its terms carry their own gap, so none cancel but by
+// their signs.
+template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, bool kSlope>
 __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     __shared__ alignas(16) bf16_t bt[NP * kChunk * DA];
     __shared__ alignas(16) bf16_t ct[NP * kChunk * DCT];
     __shared__ alignas(16) bf16_t st[NS * DCT * DA];
+    __shared__ alignas(16) bf16_t st1[kSlope ? NS * DCT * DA : 8];
     __shared__ alignas(16) int32_t tj[kChunk];
-    __shared__ float wj[kChunk];
+    __shared__ alignas(16) float wj[kChunk], wj1[kSlope ? kChunk : 4];
     const int tile = blockIdx.x % p.tiles;
     const int head = (blockIdx.x / p.tiles) % p.heads;
     const int seg = blockIdx.x / p.tiles / p.heads;
@@ -205,8 +238,11 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     const int dc0 = tile * DCT;
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
     const int mine = 16 * wave + l;  // this lane's token of a chunk
-    const T *a_data = static_cast<const T *>(p.a.data) + (int64_t)head * p.a.head_stride;
-    T *y_data = static_cast<T *>(p.y.data) + (int64_t)head * p.y.head_stride + dc0;
+    const Rows<T> ra(p.a, head, 0), rb(p.b, head, 0), rc(p.c, head, dc0), ry(p.y, head, dc0);
+    Staged<T, DA, kWhole, kRev> sb(rb, p.da);
+    Staged<T, DCT, kWhole, kRev> sc(rc, p.dc - dc0);
+    RowFrag<T, DA, kWhole, kRev> sa;
+    double slope = 0.0;
 
     const int32_t b_new = first_from(p, kRev ? g1 : g0);  // the first sequence that starts here
     int32_t b = b_new;
@@ -219,14 +255,31 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
         const bool ends = !kRev && e <= g1;
         const int32_t length = hi > lo ? hi - lo : 0;
 
-        floatx4 acc[S::kTiles];
+        int32_t t_next = 0;
+        auto fetch = [&](int32_t at) {  // the chunk `at` tokens into the piece
+            const int32_t left = length - at;
+            const int count = left < kChunk ? left : kChunk;
+            const int32_t lowest = kRev ? hi - at - count : lo + at;
+            sb.load(rb, lowest, count, p.da);
+            sc.load(rc, lowest, count, p.dc - dc0);
+            sa.load(ra, lowest, count, p.da, mine);
+            if (threadIdx.x < kChunk) {
+                const int i = (int)threadIdx.x < count ? threadIdx.x : 0;
+                t_next = time_at(p, kRev ? lowest + count - 1 - i : lowest + i);
+            }
+        };
+        if (length > 0) fetch(0);
+
+        floatx4 acc[S::kTiles], acc1[S::kTiles];
         bool some = false;  // whether there is a state
         int32_t ref = 0;    // its time
         {
-            const float *from = nullptr;
+            const float *from = nullptr, *from1 = nullptr;
             int64_t si = 0, sj = 0;
             if (came_in) {
-                from = p.carry + ((int64_t)seg * p.heads + head) * p.state_stride;
+                const int64_t place = ((int64_t)seg * p.heads + head) * p.state_stride;
+                from = p.carry + place;
+                if constexpr (kSlope) from1 = p.carry1 + place;
                 si = p.carry_i;
                 sj = p.carry_j;
                 ref = time_at(p, kRev ? g1 : g0 - 1);
@@ -239,185 +292,186 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                 ref = time_at(p, kRev ? hi - 1 : lo);
             }
             some = from != nullptr;
-            const int col = dc0 + S::col();
+            const int col = dc0 + S::col(), row0 = in_loop(S::row(0));
 #pragma unroll
             for (int u = 0; u < S::kTiles; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = S::row(u) + r;
-                    acc[u][r] = some && row < p.da && col < p.dc ? from[row * si + col * sj] : 0.f;
+                    const int row = row0 + 16 * u + r;
+                    const bool ok = some && row < p.da && col < p.dc;
+                    acc[u][r] = ok ? from[row * si + col * sj] : 0.f;
+                    if constexpr (kSlope) acc1[u][r] = ok ? from1[row * si + col * sj] : 0.f;
                 }
         }
 
-        Staged<T, DA> sb;
-        Staged<T, DCT> sc;
-        auto fetch = [&](int32_t at) {  // the chunk `at` tokens into the piece
-            const int32_t left = length - at;
-            const int count = left < kChunk ? left : kChunk;
-            const int32_t first = kRev ? hi - 1 - at : lo + at;
-            sb.template load<kRev>(p.b, head, first, count, 0, p.da);
-            sc.template load<kRev>(p.c, head, first, count, dc0, p.dc);
-        };
-        if (length > 0) fetch(0);
         for (int32_t at = 0; at < length; at += kChunk) {
             const int count = length - at < kChunk ? length - at : kChunk;
-            const int32_t first = kRev ? hi - 1 - at : lo + at;
+            const int32_t lowest = kRev ? hi - at - count : lo + at;
             const bool more = at + kChunk < length;
             const bool update = more || (ends && p.state_out);
-            const int64_t token = token_of<kRev>(first, mine);
             const bool there = mine < count;
-            const int32_t t_last = time_at(p, (int32_t)token_of<kRev>(first, count - 1));
 
             __syncthreads();  // the last chunk's tiles are done with
-            sb.store(bt);
-            sc.store(ct);
             if (threadIdx.x < kChunk) {
-                const int32_t t = time_at(
-                    p, (int32_t)token_of<kRev>(first, (int)threadIdx.x < count ? threadIdx.x : 0));
-                tj[threadIdx.x] = t;
-                wj[threadIdx.x] =
-                    (int)threadIdx.x < count ? decay(rate2, elapsed<kRev>(t_last, t)) : 0.f;
+                const int32_t t_end = __shfl(t_next, count - 1);  // (the first wave has all 64)
+                const float dt = elapsed<kRev>(t_end, t_next);
+                const float w = (int)threadIdx.x < count ? decay(rate2, dt) : 0.f;
+                tj[threadIdx.x] = t_next;
+                wj[threadIdx.x] = w;
+                if constexpr (kSlope) wj1[threadIdx.x] = w * dt;
             }
+            sb.store(bt, count, p.da);
+            sc.store(ct, count, p.dc - dc0);
             if (some) {
-#pragma unroll
-                for (int u = 0; u < S::kTiles; ++u) {
-                    const int o = tile_at<DA>(S::col(), S::row(u));
-                    uint32_t w[3][2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float x = acc[u][2 * i], z = acc[u][2 * i + 1];
-                        if constexpr (NS == 3) {
-                            split2(x, z, w[0][i], w[1][i], w[2][i]);
-                        } else {
-                            w[0][i] = pack_bf16(x, z);
-                            w[1][i] = pack_bf16(x - __uint_as_float(w[0][i] << 16),
-                                                z - __uint_as_float(w[0][i] & 0xFFFF0000u));
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < NS; ++i)
-                        *reinterpret_cast<uint2 *>(st + i * DCT * DA + o) = uint2{w[i][0], w[i][1]};
-                }
+                store_state<DA, DCT, NS>(st, acc);
+                if constexpr (kSlope) store_state<DA, DCT, NS>(st1, acc1);
             }
-            // the rows of a, as an operand
-            bf16x8 a[DA / 32][NP];
-            const T *a_row = a_data + (there ? token : 0) * p.a.token_stride;
-#pragma unroll
-            for (int k = 0; k < DA / 32; ++k)
-                frag_global<T>(a_row, 32 * k + 8 * g, p.da, there, a[k]);
+            bf16x8 a[DA / 32][NP];  // the rows of a, as an operand
+            sa.parts(a, count, p.da, mine);
             __syncthreads();
             if (more) fetch(at + kChunk);
 
             // P^T: keys 16 kt + 4 g + r of the lane's token, masked and decayed
-            const int32_t t_mine = tj[mine];
-            float pk[kChunk / 16][4];
-#pragma unroll
-            for (int kt = 0; kt < kChunk / 16; ++kt) {
-                floatx4 d{0.f, 0.f, 0.f, 0.f};
-                if (kt <= wave) {
-#pragma unroll
-                    for (int k = 0; k < DA / 32; ++k) {
-                        bf16x8 bk[NP];
-                        frag_row<DA, NP>(bt, kChunk * DA, 16 * kt + l, 32 * k + 8 * g, bk);
-                        mma<NP, NP>(bk, a[k], d);
-                    }
-                    const int4 t = *reinterpret_cast<const int4 *>(tj + 16 * kt + 4 * g);
-                    const int32_t tk[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float x = d[r] * decay(rate2, elapsed<kRev>(t_mine, tk[r]));
-                        d[r] = 16 * kt + 4 * g + r <= mine ? x : 0.f;
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) pk[kt][r] = d[r];
-            }
-            bf16x8 pf[kChunk / 32][NS];
+            const int32_t t_mine = tj[mine], t_last = __builtin_amdgcn_readfirstlane(tj[count - 1]);
+            bf16x8 pf[kChunk / 32][NS], pf1[kChunk / 32][NS];
 #pragma unroll
             for (int s2 = 0; s2 < kChunk / 32; ++s2) {
-                float x[8];
+                float x[8], x1[8];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[r] = pk[2 * s2][r];
-                    x[4 + r] = pk[2 * s2 + 1][r];
+                for (int half = 0; half < 2; ++half) {
+                    const int kt = 2 * s2 + half;
+                    floatx4 d{0.f, 0.f, 0.f, 0.f}, d1{0.f, 0.f, 0.f, 0.f};
+                    if (kt <= wave) {
+#pragma unroll
+                        for (int k = 0; k < DA / 32; ++k) {
+                            bf16x8 bk[NP];
+                            frag_row<DA, NP>(bt, kChunk * DA, 16 * kt + l, 32 * k + 8 * g, bk);
+                            mma<NP, NP>(bk, a[k], d);
+                        }
+                        const int4 t = *reinterpret_cast<const int4 *>(tj + 16 * kt + 4 * g);
+                        const int32_t tk[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float dt = elapsed<kRev>(t_mine, tk[r]);
+                            d[r] *= decay(rate2, dt);
+                            if constexpr (kSlope) d1[r] = d[r] * dt;
+                        }
+                        if (kt == wave) {
+                            const int behind = in_loop(l - 4 * g);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                d[r] = r <= behind ? d[r] : 0.f;
+                                if constexpr (kSlope) d1[r] = r <= behind ? d1[r] : 0.f;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        x[4 * half + r] = d[r];
+                        x1[4 * half + r] = d1[r];
+                    }
                 }
                 split8<NS>(x, pf[s2]);
+                if constexpr (kSlope) split8<NS>(x1, pf1[s2]);
             }
-            const float since = some ? decay(rate2, elapsed<kRev>(t_mine, ref)) : 0.f;
+            const float dt_ref = elapsed<kRev>(t_mine, ref);
+            const float since = decay(rate2, dt_ref) * p.scale;
+            const int up = kRev ? count - 1 - mine : mine;
             float dot = 0.f;
 #pragma unroll
             for (int ti = 0; ti < DCT / 16; ++ti) {
-                floatx4 o{0.f, 0.f, 0.f, 0.f};
+                floatx4 o{0.f, 0.f, 0.f, 0.f}, z{0.f, 0.f, 0.f, 0.f}, in = o;
                 if (some) {
+                    floatx4 in1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = 0; k < DA / 32; ++k) {
                         bf16x8 sf[NS];
                         frag_row<DA, NS>(st, DCT * DA, 16 * ti + l, 32 * k + 8 * g, sf);
-                        mma<NS, NP>(sf, a[k], o);
+                        mma<NS, NP>(sf, a[k], in);
+                        if constexpr (kSlope) {
+                            frag_row<DA, NS>(st1, DCT * DA, 16 * ti + l, 32 * k + 8 * g, sf);
+                            mma<NS, NP>(sf, a[k], in1);
+                        }
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[r] *= since;
+                    for (int r = 0; r < 4; ++r) {
+                        if constexpr (kSlope) z[r] = since * fmaf(dt_ref, in[r], in1[r]);
+                        in[r] *= since;
+                    }
                 }
+                floatx4 o1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s2 = 0; s2 < kChunk / 32; ++s2) {
                     if (2 * s2 > wave) break;
                     bf16x8 cf[NP];
                     frag_col<DCT, NP>(ct, kChunk * DCT, 32 * s2, 16 * ti, cf);
                     mma<NP, NS>(cf, pf[s2], o);
+                    if constexpr (kSlope) mma<NP, NS>(cf, pf1[s2], o1);
                 }
-                const int c = 16 * ti + 4 * g;  // the lane's channels c .. + 3 of its token
-                if (there && dc0 + c < p.dc) {
-                    const int have = p.dc - dc0 - c;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    o[r] = fmaf(o[r], p.scale, in[r]);
+                    if constexpr (kSlope) z[r] = fmaf(o1[r], p.scale, z[r]);
+                }
+                const int c = 16 * ti + in_loop(4 * g);  // the lane's channels c .. + 3 of its token
+                const int have = p.dc - dc0 - c;
+                if (there && have > 0) {
                     T raw[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        o[r] *= p.scale;
-                        raw[r] = from_f32<T>(o[r]);
-                    }
-                    T *dst = y_data + token * p.y.token_stride + c;
-                    if (have >= 4) {
+                    for (int r = 0; r < 4; ++r) raw[r] = from_f32<T>(o[r]);
+                    T *dst = const_cast<T *>(ry.base) + (int64_t)lowest * ry.stride +
+                             (int64_t)up * ry.stride + c;
+                    if constexpr (kWhole) {
                         __builtin_memcpy(dst, raw, sizeof(raw));
                     } else {
 #pragma unroll
-                        for (int r = 0; r < 3; ++r)
+                        for (int r = 0; r < 4; ++r)
                             if (r < have) dst[r] = raw[r];
                     }
-                    if (p.dots) {
-                        const T *x = static_cast<const T *>(p.x.data) + token * p.x.token_stride +
+                    if constexpr (kSlope) {
+                        const T *x = static_cast<const T *>(p.x.data) +
+                                     (int64_t)(lowest + up) * p.x.token_stride +
                                      (int64_t)head * p.x.head_stride + dc0 + c;
+                        if constexpr (kWhole) {
+                            __builtin_memcpy(raw, x, sizeof(raw));
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) raw[r] = r < have ? x[r] : T(0);
+                        }
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (r < have) dot += o[r] * to_f32(x[r]);
+                            if (kWhole || r < have) dot += z[r] * to_f32(raw[r]);
                     }
                 }
             }
-            if (p.dots) {
-                dot += __shfl_xor(dot, 16);
-                dot += __shfl_xor(dot, 32);
-                if (there && g == 0)
-                    p.dots[((int64_t)tile * p.heads + head) * p.n + token] = dot;
-            }
+            if constexpr (kSlope) slope += (double)dot;
             if (update) {
-                const float f = step_factor(rate, elapsed<kRev>(t_last, ref));
                 if (some) {
+                    const float gap = elapsed<kRev>(t_last, ref);
+                    const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(
+                        __float_as_uint(step_factor(rate, gap))));
 #pragma unroll
                     for (int u = 0; u < S::kTiles; ++u)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[u][r] = apply_factor(f, acc[u][r]);
+                        for (int r = 0; r < 4; ++r) {
+                            if constexpr (kSlope)
+                                acc1[u][r] = apply_factor(f, fmaf(gap, acc[u][r], acc1[u][r]));
+                            acc[u][r] = apply_factor(f, acc[u][r]);
+                        }
                 }
-                add_chunk<T, DA, DCT>(bt, ct, wj, acc);
+                add_chunk<T, DA, DCT, kSlope>(bt, ct, wj, wj1, acc, acc1);
                 some = true;
                 ref = t_last;
             }
         }
         if (ends && p.state_out) {
-            const int col = dc0 + S::col();
+            const int col = dc0 + S::col(), row0 = in_loop(S::row(0));
             float *to = p.state_out + ((int64_t)b * p.heads + head) * p.da * p.dc;
 #pragma unroll
             for (int u = 0; u < S::kTiles; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = S::row(u) + r;
+                    const int row = row0 + 16 * u + r;
                     if (row < p.da && col < p.dc) to[(int64_t)row * p.dc + col] = acc[u][r];
                 }
             if (p.time_out && tile == 0 && head == 0 && threadIdx.x == 0)
@@ -426,25 +480,47 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
         }
         b += kRev ? -1 : 1;
     }
+    if constexpr (kSlope) {
+        __shared__ double sums[kWaves];
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) slope += __shfl_xor(slope, m);
+        if ((threadIdx.x & 63) == 0) sums[wave] = slope;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            p.slope[((int64_t)tile * p.n_seg + seg) * p.heads + head] =
+                (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    }
 }
 
 // ---------------------------------------------------------------- launches
-// Calls f with the padded channels of a (32, 64 or 128) and the columns of a tile
-// of c (32 or 64).
-template <typename F> void pass_dispatch(int32_t da, int32_t dct, F &&f) {
-#define SBC_PASS(x, y) f(std::integral_constant<int, x>{}, std::integral_constant<int, y>{})
-    if (dct == 32) {
-        if (da <= 32) SBC_PASS(32, 32);
-        else if (da <= 64) SBC_PASS(64, 32);
-        else SBC_PASS(128, 32);
+// Calls f with the padded channels of a, the columns of a tile of c, and whether rows
+// are whole 16-byte pieces.  (Rows that are not take the sizes up to 64 or 128.)
+template <typename T, typename F> void pass_dispatch(int32_t da, int32_t dct, bool whole, F &&f) {
+#define SBC_PASS(x, y, w)                                                        \
+    f(std::integral_constant<int, x>{}, std::integral_constant<int, y>{},        \
+      std::integral_constant<bool, w>{})
+    if (!whole) {
+        if (dct == 32 && da <= 64) SBC_PASS(64, 32, false);
+        else if (dct == 32) SBC_PASS(128, 32, false);
+        else if (da <= 64) SBC_PASS(64, 64, false);
+        else SBC_PASS(128, 64, false);
+    } else if (dct == 32) {
+        if (da <= 32) SBC_PASS(32, 32, true);
+        else if (da <= 64) SBC_PASS(64, 32, true);
+        else if (da <= 96) SBC_PASS(96, 32, true);
+        else SBC_PASS(128, 32, true);
     } else {
-        if (da <= 32) SBC_PASS(32, 64);
-        else if (da <= 64) SBC_PASS(64, 64);
-        else SBC_PASS(128, 64);
+        if (da <= 32) SBC_PASS(32, 64, true);
+        else if (da <= 64) SBC_PASS(64, 64, true);
+        else if (da <= 96) SBC_PASS(96, 64, true);
+        else SBC_PASS(128, 64, true);
     }
 #undef SBC_PASS
 }
 
+inline dim3 scan_grid(const AttnPass &p) {
+    return dim3((unsigned)grid_for(p.state_stride, 64), (unsigned)p.heads);
+}
 inline dim3 pass_grid(const AttnPass &p) {
     return dim3((unsigned)((int64_t)p.n_seg * p.heads * p.tiles));
 }
