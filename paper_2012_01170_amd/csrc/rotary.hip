@@ -5,8 +5,9 @@
 //   (a, b) -> (a cos - b sin, b cos + a sin),
 // the gradient by the opposite angle.  Every value is moved twice and turned with
 // four products, so memory bounds it as long as the angle's sine and cosine are
-// not made for every head: a lane makes those of kVec pairs of a token once and
-// then takes the token's heads in turn, of both arrays.
+// not made for every head: a lane makes those of some pairs of a token once and
+// takes the token's heads, of both arrays, kBatch at a time, so that their loads are
+// in flight together (and the first ones while it makes them).
 //
 // The angle is taken in revolutions in float64, where the product of two float32
 // is exact and 1 / 2 pi costs 2^-53 of it, and reduced before sine and cosine in
@@ -31,80 +32,86 @@ struct RotaryArgs {
     float sign;
 };
 
+// Pairs of a lane: one vector of them, or of each of their halves
+template <typename T, bool kInterleaved> constexpr int kPairs = kInterleaved ? kVec<T> / 2 : kVec<T>;
+
 template <typename T, typename P, bool kInterleaved>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, N = kPairs<T, kInterleaved>;
+    constexpr int kVecs = kInterleaved ? 1 : 2, kBatch = kInterleaved ? 4 : 2;
     const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int64_t i = at / a.units;
     if (i >= a.n) return;
     const int unit = (int)(at - i * a.units);
-    const int turning = (a.pairs + V - 1) / V;
+    const int turning = (a.pairs + N - 1) / N;
+    const int total = a.heads[0] + a.heads[1];
+    auto source = [&](int j) {
+        const int w = j >= a.heads[0], h = w ? j - a.heads[0] : j;
+        return static_cast<const T *>(a.in[w].data) + i * a.in[w].token_stride +
+               h * a.in[w].head_stride;
+    };
+    auto target = [&](int j) {
+        const int w = j >= a.heads[0], h = w ? j - a.heads[0] : j;
+        return static_cast<T *>(a.out[w].data) + i * a.out[w].token_stride +
+               h * a.out[w].head_stride;
+    };
     if (unit >= turning) {  // channels past the last pair are copied
         const int c = 2 * a.pairs + (unit - turning) * V;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const T *src = static_cast<const T *>(a.in[w].data) + i * a.in[w].token_stride + c;
-            T *dst = static_cast<T *>(a.out[w].data) + i * a.out[w].token_stride + c;
-            for (int h = 0; h < a.heads[w]; ++h) {
-                float v[V];
-                load_vec<T>(src + h * a.in[w].head_stride, a.d - c, v);
-                store_vec<T>(dst + h * a.out[w].head_stride, a.d - c, v);
-            }
+        for (int j = 0; j < total; ++j) {
+            float v[V];
+            load_vec<T>(source(j) + c, a.d - c, v);
+            store_vec<T>(target(j) + c, a.d - c, v);
         }
         return;
     }
-    const int p0 = unit * V;
-    const int have = a.pairs - p0;  // pairs of this lane, if fewer than V
-    float cs[V], sn[V];
+    const int p0 = unit * N;
+    const int have = a.pairs - p0;  // pairs of this lane, if fewer than N
+    // the lane's vectors: of the pairs themselves, or of their first and second halves
+    const int c[2] = {kInterleaved ? 2 * p0 : p0, a.pairs + p0};
+    const int width = kInterleaved ? 2 * have : have;
+    float x[kBatch][kVecs][V];
+    auto fetch = [&](int j0) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
+        for (int u = 0; u < kBatch; ++u)
+            if (j0 + u < total) {
+#pragma unroll
+                for (int w = 0; w < kVecs; ++w) load_vec<T>(source(j0 + u) + c[w], width, x[u][w]);
+            }
+    };
+    fetch(0);
+    float cs[N], sn[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
         cs[k] = 1.f;
         sn[k] = 0.f;
         if (k < have) {
             int axis = 0;
-            for (int x = 0; x + 1 < a.n_axes; ++x) axis += p0 + k >= a.upto[x];
+            for (int y = 0; y + 1 < a.n_axes; ++y) axis += p0 + k >= a.upto[y];
             const double pos = (double)static_cast<const P *>(a.positions)[i * a.pos_stride + axis];
             double rev = pos * (double)a.freqs[p0 + k] * 0.15915494309189533577;
             rev -= rint(rev);
-            float s, c;
-            sincospif((float)(2.0 * rev), &s, &c);
-            cs[k] = c;
+            float s, co;
+            sincospif((float)(2.0 * rev), &s, &co);
+            cs[k] = co;
             sn[k] = a.sign * s;
         }
     }
-    // the lane's two vectors: the pairs' first and second halves, or the pairs themselves
-    const int c0 = kInterleaved ? 2 * p0 : p0;
-    const int c1 = kInterleaved ? 2 * p0 + V : a.pairs + p0;
-    const int have0 = kInterleaved ? 2 * have : have;
-    const int have1 = kInterleaved ? 2 * have - V : have;
+    for (int j0 = 0; j0 < total; j0 += kBatch) {
+        if (j0 > 0) fetch(j0);
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const T *src = static_cast<const T *>(a.in[w].data) + i * a.in[w].token_stride;
-        T *dst = static_cast<T *>(a.out[w].data) + i * a.out[w].token_stride;
-        for (int h = 0; h < a.heads[w]; ++h) {
-            float x[2 * V], lo[V], hi[V];
-            load_vec<T>(src + h * a.in[w].head_stride + c0, have0, lo);
-            load_vec<T>(src + h * a.in[w].head_stride + c1, have1, hi);
+        for (int u = 0; u < kBatch; ++u)
+            if (j0 + u < total) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                x[k] = lo[k];
-                x[V + k] = hi[k];
+                for (int k = 0; k < N; ++k) {
+                    float &p = kInterleaved ? x[u][0][2 * k] : x[u][0][k];
+                    float &q = kInterleaved ? x[u][0][2 * k + 1] : x[u][kVecs - 1][k];
+                    const float turned = p * cs[k] - q * sn[k];
+                    q = q * cs[k] + p * sn[k];
+                    p = turned;
+                }
+#pragma unroll
+                for (int w = 0; w < kVecs; ++w) store_vec<T>(target(j0 + u) + c[w], width, x[u][w]);
             }
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int u = kInterleaved ? 2 * k : k, v = kInterleaved ? 2 * k + 1 : V + k;
-                const float s = x[u] * cs[k] - x[v] * sn[k];
-                x[v] = x[v] * cs[k] + x[u] * sn[k];
-                x[u] = s;
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                lo[k] = x[k];
-                hi[k] = x[V + k];
-            }
-            store_vec<T>(dst + h * a.out[w].head_stride + c0, have0, lo);
-            store_vec<T>(dst + h * a.out[w].head_stride + c1, have1, hi);
-        }
     }
 }
 
@@ -176,10 +183,11 @@ extern "C" sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q
     if (heads_overlap(*out[0], heads[0], d, *out[1], heads[1], d, n, dtype))
         return fail(SBC_ERR_INVALID_ARG, "q_out and k_out overlap");
     const int V = dtype == SBC_F32 ? 4 : 8;
+    const int N = plan->interleaved ? V / 2 : V;  // (kPairs)
     a.n = n;
     a.d = d;
     a.pairs = (int32_t)pairs;
-    a.units = (int32_t)((pairs + V - 1) / V + (d - 2 * pairs + V - 1) / V);
+    a.units = (int32_t)((pairs + N - 1) / N + (d - 2 * pairs + V - 1) / V);
     a.positions = plan->positions;
     a.pos_stride = plan->position_stride;
     a.freqs = plan->freqs;
