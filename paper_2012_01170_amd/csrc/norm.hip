@@ -59,17 +59,27 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(
     constexpr int kRows = kThreads / G;
     const int lane = threadIdx.x % G;
     auto sum = row_sum<G>(buf);
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < n;
-         r += (int64_t)gridDim.x * kRows) {
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+    raw16 next[K];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * G + lane) * V;
+            next[k] = load_raw16<T>(x + row * x_stride + c, C - c);
+        }
+    };
+    if (r < n) fetch(r);
+    for (; r < n; r += step) {
         float v[K][V];
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * G + lane) * V;
-            load_vec<T>(x + r * x_stride + c, C - c, v[k]);
+            unpack<T>(next[k], v[k]);
 #pragma unroll
             for (int i = 0; i < V; ++i) s += v[k][i];
         }
+        if (r + step < n) fetch(r + step);
         const float mu = sum(s) / (float)C;  // (exact where all values are equal)
         s = 0.f;
 #pragma unroll
@@ -176,16 +186,31 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_kernel(
             dw[k][i] = db[k][i] = 0.f;
         }
     }
-    for (int64_t r = (int64_t)blockIdx.x * kRows + group; r < n; r += (int64_t)gridDim.x * kRows) {
-        const float mu = mean[r], rs = rstd[r];
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t r = (int64_t)blockIdx.x * kRows + group;
+    raw16 next_x[K], next_g[K];
+    float next_mu = 0.f, next_rs = 0.f;
+    auto fetch = [&](int64_t row) {
+        next_mu = mean[row];
+        next_rs = rstd[row];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * G + lane) * V;
+            next_x[k] = load_raw16<T>(x + row * x_stride + c, C - c);
+            next_g[k] = load_raw16<T>(dy + row * dy_stride + c, C - c);
+        }
+    };
+    if (r < n) fetch(r);
+    for (; r < n; r += step) {
+        const float mu = next_mu, rs = next_rs;
         float xn[K][V], g[K][V];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * G + lane) * V;
-            load_vec<T>(x + r * x_stride + c, C - c, xn[k]);
-            load_vec<T>(dy + r * dy_stride + c, C - c, g[k]);
+            unpack<T>(next_x[k], xn[k]);
+            unpack<T>(next_g[k], g[k]);
         }
+        if (r + step < n) fetch(r + step);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * G + lane) * V;
@@ -311,27 +336,38 @@ __global__ __launch_bounds__(kThreads) void wide_dw_kernel(
         }
 }
 
-// dw and db from `parts` workgroups' sums: 16 channels a workgroup, 16 lanes a
-// channel, in float64.
-__global__ __launch_bounds__(kThreads) void norm_reduce_kernel(const float *__restrict__ part,
-                                                               int32_t parts, int32_t C,
-                                                               float *__restrict__ dw,
-                                                               float *__restrict__ db) {
-    __shared__ double red[16][17];
+// dw and db from `parts` workgroups' sums: 16 channels a workgroup, 64 lanes a
+// channel, in float64.  (A round of loads takes 1.7 us here, from what other XCDs
+// have just written: with 16 lanes a channel 512 parts of 64 channels took 7 us.)
+constexpr int kReduceThreads = 1024;
+__global__ __launch_bounds__(kReduceThreads) void norm_reduce_kernel(
+    const float *__restrict__ part, int32_t parts, int32_t C, float *__restrict__ dw,
+    float *__restrict__ db) {
+    constexpr int kDown = kReduceThreads / 16, kAhead = 8;  // loads in flight
+    __shared__ double red[kDown][17];
     const int cl = threadIdx.x % 16, pl = threadIdx.x / 16;
-    const int64_t j = (int64_t)blockIdx.x * 16 + cl;
+    const int64_t j = (int64_t)blockIdx.x * 16 + cl, width = 2 * (int64_t)C;
     double s = 0.0;
-    if (j < 2 * (int64_t)C)
-        for (int p = pl; p < parts; p += 16) s += (double)part[(int64_t)p * 2 * C + j];
+    if (j < width) {
+        for (int p0 = pl; p0 < parts; p0 += kDown * kAhead) {
+            float v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                v[k] = p0 + kDown * k < parts ? part[(p0 + kDown * k) * width + j] : 0.f;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) s += (double)v[k];
+        }
+    }
     red[pl][cl] = s;
-    __syncthreads();
-    if (pl == 0 && j < 2 * (int64_t)C) {
-        double t = 0.0;
-        for (int p = 0; p < 16; ++p) t += red[p][cl];
+    for (int half = kDown / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (pl < half) red[pl][cl] += red[pl + half][cl];
+    }
+    if (pl == 0 && j < width) {
         if (j < C) {
-            if (dw) dw[j] = (float)t;
+            if (dw) dw[j] = (float)red[0][cl];
         } else if (db) {
-            db[j - C] = (float)t;
+            db[j - C] = (float)red[0][cl];
         }
     }
 }
@@ -357,19 +393,21 @@ template <int V, typename F> bool row_dispatch(int32_t C, F &&f) {
     return true;
 }
 
-// Workgroups of the forward pass (and of dx in wide rows); what is left is taken
-// in turn.  (A launch holds fewer than 2^32 work-items.)
+// Workgroups of the forward pass (and of dx in wide rows), one for the rows that it
+// takes at once; rows past 2^22 workgroups' are taken in turn.  (A launch holds fewer
+// than 2^32 work-items.  1M rows of 64 bf16 take 66 us so, 70 in 8192 workgroups.)
 constexpr int64_t kMostBlocks = 1 << 22;
 unsigned row_blocks(int64_t n, int rows) {
     const int64_t b = (n + rows - 1) / rows;
     return (unsigned)(b < kMostBlocks ? b : kMostBlocks);
 }
 
-// Workgroups of the backward pass.  Each leaves 2 C sums: at most 4 a CU, and one
-// for 32 rows, whose sums, written and read, are 8 % of the rows' bytes in bf16.
+// Workgroups of the backward pass: at most 2 a CU, and one for 16 rows, since each
+// leaves 2 C sums to be read again (12007 rows of 1001 bf16: 25.5 us so, 31 at one a
+// CU, 31 to 34 at 8 rows).
 int32_t bwd_blocks(int32_t n) {
-    const int64_t most = 4 * (int64_t)device_cus();
-    int64_t b = ((int64_t)n + 31) / 32;
+    const int64_t most = 2 * (int64_t)device_cus();
+    int64_t b = ((int64_t)n + 15) / 16;
     if (b > most) b = most;
     return (int32_t)(b < 1 ? 1 : b);
 }
@@ -495,8 +533,8 @@ extern "C" sbc_status sbc_layer_norm_backward(const void *dy, int64_t dy_stride,
     trace_after("norm_bwd", stream);
     if (!sums) return SBC_OK;
     trace_before("norm_reduce", stream);
-    hipLaunchKernelGGL(norm_reduce_kernel, dim3(grid_for(2 * (int64_t)C, 16)), dim3(kThreads), 0,
-                       stream, part, parts, C, dweight, dbias);
+    hipLaunchKernelGGL(norm_reduce_kernel, dim3(grid_for(2 * (int64_t)C, 16)),
+                       dim3(kReduceThreads), 0, stream, part, parts, C, dweight, dbias);
     SBC_LAUNCH_CHECK();
     trace_after("norm_reduce", stream);
     return SBC_OK;

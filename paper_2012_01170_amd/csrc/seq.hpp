@@ -26,21 +26,34 @@ template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float x) {
 
 template <typename T> constexpr int kVec = 16 / sizeof(T);  // elements of 16 bytes
 
-// kVec<T> elements at p as float32, of which the first `have` exist (the others
-// read as 0 and are not touched).  p needs an element's alignment only: global
-// memory takes 16-byte accesses at any address, and one that is not aligned
-// costs a second cache line at most, less than accesses by elements.
+typedef uint32_t raw16 __attribute__((ext_vector_type(4)));  // 16 bytes as they lie
+
+// kVec<T> elements at p, of which the first `have` exist (the others read as 0 and
+// are not touched).  p needs an element's alignment only: global memory takes
+// 16-byte accesses at any address, and one that is not aligned costs a second cache
+// line at most, less than accesses by elements.
+template <typename T> __device__ __forceinline__ raw16 load_raw16(const T *p, int have) {
+    raw16 r;
+    if (have >= kVec<T>) {
+        __builtin_memcpy(&r, p, 16);
+    } else {
+        T e[kVec<T>];
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) e[i] = i < have ? p[i] : T(0);
+        __builtin_memcpy(&r, e, 16);
+    }
+    return r;
+}
+template <typename T> __device__ __forceinline__ void unpack(const raw16 &r, float (&out)[kVec<T>]) {
+    T e[kVec<T>];
+    __builtin_memcpy(e, &r, 16);
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) out[i] = to_f32(e[i]);
+}
+// the same as float32
 template <typename T>
 __device__ __forceinline__ void load_vec(const T *p, int have, float (&out)[kVec<T>]) {
-    T raw[kVec<T>];
-    if (have >= kVec<T>) {
-        __builtin_memcpy(raw, p, 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) raw[i] = i < have ? p[i] : T(0);
-    }
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) out[i] = to_f32(raw[i]);
+    unpack<T>(load_raw16<T>(p, have), out);
 }
 
 template <typename T>
