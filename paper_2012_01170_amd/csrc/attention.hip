@@ -20,16 +20,16 @@ template <typename T> sbc_status forward(const AttnPass &p, bool whole_rows, hip
         constexpr bool W = decltype(whole)::value;
         if (p.n_seg > 1) {
             trace_before("attn_state", stream);
-            hipLaunchKernelGGL((attn_state_kernel<T, DA, DCT, W, false, false>), pass_grid(p),
+            hipLaunchKernelGGL((attn_state_kernel<T, DA, DCT, W, false>), pass_grid(p),
                                dim3(kAttnThreads), 0, stream, p);
             trace_after("attn_state", stream);
             trace_before("attn_scan", stream);
-            hipLaunchKernelGGL((attn_scan_kernel<false, false>), scan_grid(p), dim3(256), 0, stream,
+            hipLaunchKernelGGL(attn_scan_kernel<false>, scan_grid(p), dim3(256), 0, stream,
                                p);
             trace_after("attn_scan", stream);
         }
         trace_before("attn_fwd", stream);
-        hipLaunchKernelGGL((attn_pass_kernel<T, DA, DCT, W, false, NS, false>), pass_grid(p),
+        hipLaunchKernelGGL((attn_pass_kernel<T, DA, DCT, W, false, NS, 0>), pass_grid(p),
                            dim3(kAttnThreads), 0, stream, p);
         trace_after("attn_fwd", stream);
     });

@@ -53,12 +53,10 @@ struct AttnPass {
     const int32_t *state_time;
     float *state_out;
     int32_t *time_out;
-    // The derivative by the rate (kSlope): with z_i = -d y_i / d rate, the sums of
-    // x_i . z_i over a workgroup's tokens and columns, [tiles, n_seg, heads]; carry1
-    // holds the states' own derivatives, gap [n_seg] the time over which `factor`
-    // decays
+    // for the rates' gradient (Dots): rows whose products with y are wanted, the states
+    // that come into the segments along the sequence, and the sums, [tiles, n_seg, heads]
     sbc_heads x;
-    float *carry1, *gap;
+    const float *before;
     double *slope;
 };
 
@@ -155,15 +153,17 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[N]) {
     if constexpr (N > 2) out[2] = __builtin_bit_cast(bf16x8, l);
 }
 
+// value e of an operand's parts
+template <int N> __device__ __forceinline__ float part_sum(const bf16x8 (&in)[N], int e) {
+    float s = (float)in[N - 1][e];
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i) s += (float)in[i][e];
+    return s;
+}
 // the sum of the parts of 8 values
 template <int N> __device__ __forceinline__ void join8(const bf16x8 (&in)[N], float (&x)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float s = (float)in[N - 1][e];
-#pragma unroll
-        for (int i = N - 2; i >= 0; --i) s += (float)in[i][e];
-        x[e] = s;
-    }
+    for (int e = 0; e < 8; ++e) x[e] = part_sum<N>(in, e);
 }
 
 // A tile of D columns in LDS, row after row, one plane a part.  The 16-byte
@@ -180,6 +180,21 @@ __device__ __forceinline__ void frag_row(const bf16_t *tile, int plane, int row,
 #pragma unroll
     for (int i = 0; i < N; ++i)
         out[i] = *reinterpret_cast<const bf16x8 *>(tile + i * plane + tile_at<D>(row, col));
+}
+// The same in the order of frag_col's rows: columns col + 4 g .. + 3 and col + 16 +
+// 4 g .. + 3 (col without the lane's own 8 g)
+template <int D, int N>
+__device__ __forceinline__ void frag_row_split(const bf16_t *tile, int plane, int row, int col,
+                                               bf16x8 (&out)[N]) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint2 lo = *reinterpret_cast<const uint2 *>(tile + i * plane +
+                                                          tile_at<D>(row, col + 4 * g));
+        const uint2 hi = *reinterpret_cast<const uint2 *>(tile + i * plane +
+                                                          tile_at<D>(row, col + 16 + 4 * g));
+        out[i] = __builtin_bit_cast(bf16x8, u32x4v{lo.x, lo.y, hi.x, hi.y});
+    }
 }
 // For every lane 8 rows of one column: with l = lane & 15 and g = lane >> 4,
 // rows row0 + 4 g .. + 3 and row0 + 16 + 4 g .. + 3 of column col0 + l: the order
@@ -316,41 +331,66 @@ template <typename T, int D, bool kWhole, bool kRev> struct Staged {
 };
 
 // Each lane's own row (token `mine` of the chunk) as an operand of D columns:
-// columns 32 k + 8 g .. + 7 of k-step k
-template <typename T, int D, bool kWhole, bool kRev> struct RowFrag {
+// columns 32 k + 8 g .. + 7 of k-step k, or (kSplit) 32 k + 4 g .. + 3 and 32 k + 16 +
+// 4 g .. + 3
+template <typename T, int D, bool kWhole, bool kRev, bool kSplit = false> struct RowFrag {
     static constexpr int kRaw = 8 / kVec<T>;
     u32x4v raw[D / 32][kRaw];
 
+    // the columns' start for half of 4 (part) elements
+    __device__ __forceinline__ static int col_of(int k, int half) {
+        return 32 * k + (kSplit ? 16 * half : 4 * half);
+    }
     __device__ __forceinline__ void load(const Rows<T> &x, int32_t lowest, int count, int width,
                                          int mine) {
         const T *base = x.base + (int64_t)lowest * x.stride;
-        const int g = (threadIdx.x & 63) >> 4;
+        const int lane0 = (kSplit ? 4 : 8) * ((threadIdx.x & 63) >> 4);
         const bool there = mine < count;
         const int up = kRev ? count - 1 - mine : mine;
-        const T *row = kWhole ? base + (uint32_t)((there ? up : 0) * (uint32_t)x.stride + 8 * g)
-                              : base + (int64_t)(there ? up : 0) * x.stride + 8 * g;
+        const T *row = kWhole
+                           ? base + (uint32_t)((there ? up : 0) * (uint32_t)x.stride + lane0)
+                           : base + (int64_t)(there ? up : 0) * x.stride + lane0;
+        constexpr int kBytes = sizeof(T) * 4;  // of a half
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k)
-#pragma unroll
-            for (int i = 0; i < kRaw; ++i) {
-                const int col = 32 * k + i * kVec<T>;
+        for (int k = 0; k < D / 32; ++k) {
+            if constexpr (!kSplit && sizeof(T) == 2) {
                 if constexpr (kWhole)
-                    __builtin_memcpy(&raw[k][i], col + 8 * g < width ? row + col : base, 16);
+                    __builtin_memcpy(&raw[k][0], 32 * k + lane0 < width ? row + 32 * k : base, 16);
                 else
-                    raw[k][i] = load_elements<T>(row, col, width - 8 * g, there);
+                    raw[k][0] = load_elements<T>(row, 32 * k, width - lane0, there);
+            } else {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int col = col_of(k, half);
+                    char *to = reinterpret_cast<char *>(&raw[k][0]) + half * kBytes;
+                    if constexpr (kWhole) {
+                        __builtin_memcpy(to, col + lane0 < width ? row + col : base, kBytes);
+                    } else {
+                        T e[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            e[i] = there && col + lane0 + i < width ? row[col + i] : T(0);
+                        __builtin_memcpy(to, e, kBytes);
+                    }
+                }
             }
+        }
     }
     __device__ __forceinline__ void parts(bf16x8 (&out)[D / 32][kParts<T>], int count, int width,
                                           int mine) {
         if (kWhole && (count < kChunk || width < D)) {
-            const int g = in_loop((threadIdx.x & 63) >> 4);
+            const int lane0 = in_loop((kSplit ? 4 : 8) * ((threadIdx.x & 63) >> 4));
 #pragma unroll
             for (int k = 0; k < D / 32; ++k)
 #pragma unroll
-                for (int i = 0; i < kRaw; ++i) {
-                    const bool ok = mine < count && 32 * k + 8 * g + i * kVec<T> < width;
+                for (int half = 0; half < 2; ++half) {
+                    const bool ok = mine < count && col_of(k, half) + lane0 < width;
+                    constexpr int kWords = sizeof(T);  // of a half
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) raw[k][i][e] = ok ? raw[k][i][e] : 0u;
+                    for (int e = 0; e < kWords; ++e) {
+                        const int at = half * kWords + e;
+                        raw[k][at / 4][at % 4] = ok ? raw[k][at / 4][at % 4] : 0u;
+                    }
                 }
         }
 #pragma unroll
@@ -382,41 +422,43 @@ template <int DA, int DCT> struct StateTiles {
     __device__ __forceinline__ static int row(int u) { return row0(u) + 4 * ((threadIdx.x & 63) >> 4); }
 };
 
-// acc += sum over the chunk's tokens of w_j b_j c_j^T, with kSlope also acc1 += .. w1_j ..
-template <typename T, int DA, int DCT, bool kSlope>
+// acc += sum over the chunk's tokens of w_j b_j c_j^T
+template <typename T, int DA, int DCT>
 __device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct, const float *w,
-                                          const float *w1,
-                                          floatx4 (&acc)[StateTiles<DA, DCT>::kTiles],
-                                          floatx4 (&acc1)[StateTiles<DA, DCT>::kTiles]) {
+                                          floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int s = 0; s < kChunk / 32; ++s) {
-        bf16x8 raw[NP], cw[3], cw1[3];
+        bf16x8 raw[NP], cw[3];
         frag_col<DCT, NP>(ct, kChunk * DCT, 32 * s, S::col0(), raw);
-        float x[8], y[8];
+        float x[8];
         join8<NP>(raw, x);
-        auto weigh = [&](const float *weights, bf16x8(&out)[3]) {
-            const floatx4 lo = *reinterpret_cast<const floatx4 *>(weights + 32 * s + 4 * g);
-            const floatx4 hi = *reinterpret_cast<const floatx4 *>(weights + 32 * s + 16 + 4 * g);
+        const floatx4 lo = *reinterpret_cast<const floatx4 *>(w + 32 * s + 4 * g);
+        const floatx4 hi = *reinterpret_cast<const floatx4 *>(w + 32 * s + 16 + 4 * g);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = x[e] * lo[e];
-                y[4 + e] = x[4 + e] * hi[e];
-            }
-            split8<3>(y, out);
-        };
-        weigh(w, cw);
-        if constexpr (kSlope) weigh(w1, cw1);
+        for (int e = 0; e < 4; ++e) {
+            x[e] *= lo[e];
+            x[4 + e] *= hi[e];
+        }
+        split8<3>(x, cw);
 #pragma unroll
         for (int u = 0; u < S::kTiles; ++u) {
             bf16x8 b[NP];
             frag_col<DA, NP>(bt, kChunk * DA, 32 * s, S::row0(u), b);
             mma<NP, 3>(b, cw, acc[u]);
-            if constexpr (kSlope) mma<NP, 3>(b, cw1, acc1[u]);
         }
     }
+}
+
+// acc *= the decay of `f`, which is the same for all lanes
+template <int N> __device__ __forceinline__ void decay_state(float f, floatx4 (&acc)[N]) {
+    f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f)));
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[u][r] = apply_factor(f, acc[u][r]);
 }
 
 // The state in LDS as parts, column after column of c, its rows (the channels of a)

@@ -1,37 +1,45 @@
-// Gradients of the linear attention with decays: three passes of attention.hpp.
+// Gradients of the linear attention with decays: passes of attention.hpp,
 //
 //   dq: (dO, v, k) along the sequence       dk: (v, dO, q) back along it
 //   dv: (k, q, dO) back along it
-// and the rates' gradient beside dk: drate = - sum of (t_i - t_j) times the terms of
-// y = dk summed over j against k_j, the pass' kSlope.  (From the products k . dk and
-// q . dq of the tokens alone, as a flow that each token adds to and takes from, it
-// would lose what the flow's rounding gains over a segment: 4e-6 to 1e-5.)
+//
+// the last two in one (attention_grad.hpp) where a state is 64 x 64 or smaller.
+//
+// The rates' gradient.  With P_ij the term of a pair (its decay, both products and the
+// scale), drate = - sum of (t_i - t_j) P_ij.  A chunk's own pairs are summed as they
+// are.  Of the others, the sum of P_ij over the pairs that cross a point of the
+// sequence is a flow: it grows by k_j . dk_j (the part of dk_j from the state) behind
+// token j, falls by q_i . dq_i behind token i, and comes into a segment as the product
+// X of the states that meet there.  Over a piece of the segment up to the time t_end,
+//   sum of gap * flow = X (t_end - t_before) + sum of k . dk (t_end - t_j)
+//                       - sum of q . dq (t_end - t_i).
+// What rounding adds to the flow lasts to the end of the segment.  (Without flows, by
+// a second state that carries the gaps, the sums are as good as float32 allows, and
+// the whole backward pass takes a third longer: 723 us against 549.)
 #include "attention_host.hpp"
-#include "attention_kernels.hpp"
+#include "attention_grad.hpp"
 
 namespace sbc {
 namespace {
 
 constexpr int kBwdPerCu = 2;
 
-// drates[h] = - the sum of the workgroups' parts [parts, heads], in order
-__global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restrict__ part,
-                                                         int32_t parts, int32_t heads,
+// drates[h] = what the tokens take from the flow less what is in it, sums of the
+// workgroups' parts [parts, heads] in order
+__global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restrict__ taken,
+                                                         int32_t n_taken,
+                                                         const double *__restrict__ given,
+                                                         int32_t n_given, int32_t heads,
                                                          float *__restrict__ drates) {
     __shared__ double buf[4];
     double s = 0.0;
-    for (int i = threadIdx.x; i < parts; i += 256) s += part[(int64_t)i * heads + blockIdx.x];
+    for (int i = threadIdx.x; i < n_taken; i += 256) s += taken[(int64_t)i * heads + blockIdx.x];
+    for (int i = threadIdx.x; i < n_given; i += 256) s -= given[(int64_t)i * heads + blockIdx.x];
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) drates[blockIdx.x] = (float)-((buf[0] + buf[1]) + (buf[2] + buf[3]));
-}
-
-// Columns of a tile: of float32 and 128 channels, a state and its derivative leave
-// LDS room for 32.
-int bwd_tile(int32_t da, int32_t dc, bool slope, sbc_dtype dtype) {
-    return slope && dtype == SBC_F32 && da > 96 ? 32 : attn_tile(dc);
+    if (threadIdx.x == 0) drates[blockIdx.x] = (float)((buf[0] + buf[1]) + (buf[2] + buf[3]));
 }
 
 void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, int32_t *seg_len,
@@ -41,7 +49,7 @@ void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, int32_t
 }
 
 struct BwdSpace {
-    float *before, *behind, *behind1, *f_before, *f_behind, *gap;
+    float *before, *behind, *f_before, *f_behind;
     double *slope;
     size_t bytes;
 };
@@ -51,38 +59,53 @@ BwdSpace carve(void *ws, int32_t n, int32_t heads, int32_t dk, int32_t dv, int32
     const size_t states = (size_t)n_seg * heads * state_stride(dk, dv);
     s.before = c.take<float>(states);
     s.behind = c.take<float>(states);
-    s.behind1 = c.take<float>(states);
     s.f_before = c.take<float>((size_t)n_seg * heads);
     s.f_behind = c.take<float>((size_t)n_seg * heads);
-    s.gap = c.take<float>(n_seg);
-    s.slope = c.take<double>((size_t)((dk + 31) / 32) * n_seg * heads);
+    s.slope = c.take<double>((size_t)2 * attn_tiles(dk) * n_seg * heads);
     s.bytes = c.used;
     return s;
 }
 
-template <typename T, bool kRev, bool kSlope>
-void states(AttnPass p, bool whole_rows, hipStream_t stream) {
+template <typename T, bool kRev> void states(AttnPass p, bool whole_rows, hipStream_t stream) {
     p.tiles = attn_tiles(p.dc);
     pass_dispatch<T>(p.da, attn_tile(p.dc), whole_rows, [&](auto da, auto dct, auto whole) {
         hipLaunchKernelGGL((attn_state_kernel<T, decltype(da)::value, decltype(dct)::value,
-                                              decltype(whole)::value, kRev, kSlope>),
+                                              decltype(whole)::value, kRev>),
                            pass_grid(p), dim3(kAttnThreads), 0, stream, p);
     });
-    hipLaunchKernelGGL((attn_scan_kernel<kRev, kSlope>), scan_grid(p), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(attn_scan_kernel<kRev>, scan_grid(p), dim3(256), 0, stream, p);
 }
 
-// (dk takes three parts also without the rates' gradient, which must not change it)
-template <typename T, bool kRev, int NS, bool kSlope>
+template <typename T, bool kRev, int NS, int kDots>
 void pass(AttnPass p, bool whole_rows, hipStream_t stream) {
-    const int dct = bwd_tile(p.da, p.dc, kSlope, sizeof(T) == 4 ? SBC_F32 : SBC_BF16);
-    p.tiles = (p.dc + dct - 1) / dct;
-    pass_dispatch<T>(p.da, dct, whole_rows, [&](auto da, auto dct, auto whole) {
-        constexpr int DA = decltype(da)::value, DCT = decltype(dct)::value;
-        if constexpr (!(kSlope && sizeof(T) == 4 && DA > 96 && DCT > 32))
-            hipLaunchKernelGGL(
-                (attn_pass_kernel<T, DA, DCT, decltype(whole)::value, kRev, NS, kSlope>),
-                pass_grid(p), dim3(kAttnThreads), 0, stream, p);
+    p.tiles = attn_tiles(p.dc);
+    pass_dispatch<T>(p.da, attn_tile(p.dc), whole_rows, [&](auto da, auto dct, auto whole) {
+        hipLaunchKernelGGL((attn_pass_kernel<T, decltype(da)::value, decltype(dct)::value,
+                                             decltype(whole)::value, kRev, NS, kDots>),
+                           pass_grid(p), dim3(kAttnThreads), 0, stream, p);
     });
+}
+
+template <typename T>
+void grad(const GradPass &g, bool whole_rows, bool slope, hipStream_t stream) {
+    auto run = [&](auto dk, auto dv, auto whole) {
+        constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
+        constexpr bool W = decltype(whole)::value;
+        if (slope)
+            hipLaunchKernelGGL((attn_grad_kernel<T, DK, DV, W, true>), pass_grid(g.p),
+                               dim3(kAttnThreads), 0, stream, g);
+        else
+            hipLaunchKernelGGL((attn_grad_kernel<T, DK, DV, W, false>), pass_grid(g.p),
+                               dim3(kAttnThreads), 0, stream, g);
+    };
+    using I32 = std::integral_constant<int, 32>;
+    using I64 = std::integral_constant<int, 64>;
+    if (!whole_rows)
+        run(I64{}, I64{}, std::false_type{});
+    else if (g.p.da <= 32 && g.p.dc <= 32)
+        run(I32{}, I32{}, std::true_type{});
+    else
+        run(I64{}, I64{}, std::true_type{});
 }
 
 template <typename T>
@@ -114,9 +137,8 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
         p.da = keys ? a->dk : a->dv;
         p.dc = keys ? a->dv : a->dk;
         p.carry = back ? s.behind : s.before;
-        p.carry1 = s.behind1;
         p.factor = back ? s.f_behind : s.f_before;
-        p.gap = s.gap;
+        p.before = s.before;
         // states lie as [dk, dv]
         p.carry_i = keys ? a->dv : 1;
         p.carry_j = keys ? 1 : a->dv;
@@ -124,32 +146,46 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     };
     if (base.n_seg > 1) {
         trace_before("attn_bwd_state", stream);
-        states<T, false, false>(make(q, k, v, q, true, false), whole, stream);
-        const AttnPass back = make(k, q, dO, k, true, true);
-        if (drates)
-            states<T, true, true>(back, whole, stream);
-        else
-            states<T, true, false>(back, whole, stream);
+        states<T, false>(make(q, k, v, q, true, false), whole, stream);
+        states<T, true>(make(k, q, dO, k, true, true), whole, stream);
         trace_after("attn_bwd_state", stream);
     }
-    constexpr int NS = sizeof(T) == 4 ? 3 : 2;
+    // The states that meet the rates' gradient have three parts (and have them without it,
+    // so that it changes no other gradient); dv has nothing to do with it.
     trace_before("attn_bwd", stream);
-    pass<T, false, NS, false>(make(dO, v, k, dq, false, false), whole, stream);
-    pass<T, true, NS, false>(make(k, q, dO, dv, true, true), whole, stream);
-    AttnPass pk = make(v, dO, q, dk, false, true);
+    const int32_t tiles = attn_tiles(a->dk), parts = tiles * base.n_seg;
+    AttnPass pq = make(dO, v, k, dq, false, false);
     if (drates) {
-        pk.x = k;
-        pk.slope = s.slope;
-        pass<T, true, 3, true>(pk, whole, stream);
+        pq.x = q;
+        pq.slope = s.slope;
+        pass<T, false, 3, 1>(pq, whole, stream);
     } else {
-        pass<T, true, 3, false>(pk, whole, stream);
+        pass<T, false, 3, 0>(pq, whole, stream);
+    }
+    double *behind = s.slope + (size_t)parts * base.heads;
+    int32_t parts_behind = parts;
+    if (a->dk <= 64 && a->dv <= 64) {
+        GradPass both{make(k, q, dO, dv, true, true), k, v, dk, dv};
+        both.p.tiles = 1;
+        both.p.slope = behind;
+        parts_behind = base.n_seg;
+        grad<T>(both, whole, drates != nullptr, stream);
+    } else {
+        pass<T, true, sizeof(T) == 4 ? 3 : 2, 0>(make(k, q, dO, dv, true, true), whole, stream);
+        AttnPass pk = make(v, dO, q, dk, false, true);
+        if (drates) {
+            pk.x = k;
+            pk.slope = behind;
+            pass<T, true, 3, 2>(pk, whole, stream);
+        } else {
+            pass<T, true, 3, 0>(pk, whole, stream);
+        }
     }
     trace_after("attn_bwd", stream);
     if (drates) {
         trace_before("attn_rates", stream);
-        const int dct = bwd_tile(a->dv, a->dk, true, a->dtype);
         hipLaunchKernelGGL(attn_rates_kernel, dim3((unsigned)base.heads), dim3(256), 0, stream,
-                           s.slope, (a->dk + dct - 1) / dct * base.n_seg, base.heads, drates);
+                           s.slope, parts, behind, parts_behind, base.heads, drates);
         trace_after("attn_rates", stream);
     }
     SBC_LAUNCH_CHECK();

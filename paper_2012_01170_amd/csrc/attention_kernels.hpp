@@ -13,13 +13,13 @@ namespace {
 // the time of the last of them.  Grid: segments x heads x column tiles.  A
 // sequence's tokens are taken from the end back, and no further than their decay
 // lasts: the weights of earlier ones are exactly 0.
-template <typename T, int DA, int DCT, bool kWhole, bool kRev, bool kSlope>
+template <typename T, int DA, int DCT, bool kWhole, bool kRev>
 __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     __shared__ alignas(16) bf16_t bt[NP * kChunk * DA];
     __shared__ alignas(16) bf16_t ct[NP * kChunk * DCT];
-    __shared__ alignas(16) float wj[kChunk], wj1[kSlope ? kChunk : 4];
+    __shared__ alignas(16) float wj[kChunk];
     __shared__ float last_w;
     const int tile = blockIdx.x % p.tiles;
     const int head = (blockIdx.x / p.tiles) % p.heads;
@@ -54,15 +54,13 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
         return;
     }
     const int32_t end = time_at(p, kRev ? g0 : g1 - 1);  // the time of the sum
-    if (first) {
-        const float dt = passes ? elapsed<kRev>(end, time_at(p, kRev ? g1 : g0 - 1)) : 0.f;
-        *factor = passes ? step_factor(rate, dt) : kFresh;
-        if (kSlope && head == 0) p.gap[seg] = dt;
-    }
+    if (first)
+        *factor = !passes ? kFresh
+                          : step_factor(rate, elapsed<kRev>(end, time_at(p, kRev ? g1 : g0 - 1)));
 
-    floatx4 acc[S::kTiles], acc1[S::kTiles];
+    floatx4 acc[S::kTiles];
 #pragma unroll
-    for (int u = 0; u < S::kTiles; ++u) acc[u] = acc1[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < S::kTiles; ++u) acc[u] = floatx4{0.f, 0.f, 0.f, 0.f};
     // row l of a chunk is l tokens before the chunk's last in the pass' order
     const Rows<T> rb(p.b, head, 0), rc(p.c, head, dc0);
     Staged<T, DA, kWhole, !kRev> sb(rb, p.da);
@@ -82,10 +80,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
         const int count = hi - lo - at < kChunk ? hi - lo - at : kChunk;
         if (threadIdx.x < kChunk) {
             const int l = threadIdx.x;
-            const float dt = elapsed<kRev>(end, t_next);
-            const float w = l < count ? decay(rate2, dt) : 0.f;
+            const float w = l < count ? decay(rate2, elapsed<kRev>(end, t_next)) : 0.f;
             wj[l] = w;
-            if constexpr (kSlope) wj1[l] = w * dt;
             if (l == count - 1) last_w = w;
         }
         sb.store(bt, count, p.da);
@@ -93,7 +89,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
         __syncthreads();
         const bool spent = last_w == 0.f;
         if (at + kChunk < hi - lo && !spent) fetch(at + kChunk);
-        add_chunk<T, DA, DCT, kSlope>(bt, ct, wj, wj1, acc, acc1);
+        add_chunk<T, DA, DCT>(bt, ct, wj, acc);
         __syncthreads();
         if (spent) break;
     }
@@ -114,9 +110,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
                 if (row < p.da) {
                     float v = acc[u][r];
                     if (s0) v += kept * s0[(int64_t)row * p.dc + col];
-                    const int64_t e = (int64_t)row * p.carry_i + (int64_t)col * p.carry_j;
-                    p.carry[place + e] = v;
-                    if constexpr (kSlope) p.carry1[place + e] = acc1[u][r];
+                    p.carry[place + (int64_t)row * p.carry_i + (int64_t)col * p.carry_j] = v;
                 }
             }
     }
@@ -124,87 +118,106 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
 
 // The states that segments start from, from the sums that they hand on, in place:
 // carry[next] = sum[g] + carry[g] decayed by factor[g], the first term alone where
-// a sequence starts in g (and of their derivatives, carry1[next] = sum1[g] +
-// (carry1[g] + gap[g] carry[g]) decayed).  16 groups of 16 lanes share the segments
-// of 4 x 16 values: each joins its run of segments, the runs are joined in LDS, and
-// each run is gone through again from what comes in.  (A place that nothing hands
-// on to holds whatever its sum's place held; nothing starts from it.)
-template <bool kRev, bool kSlope>
+// a sequence starts in g.  16 groups of 16 lanes share the segments of 4 x 16
+// values: each joins its run of segments, the runs are joined in LDS, and each
+// run is gone through again from what comes in.  (A place that nothing hands on
+// to holds whatever its sum's place held; nothing starts from it.)
+template <bool kRev>
 __global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass p) {
-    __shared__ floatx4 sums[kSlope ? 2 : 1][16][16];
-    __shared__ float through[2][16];
+    __shared__ floatx4 sums[16][16];
+    __shared__ float through[16];
     const int lane = threadIdx.x % 16, run = threadIdx.x / 16;
     const int head = blockIdx.y;
     const int64_t e = ((int64_t)blockIdx.x * 16 + lane) * 4;
     const bool there = e < p.state_stride;
     const int per = (p.n_seg + 15) / 16;
     const int s0 = run * per, s1 = s0 + per < p.n_seg ? s0 + per : p.n_seg;
-    struct State {
-        floatx4 c, c1;
+    auto place = [&](int s) { return (int64_t)(kRev ? p.n_seg - 1 - s : s) * p.heads + head; };
+    auto at = [&](int s) {
+        return reinterpret_cast<floatx4 *>(p.carry + place(s) * p.state_stride + e);
     };
-    auto seg_of = [&](int s) { return kRev ? p.n_seg - 1 - s : s; };
-    auto at = [&](float *x, int s) {
-        return reinterpret_cast<floatx4 *>(
-            x + ((int64_t)seg_of(s) * p.heads + head) * p.state_stride + e);
-    };
-    auto step = [](const State &x, const State &sum, float f, float gap) {
-        State y = sum;
+    auto step = [](const floatx4 &c, floatx4 sum, float f) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (kSlope) y.c1[i] += apply_factor(f, fmaf(gap, x.c[i], x.c1[i]));
-            y.c[i] += apply_factor(f, x.c[i]);
-        }
-        return y;
+        for (int i = 0; i < 4; ++i) sum[i] += apply_factor(f, c[i]);
+        return sum;
     };
     constexpr int kAhead = 8;
-    State v[kAhead];
-    float f[kAhead], gap[kAhead];
+    floatx4 v[kAhead];
+    float f[kAhead];
     auto fetch = [&](int s) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
             if (s + k < s1) {
-                v[k].c = *at(p.carry, s + k);
-                if constexpr (kSlope) v[k].c1 = *at(p.carry1, s + k);
-                f[k] = p.factor[(int64_t)seg_of(s + k) * p.heads + head];
-                gap[k] = kSlope ? p.gap[seg_of(s + k)] : 0.f;
+                v[k] = *at(s + k);
+                f[k] = p.factor[place(s + k)];
             }
     };
-    State x{};
-    float f_run = 0.f, gap_run = 0.f;  // the run's decay and time
+    floatx4 c{0.f, 0.f, 0.f, 0.f};
+    float f_run = 0.f;  // the run's decay
     if (there) {
         for (int s = s0; s < s1; s += kAhead) {
             fetch(s);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
                 if (s + k < s1) {
-                    x = step(x, v[k], f[k], gap[k]);
+                    c = step(c, v[k], f[k]);
                     f_run = join_factors(f_run, f[k]);
-                    gap_run += gap[k];
                 }
         }
-        sums[0][run][lane] = x.c;
-        if constexpr (kSlope) sums[1][run][lane] = x.c1;
-        through[0][run] = f_run;
-        through[1][run] = gap_run;
+        sums[run][lane] = c;
+        through[run] = f_run;
     }
     __syncthreads();
     if (!there) return;
-    x = State{};
-    for (int r = 0; r < run; ++r) {
-        State sum{sums[0][r][lane], floatx4{}};
-        if constexpr (kSlope) sum.c1 = sums[1][r][lane];
-        x = step(x, sum, through[0][r], through[1][r]);
-    }
+    c = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < run; ++r) c = step(c, sums[r][lane], through[r]);
     for (int s = s0; s < s1; s += kAhead) {
         fetch(s);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
             if (s + k < s1) {
-                *at(p.carry, s + k) = x.c;
-                if constexpr (kSlope) *at(p.carry1, s + k) = x.c1;
-                x = step(x, v[k], f[k], gap[k]);
+                *at(s + k) = c;
+                c = step(c, v[k], f[k]);
             }
     }
+}
+
+// This lane's part of the flow into a segment from before its first token, times the
+// time from there to t_end: of the state in front of the segment, p.before, with the
+// one behind it, `acc` (laid out alike)
+template <int DA, int DCT>
+__device__ __forceinline__ double flow_in(const AttnPass &p,
+                                          const floatx4 (&acc)[StateTiles<DA, DCT>::kTiles],
+                                          float rate2, int seg, int head, int dc0, int32_t g0,
+                                          int32_t t_end) {
+    using S = StateTiles<DA, DCT>;
+    const float *before = p.before + ((int64_t)seg * p.heads + head) * p.state_stride;
+    const int32_t t_before = time_at(p, g0 - 1);
+    const int col = dc0 + S::col(), row0 = in_loop(S::row(0));
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < S::kTiles; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = row0 + 16 * u + r;
+            if (row < p.da && col < p.dc)
+                sum = fmaf(acc[u][r], before[row * p.carry_i + col * p.carry_j], sum);
+        }
+    return (double)(sum * p.scale * decay(rate2, elapsed<false>(time_at(p, g0), t_before))) *
+           (double)elapsed<false>(t_end, t_before);
+}
+
+// The sum of a workgroup's lanes to its place in p.slope
+__device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int tile, int seg,
+                                          int head) {
+    __shared__ double sums[kWaves];
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) slope += __shfl_xor(slope, m);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = slope;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        p.slope[((int64_t)tile * p.n_seg + seg) * p.heads + head] =
+            (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
 // The pass over one segment's tokens.  Grid: segments x heads x column tiles.
@@ -215,20 +228,19 @@ __global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass p) {
 // into, two where they only reach bf16 outputs (2^-17 of them, beside the
 // output's rounding of 2^-8).
 //
-// kSlope: z_i = -d y_i / d rate = scale (sum over the chunk of (t_i - t_j) P_ij c_j
-// + D(i, last) ((t_i - t_last) a_i S + a_i S1)), S1 = -dS / d rate = the sum of
-// (t_last - t_j) D b c^T.  All its terms carry their own gap, so none cancel but by
-// their signs.
-template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, bool kSlope>
+// kDots: what the pass adds to the rates' gradient (attention_bwd.hip), products of
+// x with y's two parts: that from the state, times the time from the token to the
+// last of its piece, and, with kDots == 2, that within the chunk with every pair's
+// own gap, and the flow into the segment.
+template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
 __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     __shared__ alignas(16) bf16_t bt[NP * kChunk * DA];
     __shared__ alignas(16) bf16_t ct[NP * kChunk * DCT];
     __shared__ alignas(16) bf16_t st[NS * DCT * DA];
-    __shared__ alignas(16) bf16_t st1[kSlope ? NS * DCT * DA : 8];
     __shared__ alignas(16) int32_t tj[kChunk];
-    __shared__ alignas(16) float wj[kChunk], wj1[kSlope ? kChunk : 4];
+    __shared__ alignas(16) float wj[kChunk];
     const int tile = blockIdx.x % p.tiles;
     const int head = (blockIdx.x / p.tiles) % p.heads;
     const int seg = blockIdx.x / p.tiles / p.heads;
@@ -242,6 +254,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     Staged<T, DA, kWhole, kRev> sb(rb, p.da);
     Staged<T, DCT, kWhole, kRev> sc(rc, p.dc - dc0);
     RowFrag<T, DA, kWhole, kRev> sa;
+    // (columns 16 ti + 4 g .. + 3: loaded with the others, since a load behind them would
+    // wait for them all)
+    RowFrag<T, DCT, kWhole, kRev, true> sx;
+    const Rows<T> rx(p.x, head, dc0);
     double slope = 0.0;
 
     const int32_t b_new = first_from(p, kRev ? g1 : g0);  // the first sequence that starts here
@@ -256,30 +272,37 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
         const int32_t length = hi > lo ? hi - lo : 0;
 
         int32_t t_next = 0;
-        auto fetch = [&](int32_t at) {  // the chunk `at` tokens into the piece
-            const int32_t left = length - at;
-            const int count = left < kChunk ? left : kChunk;
-            const int32_t lowest = kRev ? hi - at - count : lo + at;
+        const int32_t chunks = (length + kChunk - 1) / kChunk;
+        // The pass' chunk i: chunks are cut from the piece's first token on, also where the
+        // pass goes back (passes must agree on what is a chunk's own pair).
+        auto lowest_of = [&](int32_t i) { return lo + (kRev ? chunks - 1 - i : i) * kChunk; };
+        auto count_from = [&](int32_t lowest) {
+            return hi - lowest < kChunk ? hi - lowest : kChunk;
+        };
+        auto fetch = [&](int32_t i) {
+            const int32_t lowest = lowest_of(i);
+            const int count = count_from(lowest);
             sb.load(rb, lowest, count, p.da);
             sc.load(rc, lowest, count, p.dc - dc0);
             sa.load(ra, lowest, count, p.da, mine);
+            if constexpr (kDots > 0) sx.load(rx, lowest, count, p.dc - dc0, mine);
             if (threadIdx.x < kChunk) {
-                const int i = (int)threadIdx.x < count ? threadIdx.x : 0;
-                t_next = time_at(p, kRev ? lowest + count - 1 - i : lowest + i);
+                const int l = (int)threadIdx.x < count ? threadIdx.x : 0;
+                t_next = time_at(p, kRev ? lowest + count - 1 - l : lowest + l);
             }
         };
         if (length > 0) fetch(0);
 
-        floatx4 acc[S::kTiles], acc1[S::kTiles];
+        const int32_t t_end = length > 0 ? time_at(p, hi - 1) : 0;  // (of kDots)
+        const bool flows_in = kDots == 2 && s < g0;
+        floatx4 acc[S::kTiles];
         bool some = false;  // whether there is a state
         int32_t ref = 0;    // its time
         {
-            const float *from = nullptr, *from1 = nullptr;
+            const float *from = nullptr;
             int64_t si = 0, sj = 0;
             if (came_in) {
-                const int64_t place = ((int64_t)seg * p.heads + head) * p.state_stride;
-                from = p.carry + place;
-                if constexpr (kSlope) from1 = p.carry1 + place;
+                from = p.carry + ((int64_t)seg * p.heads + head) * p.state_stride;
                 si = p.carry_i;
                 sj = p.carry_j;
                 ref = time_at(p, kRev ? g1 : g0 - 1);
@@ -298,38 +321,33 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = row0 + 16 * u + r;
-                    const bool ok = some && row < p.da && col < p.dc;
-                    acc[u][r] = ok ? from[row * si + col * sj] : 0.f;
-                    if constexpr (kSlope) acc1[u][r] = ok ? from1[row * si + col * sj] : 0.f;
+                    acc[u][r] = some && row < p.da && col < p.dc ? from[row * si + col * sj] : 0.f;
                 }
         }
 
-        for (int32_t at = 0; at < length; at += kChunk) {
-            const int count = length - at < kChunk ? length - at : kChunk;
-            const int32_t lowest = kRev ? hi - at - count : lo + at;
-            const bool more = at + kChunk < length;
-            const bool update = more || (ends && p.state_out);
+        for (int32_t i = 0; i < chunks; ++i) {
+            const int32_t lowest = lowest_of(i);
+            const int count = count_from(lowest);
+            const bool more = i + 1 < chunks;
+            const bool update = more || (ends && p.state_out) || flows_in;
             const bool there = mine < count;
 
             __syncthreads();  // the last chunk's tiles are done with
             if (threadIdx.x < kChunk) {
-                const int32_t t_end = __shfl(t_next, count - 1);  // (the first wave has all 64)
-                const float dt = elapsed<kRev>(t_end, t_next);
-                const float w = (int)threadIdx.x < count ? decay(rate2, dt) : 0.f;
+                const int32_t last = __shfl(t_next, count - 1);  // (the first wave has all 64)
                 tj[threadIdx.x] = t_next;
-                wj[threadIdx.x] = w;
-                if constexpr (kSlope) wj1[threadIdx.x] = w * dt;
+                wj[threadIdx.x] =
+                    (int)threadIdx.x < count ? decay(rate2, elapsed<kRev>(last, t_next)) : 0.f;
             }
             sb.store(bt, count, p.da);
             sc.store(ct, count, p.dc - dc0);
-            if (some) {
-                store_state<DA, DCT, NS>(st, acc);
-                if constexpr (kSlope) store_state<DA, DCT, NS>(st1, acc1);
-            }
+            if (some) store_state<DA, DCT, NS>(st, acc);
             bf16x8 a[DA / 32][NP];  // the rows of a, as an operand
             sa.parts(a, count, p.da, mine);
+            bf16x8 xv[DCT / 32][NP];
+            if constexpr (kDots > 0) sx.parts(xv, count, p.dc - dc0, mine);
             __syncthreads();
-            if (more) fetch(at + kChunk);
+            if (more) fetch(i + 1);
 
             // P^T: keys 16 kt + 4 g + r of the lane's token, masked and decayed
             const int32_t t_mine = tj[mine], t_last = __builtin_amdgcn_readfirstlane(tj[count - 1]);
@@ -354,14 +372,14 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                         for (int r = 0; r < 4; ++r) {
                             const float dt = elapsed<kRev>(t_mine, tk[r]);
                             d[r] *= decay(rate2, dt);
-                            if constexpr (kSlope) d1[r] = d[r] * dt;
+                            if constexpr (kDots == 2) d1[r] = d[r] * dt;
                         }
                         if (kt == wave) {
                             const int behind = in_loop(l - 4 * g);
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 d[r] = r <= behind ? d[r] : 0.f;
-                                if constexpr (kSlope) d1[r] = r <= behind ? d1[r] : 0.f;
+                                if constexpr (kDots == 2) d1[r] = r <= behind ? d1[r] : 0.f;
                             }
                         }
                     }
@@ -372,46 +390,34 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                     }
                 }
                 split8<NS>(x, pf[s2]);
-                if constexpr (kSlope) split8<NS>(x1, pf1[s2]);
+                if constexpr (kDots == 2) split8<NS>(x1, pf1[s2]);
             }
-            const float dt_ref = elapsed<kRev>(t_mine, ref);
-            const float since = decay(rate2, dt_ref) * p.scale;
+            const float since = decay(rate2, elapsed<kRev>(t_mine, ref)) * p.scale;
             const int up = kRev ? count - 1 - mine : mine;
-            float dot = 0.f;
+            float dot = 0.f, dot1 = 0.f;
 #pragma unroll
             for (int ti = 0; ti < DCT / 16; ++ti) {
-                floatx4 o{0.f, 0.f, 0.f, 0.f}, z{0.f, 0.f, 0.f, 0.f}, in = o;
+                floatx4 o{0.f, 0.f, 0.f, 0.f}, o1 = o, in = o;
                 if (some) {
-                    floatx4 in1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = 0; k < DA / 32; ++k) {
                         bf16x8 sf[NS];
                         frag_row<DA, NS>(st, DCT * DA, 16 * ti + l, 32 * k + 8 * g, sf);
                         mma<NS, NP>(sf, a[k], in);
-                        if constexpr (kSlope) {
-                            frag_row<DA, NS>(st1, DCT * DA, 16 * ti + l, 32 * k + 8 * g, sf);
-                            mma<NS, NP>(sf, a[k], in1);
-                        }
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if constexpr (kSlope) z[r] = since * fmaf(dt_ref, in[r], in1[r]);
-                        in[r] *= since;
                     }
                 }
-                floatx4 o1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s2 = 0; s2 < kChunk / 32; ++s2) {
                     if (2 * s2 > wave) break;
                     bf16x8 cf[NP];
                     frag_col<DCT, NP>(ct, kChunk * DCT, 32 * s2, 16 * ti, cf);
                     mma<NP, NS>(cf, pf[s2], o);
-                    if constexpr (kSlope) mma<NP, NS>(cf, pf1[s2], o1);
+                    if constexpr (kDots == 2) mma<NP, NS>(cf, pf1[s2], o1);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
+                    in[r] *= since;
                     o[r] = fmaf(o[r], p.scale, in[r]);
-                    if constexpr (kSlope) z[r] = fmaf(o1[r], p.scale, z[r]);
                 }
                 const int c = 16 * ti + in_loop(4 * g);  // the lane's channels c .. + 3 of its token
                 const int have = p.dc - dc0 - c;
@@ -428,42 +434,27 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                         for (int r = 0; r < 4; ++r)
                             if (r < have) dst[r] = raw[r];
                     }
-                    if constexpr (kSlope) {
-                        const T *x = static_cast<const T *>(p.x.data) +
-                                     (int64_t)(lowest + up) * p.x.token_stride +
-                                     (int64_t)head * p.x.head_stride + dc0 + c;
-                        if constexpr (kWhole) {
-                            __builtin_memcpy(raw, x, sizeof(raw));
-                        } else {
+                }
+                if constexpr (kDots > 0) {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) raw[r] = r < have ? x[r] : T(0);
-                        }
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (kWhole || r < have) dot += z[r] * to_f32(raw[r]);
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = part_sum<NP>(xv[ti / 2], 4 * (ti % 2) + r);
+                        dot = fmaf(x, in[r], dot);
+                        if constexpr (kDots == 2) dot1 = fmaf(x, o1[r], dot1);
                     }
                 }
             }
-            if constexpr (kSlope) slope += (double)dot;
+            if constexpr (kDots > 0)
+                slope += (double)dot * (double)elapsed<false>(t_end, t_mine) +
+                         (double)dot1 * (double)p.scale;
             if (update) {
-                if (some) {
-                    const float gap = elapsed<kRev>(t_last, ref);
-                    const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(
-                        __float_as_uint(step_factor(rate, gap))));
-#pragma unroll
-                    for (int u = 0; u < S::kTiles; ++u)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            if constexpr (kSlope)
-                                acc1[u][r] = apply_factor(f, fmaf(gap, acc[u][r], acc1[u][r]));
-                            acc[u][r] = apply_factor(f, acc[u][r]);
-                        }
-                }
-                add_chunk<T, DA, DCT, kSlope>(bt, ct, wj, wj1, acc, acc1);
+                if (some) decay_state(step_factor(rate, elapsed<kRev>(t_last, ref)), acc);
+                add_chunk<T, DA, DCT>(bt, ct, wj, acc);
                 some = true;
                 ref = t_last;
             }
         }
+        if (flows_in) slope += flow_in<DA, DCT>(p, acc, rate2, seg, head, dc0, g0, t_end);
         if (ends && p.state_out) {
             const int col = dc0 + S::col(), row0 = in_loop(S::row(0));
             float *to = p.state_out + ((int64_t)b * p.heads + head) * p.da * p.dc;
@@ -480,16 +471,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
         }
         b += kRev ? -1 : 1;
     }
-    if constexpr (kSlope) {
-        __shared__ double sums[kWaves];
-#pragma unroll
-        for (int m = 32; m > 0; m >>= 1) slope += __shfl_xor(slope, m);
-        if ((threadIdx.x & 63) == 0) sums[wave] = slope;
-        __syncthreads();
-        if (threadIdx.x == 0)
-            p.slope[((int64_t)tile * p.n_seg + seg) * p.heads + head] =
-                (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    }
+    if constexpr (kDots > 0) put_slope(p, slope, tile, seg, head);
 }
 
 // ---------------------------------------------------------------- launches
