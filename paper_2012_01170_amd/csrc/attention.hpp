@@ -173,58 +173,84 @@ template <int D> __device__ __forceinline__ int tile_at(int row, int col) {
     constexpr int kMask = ((D / 8) & -(D / 8)) - 1;  // (as many low bits as stay inside the row)
     return row * D + (((col >> 3) ^ (row & kMask)) << 3) + (col & 7);
 }
-// 8 columns of a row
-template <int D, int N>
-__device__ __forceinline__ void frag_row(const bf16_t *tile, int plane, int row, int col,
-                                         bf16x8 (&out)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        out[i] = *reinterpret_cast<const bf16x8 *>(tile + i * plane + tile_at<D>(row, col));
-}
-// The same in the order of frag_col's rows: columns col + 4 g .. + 3 and col + 16 +
-// 4 g .. + 3 (col without the lane's own 8 g)
-template <int D, int N>
-__device__ __forceinline__ void frag_row_split(const bf16_t *tile, int plane, int row, int col,
-                                               bf16x8 (&out)[N]) {
-    const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const uint2 lo = *reinterpret_cast<const uint2 *>(tile + i * plane +
-                                                          tile_at<D>(row, col + 4 * g));
-        const uint2 hi = *reinterpret_cast<const uint2 *>(tile + i * plane +
-                                                          tile_at<D>(row, col + 16 + 4 * g));
-        out[i] = __builtin_bit_cast(bf16x8, u32x4v{lo.x, lo.y, hi.x, hi.y});
-    }
-}
-// For every lane 8 rows of one column: with l = lane & 15 and g = lane >> 4,
-// rows row0 + 4 g .. + 3 and row0 + 16 + 4 g .. + 3 of column col0 + l: the order
-// in which a product of two 16-row tiles leaves its rows in a lane's registers.
-// (The transposing read gives lane l of 16 the l-th column of the 4 x 16 block
-// whose rows' quarters the 16 lanes address.)
-template <int D, int N>
-__device__ __forceinline__ void frag_col(const bf16_t *tile, int plane, int row0, int col0,
-                                         bf16x8 (&out)[N]) {
-    typedef short s4 __attribute__((ext_vector_type(4)));
-    typedef short s8 __attribute__((ext_vector_type(8)));
-    typedef __attribute__((address_space(3))) s4 *lds_s4;
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
-    const int row = row0 + 4 * g + (l >> 2), col = col0 + 4 * (l & 3);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        bf16_t *base = const_cast<bf16_t *>(tile) + i * plane;
-        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(base + tile_at<D>(row, col)));
-        const s4 hi =
-            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(base + tile_at<D>(row + 16, col)));
-        out[i] = __builtin_bit_cast(bf16x8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-    }
-}
-
 // x, of which the compiler knows nothing: what is computed from it inside a loop
 // stays there.  (Comparisons of lanes with sizes, kept in scalar registers across the
 // chunks, took all of those and spilled.)
 __device__ __forceinline__ int in_loop(int x) {
     asm volatile("" : "+v"(x));
     return x;
+}
+
+// A lane's places in such a tile (l = lane & 15, g = lane >> 4), which are the same 16
+// rows further on: three, from which the others of the first 16 rows differ in bits of
+// the piece's number and the rest lies at constant distances.  (Left to the compiler,
+// every fragment's address took a register for the whole loop.)
+template <int D> struct LaneAt {
+    static constexpr int kMask = ((D / 8) & -(D / 8)) - 1;  // (tile_at)
+    int row0, split0, col0;
+    __device__ __forceinline__ LaneAt() {
+        const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+        row0 = in_loop(tile_at<D>(l, 8 * g));
+        split0 = in_loop(tile_at<D>(l, 4 * g));
+        col0 = in_loop(tile_at<D>(4 * g + (l >> 2), 4 * (l & 3)));
+    }
+    // `pieces` further along the row (a multiple of a power of two above the lanes' own)
+    __device__ __forceinline__ static int along(int at, int pieces) {
+        return (at ^ ((pieces & kMask) << 3)) + ((pieces & ~kMask) << 3);
+    }
+    // row l, columns 32 k + 8 g .. + 7
+    __device__ __forceinline__ int row(int k) const { return along(row0, 4 * k); }
+    // row l, columns 32 k + 16 half + 4 g .. + 3
+    __device__ __forceinline__ int split(int k, int half) const {
+        return along(split0, 4 * k + 2 * half);
+    }
+    // for frag_col: row 4 g + l / 4, columns 16 t + 4 (l & 3) .. + 3
+    __device__ __forceinline__ int col(int t) const { return along(col0, 2 * t); }
+};
+// 8 columns of row 16 t + l: k-step k of an operand
+template <int D, int N>
+__device__ __forceinline__ void frag_row(const bf16_t *tile, int plane, int t, int k,
+                                         const LaneAt<D> &at, bf16x8 (&out)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        out[i] = *reinterpret_cast<const bf16x8 *>(tile + (i * plane + 16 * t * D) + at.row(k));
+}
+// The same in the order of frag_col's rows: columns 32 k + 4 g .. + 3 and 32 k + 16 +
+// 4 g .. + 3
+template <int D, int N>
+__device__ __forceinline__ void frag_row_split(const bf16_t *tile, int plane, int t, int k,
+                                               const LaneAt<D> &at, bf16x8 (&out)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bf16_t *row = tile + (i * plane + 16 * t * D);
+        const uint2 lo = *reinterpret_cast<const uint2 *>(row + at.split(k, 0));
+        const uint2 hi = *reinterpret_cast<const uint2 *>(row + at.split(k, 1));
+        out[i] = __builtin_bit_cast(bf16x8, u32x4v{lo.x, lo.y, hi.x, hi.y});
+    }
+}
+// For every lane 8 rows of one column: with l = lane & 15 and g = lane >> 4,
+// rows 32 s + 4 g .. + 3 and 32 s + 16 + 4 g .. + 3 of column 16 t + l, at = LaneAt::col(t):
+// the order in which a product of two 16-row tiles leaves its rows in a lane's
+// registers.  (The transposing read gives lane l of 16 the l-th column of the 4 x 16
+// block whose rows' quarters the 16 lanes address.)
+template <int D, int N>
+__device__ __forceinline__ void frag_col(const bf16_t *tile, int plane, int s, int at,
+                                         bf16x8 (&out)[N]) {
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef short s8 __attribute__((ext_vector_type(8)));
+    typedef __attribute__((address_space(3))) s4 *lds_s4;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        bf16_t *base = const_cast<bf16_t *>(tile) + (i * plane + 32 * s * D);
+        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(base + at));
+        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(base + 16 * D + at));
+        out[i] = __builtin_bit_cast(bf16x8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
+}
+
+// This wave's number, in a scalar register: branches on it are then branches.
+__device__ __forceinline__ int wave_of_block() {
+    return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 }
 
 // ---------------------------------------------------------------- loads
@@ -415,16 +441,18 @@ template <int DA, int DCT> struct StateTiles {
     static constexpr int kDown = kWaves / kCols;
     static constexpr int kTiles = DA / 16 / kDown;
     static_assert(kCols * kDown == kWaves && kTiles >= 1, "tiles");
-    __device__ __forceinline__ static int wave() { return threadIdx.x >> 6; }
+    __device__ __forceinline__ static int wave() { return wave_of_block(); }
     __device__ __forceinline__ static int col0() { return 16 * (wave() % kCols); }
     __device__ __forceinline__ static int col() { return col0() + (threadIdx.x & 15); }
     __device__ __forceinline__ static int row0(int u) { return 16 * ((wave() / kCols) * kTiles + u); }
     __device__ __forceinline__ static int row(int u) { return row0(u) + 4 * ((threadIdx.x & 63) >> 4); }
 };
 
-// acc += sum over the chunk's tokens of w_j b_j c_j^T
+// acc += sum over the chunk's tokens of w_j b_j c_j^T; at_c: the lane's place in ct for
+// its wave's columns
 template <typename T, int DA, int DCT>
-__device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct, const float *w,
+__device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct,
+                                          const LaneAt<DA> &at_b, int at_c, const float *w,
                                           floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
@@ -432,7 +460,7 @@ __device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct, co
 #pragma unroll
     for (int s = 0; s < kChunk / 32; ++s) {
         bf16x8 raw[NP], cw[3];
-        frag_col<DCT, NP>(ct, kChunk * DCT, 32 * s, S::col0(), raw);
+        frag_col<DCT, NP>(ct, kChunk * DCT, s, at_c, raw);
         float x[8];
         join8<NP>(raw, x);
         const floatx4 lo = *reinterpret_cast<const floatx4 *>(w + 32 * s + 4 * g);
@@ -446,7 +474,7 @@ __device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct, co
 #pragma unroll
         for (int u = 0; u < S::kTiles; ++u) {
             bf16x8 b[NP];
-            frag_col<DA, NP>(bt, kChunk * DA, 32 * s, S::row0(u), b);
+            frag_col<DA, NP>(bt, kChunk * DA, s, at_b.col(S::row0(u) / 16), b);
             mma<NP, 3>(b, cw, acc[u]);
         }
     }
@@ -464,8 +492,8 @@ template <int N> __device__ __forceinline__ void decay_state(float f, floatx4 (&
 // The state in LDS as parts, column after column of c, its rows (the channels of a)
 // the contraction's axis
 template <int DA, int DCT, int NS>
-__device__ __forceinline__ void store_state(bf16_t *st,
-                                            const floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
+__device__ __forceinline__ void store_state(
+    bf16_t *st, const floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
     using S = StateTiles<DA, DCT>;
 #pragma unroll
     for (int u = 0; u < S::kTiles; ++u) {

@@ -22,16 +22,20 @@ struct GradPass {
 // kDots: dk's part of the rates' gradient, as in attn_pass_kernel against k; the pairs
 // of a chunk have both of their products here
 template <typename T, int DK, int DV, bool kWhole, bool kDots>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_grad_kernel(GradPass args) {
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_grad_kernel(
+    GradPass args) {
     using S = StateTiles<DK, DV>;
     constexpr int NP = kParts<T>;
     constexpr int NS = 3;                        // parts of the state
     constexpr int NO = sizeof(T) == 4 ? 3 : 2;   // of what reaches the outputs alone
     constexpr bool kRev = true;
     const AttnPass &p = args.p;
-    __shared__ alignas(16) bf16_t qt[NP * kChunk * DK];
-    __shared__ alignas(16) bf16_t gt[NP * kChunk * DV];
-    __shared__ alignas(16) bf16_t st[NS * DK * DV];
+    __shared__ alignas(16) bf16_t lds[NP * kChunk * (DK + DV) + NS * DK * DV];
+    bf16_t *const qt = lds, *const gt = lds + NP * kChunk * DK;
+    bf16_t *const st = lds + NP * kChunk * (DK + DV);
+    const LaneAt<DK> at_k;
+    const LaneAt<DV> at_v;
+    const int at_mine = at_v.col(S::col0() / 16);
     __shared__ alignas(16) int32_t tj[kChunk];
     __shared__ alignas(16) float wj[kChunk];
     const int head = blockIdx.x % p.heads;
@@ -39,7 +43,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
     const int32_t g0 = seg * p.seg_len;
     const int32_t g1 = seg == p.n_seg - 1 ? p.n : g0 + p.seg_len;
     const float rate = p.rates[head], rate2 = rate * kLog2E;
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    const int wave = wave_of_block(), l = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
     const int mine = 16 * wave + l;  // this lane's token of a chunk
     const Rows<T> rk(args.k, head, 0), rv(args.v, head, 0), rq(p.b, head, 0), rg(p.c, head, 0);
     const Rows<T> rdk(args.dk, head, 0), rdv(args.dv, head, 0);
@@ -122,7 +126,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
             const int64_t token = lowest + (there ? count - 1 - mine : 0);
             // Products of one of the tiles with the lane's row, of the tokens 16 kt + 4 g + r
             // up to the lane's own
-            auto products = [&](auto width, const bf16_t *tile, const auto &row,
+            auto products = [&](auto width, const bf16_t *tile, const auto &at, const auto &row,
                                 float(&x)[kChunk / 16][4]) {
                 constexpr int D = decltype(width)::value;
 #pragma unroll
@@ -132,7 +136,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
 #pragma unroll
                         for (int k = 0; k < D / 32; ++k) {
                             bf16x8 f[NP];
-                            frag_row_split<D, NP>(tile, kChunk * D, 16 * kt + l, 32 * k, f);
+                            frag_row_split<D, NP>(tile, kChunk * D, kt, k, at, f);
                             mma<NP, NP>(f, row[k], d);
                         }
                         if (kt == wave) {
@@ -147,8 +151,8 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
             };
             // x = D dO . v and w = D q . k, and the pairs' own part of the rates' gradient
             float x[kChunk / 16][4], w[kChunk / 16][4], pairs = 0.f;
-            products(std::integral_constant<int, DV>{}, gt, av, x);
-            products(std::integral_constant<int, DK>{}, qt, ak, w);
+            products(std::integral_constant<int, DV>{}, gt, at_v, av, x);
+            products(std::integral_constant<int, DK>{}, qt, at_k, ak, w);
 #pragma unroll
             for (int kt = 0; kt < kChunk / 16; ++kt) {
                 const int4 t = *reinterpret_cast<const int4 *>(tj + 16 * kt + 4 * g);
@@ -190,7 +194,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
 #pragma unroll
                         for (int k = 0; k < DK / 32; ++k) {
                             bf16x8 sf[NO];
-                            frag_row_split<DK, NO>(st, DK * DV, 16 * ti + l, 32 * k, sf);
+                            frag_row_split<DK, NO>(st, DK * DV, ti, k, at_k, sf);
                             mma<NO, NP>(sf, ak[k], in);
                         }
                     }
@@ -198,7 +202,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
                     for (int s2 = 0; s2 < kChunk / 32; ++s2) {
                         if (2 * s2 > wave) break;
                         bf16x8 cf[NP];
-                        frag_col<DV, NP>(gt, kChunk * DV, 32 * s2, 16 * ti, cf);
+                        frag_col<DV, NP>(gt, kChunk * DV, s2, at_v.col(ti), cf);
                         mma<NP, NO>(cf, px[s2], o);
                     }
 #pragma unroll
@@ -206,7 +210,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
                     put(rdv, 16 * ti + in_loop(4 * g), p.dc, o);
                 }
             }
-            {  // dk, and the products with k, whose channels `ak` holds
+            {  // dk, and its products with k, whose channels `ak` holds
                 bf16x8 py[kChunk / 32][NO];
 #pragma unroll
                 for (int s2 = 0; s2 < kChunk / 32; ++s2)
@@ -219,7 +223,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
 #pragma unroll
                         for (int k = 0; k < DV / 32; ++k) {
                             bf16x8 sf[NS];
-                            frag_col<DK, NS>(st, DK * DV, 32 * k, 16 * ti, sf);
+                            frag_col<DK, NS>(st, DK * DV, k, at_k.col(ti), sf);
                             mma<NS, NP>(sf, av[k], in);
                         }
                     }
@@ -227,7 +231,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
                     for (int s2 = 0; s2 < kChunk / 32; ++s2) {
                         if (2 * s2 > wave) break;
                         bf16x8 cf[NP];
-                        frag_col<DK, NP>(qt, kChunk * DK, 32 * s2, 16 * ti, cf);
+                        frag_col<DK, NP>(qt, kChunk * DK, s2, at_k.col(ti), cf);
                         mma<NP, NO>(cf, py[s2], o);
                     }
 #pragma unroll
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
             }
             if (more || flows_in) {
                 if (some) decay_state(step_factor(rate, elapsed<kRev>(t_last, ref)), acc);
-                add_chunk<T, DK, DV>(qt, gt, wj, acc);
+                add_chunk<T, DK, DV>(qt, gt, at_k, at_mine, wj, acc);
                 some = true;
                 ref = t_last;
             }

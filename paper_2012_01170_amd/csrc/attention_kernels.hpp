@@ -17,10 +17,12 @@ template <typename T, int DA, int DCT, bool kWhole, bool kRev>
 __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
-    __shared__ alignas(16) bf16_t bt[NP * kChunk * DA];
-    __shared__ alignas(16) bf16_t ct[NP * kChunk * DCT];
+    __shared__ alignas(16) bf16_t lds[NP * kChunk * (DA + DCT)];
+    bf16_t *const bt = lds, *const ct = lds + NP * kChunk * DA;
     __shared__ alignas(16) float wj[kChunk];
     __shared__ float last_w;
+    const LaneAt<DA> at_b;
+    const int at_c = LaneAt<DCT>().col(S::col0() / 16);
     const int tile = blockIdx.x % p.tiles;
     const int head = (blockIdx.x / p.tiles) % p.heads;
     const int seg = blockIdx.x / p.tiles / p.heads;
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
         __syncthreads();
         const bool spent = last_w == 0.f;
         if (at + kChunk < hi - lo && !spent) fetch(at + kChunk);
-        add_chunk<T, DA, DCT>(bt, ct, wj, acc);
+        add_chunk<T, DA, DCT>(bt, ct, at_b, at_c, wj, acc);
         __syncthreads();
         if (spent) break;
     }
@@ -236,9 +238,13 @@ template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots
 __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
-    __shared__ alignas(16) bf16_t bt[NP * kChunk * DA];
-    __shared__ alignas(16) bf16_t ct[NP * kChunk * DCT];
-    __shared__ alignas(16) bf16_t st[NS * DCT * DA];
+    // (one array, so that all tiles are at constant distances from a lane's places)
+    __shared__ alignas(16) bf16_t lds[NP * kChunk * (DA + DCT) + NS * DCT * DA];
+    bf16_t *const bt = lds, *const ct = lds + NP * kChunk * DA;
+    bf16_t *const st = lds + NP * kChunk * (DA + DCT);
+    const LaneAt<DA> at_a;
+    const LaneAt<DCT> at_c;
+    const int at_mine = at_c.col(S::col0() / 16);
     __shared__ alignas(16) int32_t tj[kChunk];
     __shared__ alignas(16) float wj[kChunk];
     const int tile = blockIdx.x % p.tiles;
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     const int32_t g1 = seg == p.n_seg - 1 ? p.n : g0 + p.seg_len;
     const float rate = p.rates[head], rate2 = rate * kLog2E;
     const int dc0 = tile * DCT;
-    const int wave = threadIdx.x >> 6, l = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    const int wave = wave_of_block(), l = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
     const int mine = 16 * wave + l;  // this lane's token of a chunk
     const Rows<T> ra(p.a, head, 0), rb(p.b, head, 0), rc(p.c, head, dc0), ry(p.y, head, dc0);
     Staged<T, DA, kWhole, kRev> sb(rb, p.da);
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
 #pragma unroll
                         for (int k = 0; k < DA / 32; ++k) {
                             bf16x8 bk[NP];
-                            frag_row<DA, NP>(bt, kChunk * DA, 16 * kt + l, 32 * k + 8 * g, bk);
+                            frag_row<DA, NP>(bt, kChunk * DA, kt, k, at_a, bk);
                             mma<NP, NP>(bk, a[k], d);
                         }
                         const int4 t = *reinterpret_cast<const int4 *>(tj + 16 * kt + 4 * g);
@@ -402,7 +408,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
 #pragma unroll
                     for (int k = 0; k < DA / 32; ++k) {
                         bf16x8 sf[NS];
-                        frag_row<DA, NS>(st, DCT * DA, 16 * ti + l, 32 * k + 8 * g, sf);
+                        frag_row<DA, NS>(st, DCT * DA, ti, k, at_a, sf);
                         mma<NS, NP>(sf, a[k], in);
                     }
                 }
@@ -410,7 +416,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                 for (int s2 = 0; s2 < kChunk / 32; ++s2) {
                     if (2 * s2 > wave) break;
                     bf16x8 cf[NP];
-                    frag_col<DCT, NP>(ct, kChunk * DCT, 32 * s2, 16 * ti, cf);
+                    frag_col<DCT, NP>(ct, kChunk * DCT, s2, at_c.col(ti), cf);
                     mma<NP, NS>(cf, pf[s2], o);
                     if constexpr (kDots == 2) mma<NP, NS>(cf, pf1[s2], o1);
                 }
@@ -449,7 +455,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                          (double)dot1 * (double)p.scale;
             if (update) {
                 if (some) decay_state(step_factor(rate, elapsed<kRev>(t_last, ref)), acc);
-                add_chunk<T, DA, DCT>(bt, ct, wj, acc);
+                add_chunk<T, DA, DCT>(bt, ct, at_a, at_mine, wj, acc);
                 some = true;
                 ref = t_last;
             }
