@@ -16,6 +16,9 @@
 // state that it hands on, attn_scan_kernel joins them, and the pass starts each
 // segment from what came in.  (One segment: the pass alone.)
 //
+// Products whose result is then split are rounded first (no contraction with the
+// split's differences), so that variants of a kernel agree in every bit.
+//
 // Decays of the state over many chunks (step_factor): while they are weak, S += S
 // expm1(-rate dt) rather than a product with exp(-rate dt), whose rounding is the
 // same in every chunk of equal length and adds up over those that S lasts.
@@ -131,6 +134,7 @@ __device__ __forceinline__ void mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB]
 // 8 values -> N parts: their first 8, 16 or 24 bits
 template <int N>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[N]) {
+#pragma clang fp contract(off)
     u32x4v h, m, l;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -433,6 +437,29 @@ template <typename T, int D, bool kWhole, bool kRev, bool kSplit = false> struct
     }
 };
 
+// A lane's channels of its token's row of an output: 16 t + 4 g .. + 3 of tile t
+template <typename T, bool kWhole> struct RowOut {
+    T *row;
+    int width;  // channels from the lane's first on; none without a token
+    __device__ __forceinline__ RowOut(const Rows<T> &x, int64_t token, int d, bool there) {
+        const int c0 = in_loop(4 * ((threadIdx.x & 63) >> 4));
+        row = const_cast<T *>(x.base) + token * x.stride + c0;
+        width = there ? d - c0 : 0;
+    }
+    __device__ __forceinline__ void put(int t, const floatx4 &o) const {
+        T raw[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) raw[r] = from_f32<T>(o[r]);
+        if constexpr (kWhole) {
+            if (16 * t < width) __builtin_memcpy(row + 16 * t, raw, sizeof(raw));
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + r < width) row[16 * t + r] = raw[r];
+        }
+    }
+};
+
 // ---------------------------------------------------------------- state
 // The state's tiles [DA x DCT] over the four waves: a wave has 16 columns and
 // kTiles tiles of 16 rows.  A lane holds column `col` and rows row(u) .. + 3.
@@ -454,6 +481,7 @@ template <typename T, int DA, int DCT>
 __device__ __forceinline__ void add_chunk(const bf16_t *bt, const bf16_t *ct,
                                           const LaneAt<DA> &at_b, int at_c, const float *w,
                                           floatx4 (&acc)[StateTiles<DA, DCT>::kTiles]) {
+#pragma clang fp contract(off)
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     const int g = (threadIdx.x & 63) >> 4;

@@ -24,6 +24,7 @@ struct GradPass {
 template <typename T, int DK, int DV, bool kWhole, bool kDots>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_grad_kernel(
     GradPass args) {
+#pragma clang fp contract(off)
     using S = StateTiles<DK, DV>;
     constexpr int NP = kParts<T>;
     constexpr int NS = 3;                        // parts of the state
@@ -155,33 +156,19 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
             products(std::integral_constant<int, DK>{}, qt, at_k, ak, w);
 #pragma unroll
             for (int kt = 0; kt < kChunk / 16; ++kt) {
+                if (kt > wave) break;  // (both are 0 from there on)
                 const int4 t = *reinterpret_cast<const int4 *>(tj + 16 * kt + 4 * g);
                 const int32_t tk[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float dt = elapsed<kRev>(t_mine, tk[r]);
-                    const float d = kt <= wave ? decay(rate2, dt) : 0.f;
+                    const float d = decay(rate2, dt);
                     w[kt][r] *= d;
-                    if constexpr (kDots)
-                        pairs = fmaf(w[kt][r] * (kt <= wave ? dt : 0.f), x[kt][r], pairs);
+                    if constexpr (kDots) pairs = fmaf(w[kt][r] * dt, x[kt][r], pairs);
                     x[kt][r] *= d;
                 }
             }
-            // a lane's channels c .. + 3 of its token
-            auto put = [&](const Rows<T> &rows, int c, int d, const floatx4 &o) {
-                if (!there || c >= d) return;
-                T raw[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) raw[r] = from_f32<T>(o[r]);
-                T *dst = const_cast<T *>(rows.base) + token * rows.stride + c;
-                if constexpr (kWhole) {
-                    __builtin_memcpy(dst, raw, sizeof(raw));
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (c + r < d) dst[r] = raw[r];
-                }
-            };
+            const RowOut<T, kWhole> out_k(rdk, token, p.da, there), out_v(rdv, token, p.dc, there);
             {  // dv
                 bf16x8 px[kChunk / 32][NO];
 #pragma unroll
@@ -207,7 +194,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
                     }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[r] = fmaf(o[r], p.scale, in[r] * since);
-                    put(rdv, 16 * ti + in_loop(4 * g), p.dc, o);
+                    out_v.put(ti, o);
                 }
             }
             {  // dk, and its products with k, whose channels `ak` holds
@@ -241,7 +228,7 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
                             dot = fmaf(part_sum<NP>(ak[ti / 2], 4 * (ti % 2) + r), in[r], dot);
                         o[r] = fmaf(o[r], p.scale, in[r]);
                     }
-                    put(rdk, 16 * ti + in_loop(4 * g), p.da, o);
+                    out_k.put(ti, o);
                 }
                 if constexpr (kDots)
                     slope += (double)dot * (double)elapsed<false>(t_end, t_mine) +

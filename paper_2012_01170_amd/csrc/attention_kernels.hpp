@@ -236,6 +236,7 @@ __device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int t
 // own gap, and the flow into the segment.
 template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
 __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
+#pragma clang fp contract(off)
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
     // (one array, so that all tiles are at constant distances from a lane's places)
@@ -399,7 +400,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                 if constexpr (kDots == 2) split8<NS>(x1, pf1[s2]);
             }
             const float since = decay(rate2, elapsed<kRev>(t_mine, ref)) * p.scale;
-            const int up = kRev ? count - 1 - mine : mine;
+            const RowOut<T, kWhole> out(ry, (int64_t)lowest + (kRev ? count - 1 - mine : mine),
+                                        p.dc - dc0, there);
             float dot = 0.f, dot1 = 0.f;
 #pragma unroll
             for (int ti = 0; ti < DCT / 16; ++ti) {
@@ -425,22 +427,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
                     in[r] *= since;
                     o[r] = fmaf(o[r], p.scale, in[r]);
                 }
-                const int c = 16 * ti + in_loop(4 * g);  // the lane's channels c .. + 3 of its token
-                const int have = p.dc - dc0 - c;
-                if (there && have > 0) {
-                    T raw[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) raw[r] = from_f32<T>(o[r]);
-                    T *dst = const_cast<T *>(ry.base) + (int64_t)lowest * ry.stride +
-                             (int64_t)up * ry.stride + c;
-                    if constexpr (kWhole) {
-                        __builtin_memcpy(dst, raw, sizeof(raw));
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (r < have) dst[r] = raw[r];
-                    }
-                }
+                out.put(ti, o);
                 if constexpr (kDots > 0) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
