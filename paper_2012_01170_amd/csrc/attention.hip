@@ -24,8 +24,7 @@ template <typename T> sbc_status forward(const AttnPass &p, bool whole_rows, hip
                                dim3(kAttnThreads), 0, stream, p);
             trace_after("attn_state", stream);
             trace_before("attn_scan", stream);
-            hipLaunchKernelGGL(attn_scan_kernel<false>, scan_grid(p), dim3(256), 0, stream,
-                               p);
+            hipLaunchKernelGGL(attn_scan_kernel, scan_grid(p), dim3(256), 0, stream, p, p);
             trace_after("attn_scan", stream);
         }
         trace_before("attn_fwd", stream);

@@ -69,15 +69,20 @@ __device__ __forceinline__ int32_t split_at(const AttnPass &p, int32_t b) {
 __device__ __forceinline__ int32_t time_at(const AttnPass &p, int32_t i) {
     return p.t ? p.t[i] : i;
 }
-// the first b in [0, n_batch] with splits[b] >= at (n_batch if none)
+// The first b in [0, n_batch] with splits[b] >= at (n_batch if none): the wave's lanes
+// take 64 places of the range at once, so that up to 64 sequences are one round of
+// loads and 4096 two (one by one, each halving of the range waited for memory).
 __device__ __forceinline__ int32_t first_from(const AttnPass &p, int32_t at) {
     int32_t lo = 0, hi = p.n_batch;
     while (lo < hi) {
-        const int32_t mid = lo + (hi - lo) / 2;
-        if (split_at(p, mid) >= at)
-            hi = mid;
-        else
-            lo = mid + 1;
+        const int32_t step = (hi - lo + 63) / 64;
+        const int64_t b = lo + (int64_t)(threadIdx.x & 63) * step;
+        const bool below = b < hi && split_at(p, (int32_t)b) < at;
+        const int32_t n = __popcll(__ballot(below));
+        if (n == 0) break;
+        const int64_t up = lo + (int64_t)n * step;
+        lo += (n - 1) * step + 1;
+        hi = up < hi ? (int32_t)up : hi;
     }
     return lo;
 }

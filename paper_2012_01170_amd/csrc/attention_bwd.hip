@@ -22,8 +22,6 @@
 namespace sbc {
 namespace {
 
-constexpr int kBwdPerCu = 2;
-
 // drates[h] = what the tokens take from the flow less what is in it, sums of the
 // workgroups' parts [parts, heads] in order
 __global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restrict__ taken,
@@ -42,10 +40,13 @@ __global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restric
     if (threadIdx.x == 0) drates[blockIdx.x] = (float)((buf[0] + buf[1]) + (buf[2] + buf[3]));
 }
 
-void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, int32_t *seg_len,
-                       int32_t *n_seg) {
+// Workgroups a CU: what its registers hold of the passes up to 64 channels in bf16 (300k
+// tokens, 4 heads: 645 us at 3, 655 at 2 with the registers for 2), else two.
+void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, sbc_dtype dtype,
+                       int32_t *seg_len, int32_t *n_seg) {
+    const bool three = dtype == SBC_BF16 && dk <= 64 && dv <= 64;
     const int32_t tiles = attn_tiles(dk < dv ? dk : dv);
-    attn_segments(n, (int64_t)heads * tiles, kBwdPerCu, seg_len, n_seg);
+    attn_segments(n, (int64_t)heads * tiles, three ? 3 : 2, seg_len, n_seg);
 }
 
 struct BwdSpace {
@@ -66,14 +67,20 @@ BwdSpace carve(void *ws, int32_t n, int32_t heads, int32_t dk, int32_t dv, int32
     return s;
 }
 
-template <typename T, bool kRev> void states(AttnPass p, bool whole_rows, hipStream_t stream) {
-    p.tiles = attn_tiles(p.dc);
-    pass_dispatch<T>(p.da, attn_tile(p.dc), whole_rows, [&](auto da, auto dct, auto whole) {
-        hipLaunchKernelGGL((attn_state_kernel<T, decltype(da)::value, decltype(dct)::value,
-                                              decltype(whole)::value, kRev>),
-                           pass_grid(p), dim3(kAttnThreads), 0, stream, p);
+// The states that the segments start from, along the sequences and back
+template <typename T>
+void states(AttnPass along, AttnPass back, bool whole_rows, hipStream_t stream) {
+    along.tiles = back.tiles = attn_tiles(along.dc);
+    pass_dispatch<T>(along.da, attn_tile(along.dc), whole_rows, [&](auto da, auto dct, auto whole) {
+        dim3 grid = pass_grid(along);
+        grid.x *= 2;
+        hipLaunchKernelGGL((attn_states_kernel<T, decltype(da)::value, decltype(dct)::value,
+                                               decltype(whole)::value>),
+                           grid, dim3(kAttnThreads), 0, stream, along, back);
     });
-    hipLaunchKernelGGL(attn_scan_kernel<kRev>, scan_grid(p), dim3(256), 0, stream, p);
+    dim3 grid = scan_grid(along);
+    grid.z = 2;
+    hipLaunchKernelGGL(attn_scan_kernel, grid, dim3(256), 0, stream, along, back);
 }
 
 template <typename T, bool kRev, int NS, int kDots>
@@ -122,7 +129,7 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     base.splits = a->splits;
     base.t = a->t;
     base.state_stride = state_stride(a->dk, a->dv);
-    backward_segments(a->n, a->heads, a->dk, a->dv, &base.seg_len, &base.n_seg);
+    backward_segments(a->n, a->heads, a->dk, a->dv, a->dtype, &base.seg_len, &base.n_seg);
     const BwdSpace s = carve(workspace, a->n, a->heads, a->dk, a->dv, base.n_seg);
     const bool whole = whole_rows(a, {&dO, &q, &k, &v});
 
@@ -146,8 +153,7 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     };
     if (base.n_seg > 1) {
         trace_before("attn_bwd_state", stream);
-        states<T, false>(make(q, k, v, q, true, false), whole, stream);
-        states<T, true>(make(k, q, dO, k, true, true), whole, stream);
+        states<T>(make(q, k, v, q, true, false), make(k, q, dO, k, true, true), whole, stream);
         trace_after("attn_bwd_state", stream);
     }
     // The states that meet the rates' gradient have three parts (and have them without it,
@@ -201,7 +207,7 @@ extern "C" size_t sbc_linear_attention_backward_workspace_size(int32_t n, int32_
                                                                int32_t dk, int32_t dv) {
     if (n < 0 || heads <= 0 || dk <= 0 || dv <= 0 || dk > 128 || dv > 128) return 0;
     int32_t seg_len, n_seg;
-    backward_segments(n, heads, dk, dv, &seg_len, &n_seg);
+    backward_segments(n, heads, dk, dv, SBC_BF16, &seg_len, &n_seg);  // (float32 has no more)
     return carve(nullptr, n, heads, dk, dv, n_seg).bytes;
 }
 

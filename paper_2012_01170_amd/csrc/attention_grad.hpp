@@ -22,8 +22,8 @@ struct GradPass {
 // kDots: dk's part of the rates' gradient, as in attn_pass_kernel against k; the pairs
 // of a chunk have both of their products here
 template <typename T, int DK, int DV, bool kWhole, bool kDots>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_grad_kernel(
-    GradPass args) {
+__device__ __forceinline__ void grad_body(const GradPass &args, int block,
+                                          PassShared<T, DK, DV, 3> &lds) {
 #pragma clang fp contract(off)
     using S = StateTiles<DK, DV>;
     constexpr int NP = kParts<T>;
@@ -31,16 +31,15 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
     constexpr int NO = sizeof(T) == 4 ? 3 : 2;   // of what reaches the outputs alone
     constexpr bool kRev = true;
     const AttnPass &p = args.p;
-    __shared__ alignas(16) bf16_t lds[NP * kChunk * (DK + DV) + NS * DK * DV];
-    bf16_t *const qt = lds, *const gt = lds + NP * kChunk * DK;
-    bf16_t *const st = lds + NP * kChunk * (DK + DV);
+    bf16_t *const qt = lds.tiles, *const gt = lds.tiles + NP * kChunk * DK;
+    bf16_t *const st = lds.tiles + NP * kChunk * (DK + DV);
+    int32_t *const tj = lds.tj;
+    float *const wj = lds.wj;
     const LaneAt<DK> at_k;
     const LaneAt<DV> at_v;
     const int at_mine = at_v.col(S::col0() / 16);
-    __shared__ alignas(16) int32_t tj[kChunk];
-    __shared__ alignas(16) float wj[kChunk];
-    const int head = blockIdx.x % p.heads;
-    const int seg = blockIdx.x / p.heads;
+    const int head = block % p.heads;
+    const int seg = block / p.heads;
     const int32_t g0 = seg * p.seg_len;
     const int32_t g1 = seg == p.n_seg - 1 ? p.n : g0 + p.seg_len;
     const float rate = p.rates[head], rate2 = rate * kLog2E;
@@ -244,6 +243,41 @@ __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1) void attn_gra
         if (flows_in) slope += flow_in<DK, DV>(p, acc, rate2, seg, head, 0, g0, t_end);
     }
     if constexpr (kDots) put_slope(p, slope, 0, seg, head);
+}
+
+// (Three workgroups a CU in bf16.)
+template <typename T, int DK, int DV, bool kWhole, bool kDots>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 3 : 1) void attn_grad_kernel(
+    GradPass args) {
+    __shared__ PassShared<T, DK, DV, 3> lds;
+    grad_body<T, DK, DV, kWhole, kDots>(args, blockIdx.x, lds);
+}
+
+// All gradients in one launch, for problems whose passes leave CUs without work: dq's
+// workgroups, then those of dk and dv together, or of dv and of dk.  kDots: with the
+// rates' gradient.
+template <typename T, int D, bool kDots>
+__global__ __launch_bounds__(kAttnThreads) void attn_grads_kernel(AttnPass dq, GradPass both) {
+    __shared__ PassShared<T, D, D, 3> lds;
+    const int first = dq.n_seg * dq.heads * dq.tiles;
+    if ((int)blockIdx.x < first)
+        pass_body<T, D, D, true, false, 3, kDots ? 1 : 0>(dq, blockIdx.x, lds);
+    else
+        grad_body<T, D, D, true, kDots>(both, blockIdx.x - first, lds);
+}
+template <typename T, int D, bool kDots>
+__global__ __launch_bounds__(kAttnThreads) void attn_wide_grads_kernel(AttnPass dq, AttnPass dv,
+                                                                       AttnPass dk) {
+    constexpr int NO = sizeof(T) == 4 ? 3 : 2;
+    __shared__ PassShared<T, D, 64, 3> lds;
+    const int first = dq.n_seg * dq.heads * dq.tiles, second = first + dv.n_seg * dv.heads * dv.tiles;
+    if ((int)blockIdx.x < first)
+        pass_body<T, D, 64, true, false, 3, kDots ? 1 : 0>(dq, blockIdx.x, lds);
+    else if ((int)blockIdx.x < second)
+        pass_body<T, D, 64, true, true, NO, 0>(dv, blockIdx.x - first,
+                                               reinterpret_cast<PassShared<T, D, 64, NO> &>(lds));
+    else
+        pass_body<T, D, 64, true, true, 3, kDots ? 2 : 0>(dk, blockIdx.x - second, lds);
 }
 
 }  // namespace

@@ -13,19 +13,23 @@ namespace {
 // the time of the last of them.  Grid: segments x heads x column tiles.  A
 // sequence's tokens are taken from the end back, and no further than their decay
 // lasts: the weights of earlier ones are exactly 0.
+template <typename T, int DA, int DCT> struct StateShared {
+    alignas(16) bf16_t tiles[kParts<T> * kChunk * (DA + DCT)];
+    alignas(16) float wj[kChunk];
+    float last_w;
+};
 template <typename T, int DA, int DCT, bool kWhole, bool kRev>
-__global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
+__device__ __forceinline__ void state_body(const AttnPass &p, int block,
+                                           StateShared<T, DA, DCT> &lds) {
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
-    __shared__ alignas(16) bf16_t lds[NP * kChunk * (DA + DCT)];
-    bf16_t *const bt = lds, *const ct = lds + NP * kChunk * DA;
-    __shared__ alignas(16) float wj[kChunk];
-    __shared__ float last_w;
+    bf16_t *const bt = lds.tiles, *const ct = lds.tiles + NP * kChunk * DA;
+    float *const wj = lds.wj;
     const LaneAt<DA> at_b;
     const int at_c = LaneAt<DCT>().col(S::col0() / 16);
-    const int tile = blockIdx.x % p.tiles;
-    const int head = (blockIdx.x / p.tiles) % p.heads;
-    const int seg = blockIdx.x / p.tiles / p.heads;
+    const int tile = block % p.tiles;
+    const int head = (block / p.tiles) % p.heads;
+    const int seg = block / p.tiles / p.heads;
     const int32_t g0 = seg * p.seg_len;
     const int32_t g1 = seg == p.n_seg - 1 ? p.n : g0 + p.seg_len;
     const float rate = p.rates[head], rate2 = rate * kLog2E;
@@ -84,12 +88,12 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
             const int l = threadIdx.x;
             const float w = l < count ? decay(rate2, elapsed<kRev>(end, t_next)) : 0.f;
             wj[l] = w;
-            if (l == count - 1) last_w = w;
+            if (l == count - 1) lds.last_w = w;
         }
         sb.store(bt, count, p.da);
         sc.store(ct, count, p.dc - dc0);
         __syncthreads();
-        const bool spent = last_w == 0.f;
+        const bool spent = lds.last_w == 0.f;
         if (at + kChunk < hi - lo && !spent) fetch(at + kChunk);
         add_chunk<T, DA, DCT>(bt, ct, at_b, at_c, wj, acc);
         __syncthreads();
@@ -118,14 +122,29 @@ __global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
     }
 }
 
+template <typename T, int DA, int DCT, bool kWhole, bool kRev>
+__global__ __launch_bounds__(kAttnThreads) void attn_state_kernel(AttnPass p) {
+    __shared__ StateShared<T, DA, DCT> lds;
+    state_body<T, DA, DCT, kWhole, kRev>(p, blockIdx.x, lds);
+}
+// Both directions in one launch, the first half of the workgroups along the sequences
+template <typename T, int DA, int DCT, bool kWhole>
+__global__ __launch_bounds__(kAttnThreads) void attn_states_kernel(AttnPass along, AttnPass back) {
+    __shared__ StateShared<T, DA, DCT> lds;
+    const int half = gridDim.x / 2;
+    if ((int)blockIdx.x < half)
+        state_body<T, DA, DCT, kWhole, false>(along, blockIdx.x, lds);
+    else
+        state_body<T, DA, DCT, kWhole, true>(back, blockIdx.x - half, lds);
+}
+
 // The states that segments start from, from the sums that they hand on, in place:
 // carry[next] = sum[g] + carry[g] decayed by factor[g], the first term alone where
 // a sequence starts in g.  16 groups of 16 lanes share the segments of 4 x 16
 // values: each joins its run of segments, the runs are joined in LDS, and each
 // run is gone through again from what comes in.  (A place that nothing hands on
 // to holds whatever its sum's place held; nothing starts from it.)
-template <bool kRev>
-__global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass p) {
+template <bool kRev> __device__ __forceinline__ void scan_body(const AttnPass &p) {
     __shared__ floatx4 sums[16][16];
     __shared__ float through[16];
     const int lane = threadIdx.x % 16, run = threadIdx.x / 16;
@@ -184,6 +203,14 @@ __global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass p) {
     }
 }
 
+// The scan along (blockIdx.z 0) and back (1)
+__global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass along, AttnPass back) {
+    if (blockIdx.z == 0)
+        scan_body<false>(along);
+    else
+        scan_body<true>(back);
+}
+
 // This lane's part of the flow into a segment from before its first token, times the
 // time from there to t_end: of the state in front of the segment, p.before, with the
 // one behind it, `acc` (laid out alike)
@@ -234,23 +261,28 @@ __device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int t
 // x with y's two parts: that from the state, times the time from the token to the
 // last of its piece, and, with kDots == 2, that within the chunk with every pair's
 // own gap, and the flow into the segment.
+template <typename T, int DA, int DCT, int NS> struct PassShared {
+    // (one array, so that all tiles are at constant distances from a lane's places)
+    alignas(16) bf16_t tiles[kParts<T> * kChunk * (DA + DCT) + NS * DCT * DA];
+    alignas(16) int32_t tj[kChunk];
+    alignas(16) float wj[kChunk];
+};
 template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
-__global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
+__device__ __forceinline__ void pass_body(const AttnPass &p, int block,
+                                          PassShared<T, DA, DCT, NS> &lds) {
 #pragma clang fp contract(off)
     using S = StateTiles<DA, DCT>;
     constexpr int NP = kParts<T>;
-    // (one array, so that all tiles are at constant distances from a lane's places)
-    __shared__ alignas(16) bf16_t lds[NP * kChunk * (DA + DCT) + NS * DCT * DA];
-    bf16_t *const bt = lds, *const ct = lds + NP * kChunk * DA;
-    bf16_t *const st = lds + NP * kChunk * (DA + DCT);
+    bf16_t *const bt = lds.tiles, *const ct = lds.tiles + NP * kChunk * DA;
+    bf16_t *const st = lds.tiles + NP * kChunk * (DA + DCT);
+    int32_t *const tj = lds.tj;
+    float *const wj = lds.wj;
     const LaneAt<DA> at_a;
     const LaneAt<DCT> at_c;
     const int at_mine = at_c.col(S::col0() / 16);
-    __shared__ alignas(16) int32_t tj[kChunk];
-    __shared__ alignas(16) float wj[kChunk];
-    const int tile = blockIdx.x % p.tiles;
-    const int head = (blockIdx.x / p.tiles) % p.heads;
-    const int seg = blockIdx.x / p.tiles / p.heads;
+    const int tile = block % p.tiles;
+    const int head = (block / p.tiles) % p.heads;
+    const int seg = block / p.tiles / p.heads;
     const int32_t g0 = seg * p.seg_len;
     const int32_t g1 = seg == p.n_seg - 1 ? p.n : g0 + p.seg_len;
     const float rate = p.rates[head], rate2 = rate * kLog2E;
@@ -467,6 +499,14 @@ __global__ __launch_bounds__(kAttnThreads) void attn_pass_kernel(AttnPass p) {
     if constexpr (kDots > 0) put_slope(p, slope, tile, seg, head);
 }
 
+// (Three workgroups a CU in bf16 up to 64 channels, but for the products of kDots 2.)
+template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 && DA <= 64 && kDots < 2 ? 3 : 1) void
+attn_pass_kernel(AttnPass p) {
+    __shared__ PassShared<T, DA, DCT, NS> lds;
+    pass_body<T, DA, DCT, kWhole, kRev, NS, kDots>(p, blockIdx.x, lds);
+}
+
 // ---------------------------------------------------------------- launches
 // Calls f with the padded channels of a, the columns of a tile of c, and whether rows
 // are whole 16-byte pieces.  (Rows that are not take the sizes up to 64 or 128.)
@@ -494,7 +534,7 @@ template <typename T, typename F> void pass_dispatch(int32_t da, int32_t dct, bo
 }
 
 inline dim3 scan_grid(const AttnPass &p) {
-    return dim3((unsigned)grid_for(p.state_stride, 64), (unsigned)p.heads);
+    return dim3((unsigned)grid_for(p.state_stride, 64), (unsigned)p.heads, 1);
 }
 inline dim3 pass_grid(const AttnPass &p) {
     return dim3((unsigned)((int64_t)p.n_seg * p.heads * p.tiles));
