@@ -620,7 +620,7 @@ sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q, int32_t q
  *              splits[b] .. splits[b+1]-1, perhaps none; NULL: one sequence
  *   rates      [heads] float32, >= 0 and finite
  *   q, k       [n, heads, dk], v, o [n, heads, dv]: float32 or bf16 (dtype),
- *              1 <= dk, dv <= 128
+ *              1 <= dk, dv <= 128, heads <= 65535
  *   state_in   [n_batch, heads, dk, dv] float32, or NULL: zero; with t,
  *              state_time [n_batch] int32 its time
  *   state_out  the same after each sequence's last token, or NULL; with t,
@@ -628,7 +628,10 @@ sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q, int32_t q
  *              sequence those of state_in, zero without one)
  * Products are taken on the matrix cores with operands split into bf16 parts
  * (float32: three; of bf16 inputs only what is computed from them: two, and
- * three for the state) and summed in float32; o is rounded once.
+ * three for the state) and summed in float32; o is rounded once.  Sequences are
+ * taken in chunks of 64 tokens: a NaN or infinity in v reaches no other sequence
+ * and no earlier chunk, but may reach earlier tokens of its own chunk, and of
+ * float32 inputs an infinity may come out as NaN.
  * No output may overlap an input.
  * ------------------------------------------------------------------------ */
 typedef struct {

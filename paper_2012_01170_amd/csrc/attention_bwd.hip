@@ -13,9 +13,9 @@
 // X of the states that meet there.  Over a piece of the segment up to the time t_end,
 //   sum of gap * flow = X (t_end - t_before) + sum of k . dk (t_end - t_j)
 //                       - sum of q . dq (t_end - t_i).
-// What rounding adds to the flow lasts to the end of the segment.  (Without flows, by
-// a second state that carries the gaps, the sums are as good as float32 allows, and
-// the whole backward pass takes a third longer: 723 us against 549.)
+// What rounding adds to the flow lasts to the end of the segment: 4.6e-7 of the rates'
+// gradient at 11003 tokens in float32.  (Without flows, by a second state that carries
+// the gaps, 2e-7, and the whole backward pass of 300k tokens took 723 us against 669.)
 #include "attention_host.hpp"
 #include "attention_grad.hpp"
 
@@ -93,26 +93,35 @@ void pass(AttnPass p, bool whole_rows, hipStream_t stream) {
     });
 }
 
-template <typename T>
-void grad(const GradPass &g, bool whole_rows, bool slope, hipStream_t stream) {
-    auto run = [&](auto dk, auto dv, auto whole) {
-        constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
-        constexpr bool W = decltype(whole)::value;
-        if (slope)
-            hipLaunchKernelGGL((attn_grad_kernel<T, DK, DV, W, true>), pass_grid(g.p),
-                               dim3(kAttnThreads), 0, stream, g);
-        else
-            hipLaunchKernelGGL((attn_grad_kernel<T, DK, DV, W, false>), pass_grid(g.p),
-                               dim3(kAttnThreads), 0, stream, g);
-    };
-    using I32 = std::integral_constant<int, 32>;
-    using I64 = std::integral_constant<int, 64>;
+template <typename T, bool kDots>
+void grad(const GradPass &g, bool whole_rows, hipStream_t stream) {
+    const dim3 grid = pass_grid(g.p), block(kAttnThreads);
     if (!whole_rows)
-        run(I64{}, I64{}, std::false_type{});
+        hipLaunchKernelGGL((attn_grad_kernel<T, 64, 64, false, kDots>), grid, block, 0, stream, g);
     else if (g.p.da <= 32 && g.p.dc <= 32)
-        run(I32{}, I32{}, std::true_type{});
+        hipLaunchKernelGGL((attn_grad_kernel<T, 32, 32, true, kDots>), grid, block, 0, stream, g);
     else
-        run(I64{}, I64{}, std::true_type{});
+        hipLaunchKernelGGL((attn_grad_kernel<T, 64, 64, true, kDots>), grid, block, 0, stream, g);
+}
+
+template <typename T, bool kDots>
+void grads(const AttnPass &pq, const GradPass &both, hipStream_t stream) {
+    const dim3 grid(pass_grid(pq).x + pass_grid(both.p).x), block(kAttnThreads);
+    if (pq.da <= 32 && pq.dc <= 32)
+        hipLaunchKernelGGL((attn_grads_kernel<T, 32, kDots>), grid, block, 0, stream, pq, both);
+    else
+        hipLaunchKernelGGL((attn_grads_kernel<T, 64, kDots>), grid, block, 0, stream, pq, both);
+}
+
+template <typename T, bool kDots>
+void wide_grads(const AttnPass &pq, const AttnPass &pv, const AttnPass &pk, hipStream_t stream) {
+    const dim3 grid(pass_grid(pq).x + pass_grid(pv).x + pass_grid(pk).x), block(kAttnThreads);
+    if (pq.da <= 96 && pq.dc <= 96)
+        hipLaunchKernelGGL((attn_wide_grads_kernel<T, 96, kDots>), grid, block, 0, stream, pq, pv,
+                           pk);
+    else
+        hipLaunchKernelGGL((attn_wide_grads_kernel<T, 128, kDots>), grid, block, 0, stream, pq, pv,
+                           pk);
 }
 
 template <typename T>
@@ -159,39 +168,49 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     // The states that meet the rates' gradient have three parts (and have them without it,
     // so that it changes no other gradient); dv has nothing to do with it.
     trace_before("attn_bwd", stream);
-    const int32_t tiles = attn_tiles(a->dk), parts = tiles * base.n_seg;
-    AttnPass pq = make(dO, v, k, dq, false, false);
-    if (drates) {
-        pq.x = q;
-        pq.slope = s.slope;
-        pass<T, false, 3, 1>(pq, whole, stream);
-    } else {
-        pass<T, false, 3, 0>(pq, whole, stream);
-    }
+    const int32_t parts = attn_tiles(a->dk) * base.n_seg;
     double *behind = s.slope + (size_t)parts * base.heads;
-    int32_t parts_behind = parts;
-    if (a->dk <= 64 && a->dv <= 64) {
-        GradPass both{make(k, q, dO, dv, true, true), k, v, dk, dv};
-        both.p.tiles = 1;
-        both.p.slope = behind;
-        parts_behind = base.n_seg;
-        grad<T>(both, whole, drates != nullptr, stream);
-    } else {
-        pass<T, true, sizeof(T) == 4 ? 3 : 2, 0>(make(k, q, dO, dv, true, true), whole, stream);
-        AttnPass pk = make(v, dO, q, dk, false, true);
-        if (drates) {
-            pk.x = k;
-            pk.slope = behind;
-            pass<T, true, 3, 2>(pk, whole, stream);
-        } else {
-            pass<T, true, 3, 0>(pk, whole, stream);
+    AttnPass pq = make(dO, v, k, dq, false, false);
+    AttnPass pv = make(k, q, dO, dv, true, true), pk = make(v, dO, q, dk, false, true);
+    pq.tiles = pk.tiles = attn_tiles(a->dk);
+    pv.tiles = attn_tiles(a->dv);
+    pq.x = q;
+    pq.slope = s.slope;
+    pk.x = k;
+    pk.slope = behind;
+    const bool narrow = a->dk <= 64 && a->dv <= 64;
+    GradPass both{pv, k, v, dk, dv};
+    both.p.tiles = 1;
+    both.p.slope = behind;
+    // Together in one launch where dq's workgroups are at most three for two CUs: of 258
+    // (11003 tokens, 3 heads) 59 us against 80 in bf16 and 148 against 154 at 40 and 72
+    // channels in float32; of 64 41 against 61; of 512 229 against 175 at 128 channels in
+    // bf16, where the joint kernel's registers leave fewer workgroups on a CU.
+    const bool together = whole && 2 * (int64_t)parts * base.heads <= 3 * (int64_t)device_cus();
+    auto run = [&](auto dots) {
+        constexpr bool kDots = decltype(dots)::value;
+        if (together && narrow)
+            grads<T, kDots>(pq, both, stream);
+        else if (together)
+            wide_grads<T, kDots>(pq, pv, pk, stream);
+        else
+            pass<T, false, 3, kDots ? 1 : 0>(pq, whole, stream);
+        if (!together && narrow) grad<T, kDots>(both, whole, stream);
+        if (!together && !narrow) {
+            pass<T, true, sizeof(T) == 4 ? 3 : 2, 0>(pv, whole, stream);
+            pass<T, true, 3, kDots ? 2 : 0>(pk, whole, stream);
         }
-    }
+    };
+    if (drates)
+        run(std::true_type{});
+    else
+        run(std::false_type{});
     trace_after("attn_bwd", stream);
     if (drates) {
         trace_before("attn_rates", stream);
         hipLaunchKernelGGL(attn_rates_kernel, dim3((unsigned)base.heads), dim3(256), 0, stream,
-                           s.slope, parts, behind, parts_behind, base.heads, drates);
+                           s.slope, parts, behind, narrow ? base.n_seg : parts, base.heads,
+                           drates);
         trace_after("attn_rates", stream);
     }
     SBC_LAUNCH_CHECK();

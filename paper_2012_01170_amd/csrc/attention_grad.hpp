@@ -57,7 +57,7 @@ __device__ __forceinline__ void grad_body(const GradPass &args, int block,
         const int32_t s = split_at(p, b), e = split_at(p, b + 1);
         if (e <= g0) break;
         const int32_t lo = s > g0 ? s : g0, hi = e < g1 ? e : g1;
-        const bool came_in = e > g1;
+        const bool came_in = e > g1 && seg < p.n_seg - 1;
         const int32_t length = hi > lo ? hi - lo : 0;
         if (length == 0) continue;
 
@@ -83,7 +83,7 @@ __device__ __forceinline__ void grad_body(const GradPass &args, int block,
         fetch(0);
 
         const int32_t t_end = time_at(p, hi - 1);  // (of kDots)
-        const bool flows_in = kDots && s < g0;
+        const bool flows_in = kDots && s < g0 && seg > 0;
         floatx4 acc[S::kTiles];
         bool some = came_in;  // whether there is a state
         int32_t ref = came_in ? time_at(p, g1) : t_end;  // its time

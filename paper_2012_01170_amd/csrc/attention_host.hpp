@@ -16,7 +16,7 @@ inline sbc_status check_attention(const sbc_attention *a) {
     if (!known_dtype(a->dtype)) return fail(SBC_ERR_INVALID_ARG, "unknown dtype");
     if (a->dk > 128 || a->dv > 128)
         return fail(SBC_ERR_UNSUPPORTED, "dk and dv must be <= 128");
-    if (a->heads > 1 << 20) return fail(SBC_ERR_UNSUPPORTED, "heads must be <= 2^20");
+    if (a->heads > 65535) return fail(SBC_ERR_UNSUPPORTED, "heads must be <= 65535");
     if (a->n > 0 && !a->rates) return fail(SBC_ERR_INVALID_ARG, "rates is null");
     return SBC_OK;
 }
@@ -45,6 +45,7 @@ inline bool whole_rows(const sbc_attention *a, std::initializer_list<const sbc_h
 
 // Segments of the token axis: as many as give every CU `per_cu` workgroups, of no
 // fewer than kLeastSeg tokens.
+// (11003 tokens, 3 heads: gradients 164 us at 64 or 128, 210 at 256.)
 constexpr int32_t kLeastSeg = 128;
 inline void attn_segments(int32_t n, int64_t blocks_a_segment, int per_cu, int32_t *seg_len,
                           int32_t *n_seg) {

@@ -44,14 +44,14 @@ __device__ __forceinline__ void state_body(const AttnPass &p, int block,
         b = first_from(p, g1) - 1;
         goes_on = b >= 0 && split_at(p, b + 1) > g1;
         lo = goes_on ? split_at(p, b) : g1;
-        passes = lo < g0;
+        passes = lo < g0 && seg > 0;
         lo = lo > g0 ? lo : g0;
         hi = g1;
     } else {
         b = first_from(p, g0) - 1;
         goes_on = b >= 0 && split_at(p, b + 1) > g0;
         hi = goes_on ? split_at(p, b + 1) : g0;
-        passes = hi > g1;
+        passes = hi > g1 && seg < p.n_seg - 1;
         hi = hi < g1 ? hi : g1;
         lo = g0;
     }
@@ -249,7 +249,8 @@ __device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int t
             (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// The pass over one segment's tokens.  Grid: segments x heads x column tiles.
+// The pass over one segment's tokens.  (Rows and times are read inside the segment, and
+// beside it only where there is another, whatever the splits say.)  Grid: segments x heads x column tiles.
 // Wave w has the chunk's tokens 16 w .. + 15 as columns of its products (b a^T,
 // S^T a^T and c^T P^T: a lane then holds keys and channels of one token, the
 // masked products P go from one product's result to the next one's operand
@@ -301,12 +302,12 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
 
     const int32_t b_new = first_from(p, kRev ? g1 : g0);  // the first sequence that starts here
     int32_t b = b_new;
-    if (kRev || (b > 0 && split_at(p, b) > g0)) --b;      // or one that came in
+    if (kRev || (seg > 0 && b > 0 && split_at(p, b) > g0)) --b;  // or one that came in
     while (kRev ? b >= 0 : b < p.n_batch) {
         const int32_t s = split_at(p, b), e = split_at(p, b + 1);
         if (kRev ? e <= g0 : (b >= b_new && s >= g1 && seg != p.n_seg - 1)) break;
         const int32_t lo = s > g0 ? s : g0, hi = e < g1 ? e : g1;
-        const bool came_in = kRev ? e > g1 : b < b_new;
+        const bool came_in = kRev ? e > g1 && seg < p.n_seg - 1 : b < b_new;
         const bool ends = !kRev && e <= g1;
         const int32_t length = hi > lo ? hi - lo : 0;
 
@@ -333,7 +334,7 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
         if (length > 0) fetch(0);
 
         const int32_t t_end = length > 0 ? time_at(p, hi - 1) : 0;  // (of kDots)
-        const bool flows_in = kDots == 2 && s < g0;
+        const bool flows_in = kDots == 2 && s < g0 && seg > 0;
         floatx4 acc[S::kTiles];
         bool some = false;  // whether there is a state
         int32_t ref = 0;    // its time
@@ -491,8 +492,8 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
                     if (row < p.da && col < p.dc) to[(int64_t)row * p.dc + col] = acc[u][r];
                 }
             if (p.time_out && tile == 0 && head == 0 && threadIdx.x == 0)
-                p.time_out[b] = length > 0 || came_in ? time_at(p, hi - 1)
-                                                      : (p.state_in ? p.state_time[b] : 0);
+                p.time_out[b] =
+                    length > 0 ? time_at(p, hi - 1) : (p.state_in ? p.state_time[b] : 0);
         }
         b += kRev ? -1 : 1;
     }
