@@ -545,3 +545,32 @@ def test_binding_refusals():
         f(big, big, big, rates[:1])
     with pytest.raises(sbc.ops.L.SbcError, match="INVALID_ARG"):
         sbc.layer_norm_forward(x[0], eps=-1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("h,dk,dv", [(8, 64, 64), (8, 32, 24), (7, 96, 72), (8, 40, 128)])
+def test_attention_of_many_workgroups(h, dk, dv, dtype):
+    """Enough segments and heads that the passes of the gradients are launched one by one
+    (fewer share a launch), and that CUs take several workgroups."""
+    n, splits = 7100, [0, 900, 901, 901, 3000, 4500, 7100]
+    print(f"[attn many] {h} {dk} {dv} {dtype}", flush=True)
+    q, k, v, do, _, t = _attn_inputs(n, h, dk, dv, dtype, 31, True)
+    rates = torch.tensor([0.0005, 0.05, 0.2, 0.01, 0.003, 1.0, 0.0, 0.1], device=DEV)[:h].clone()
+    sp = torch.tensor(splits, dtype=torch.int32, device=DEV)
+    tn = t.cpu().numpy()
+    args = (_np(rates), splits, tn, 0.2)
+    o, S, T = sbc.linear_attention_forward(q, k, v, rates, splits=sp, t=t, scale=0.2,
+                                           return_state=True)
+    ro, rS, _, size = R.attention(_np(q), _np(k), _np(v), *args)
+    sS = R.attention(abs(_np(q)), abs(_np(k)), abs(_np(v)), *args)[1]
+    _close(o, ro, _tol(ro, size, dtype), "o")
+    _close(S, rS, 2.0 ** -18 * sS + 1e-30, "state")
+    got = sbc.linear_attention_backward(do, q, k, v, rates, splits=sp, t=t, scale=0.2)
+    ref, sz, total = R.attention_grad(_np(do), _np(q), _np(k), _np(v), *args)
+    for name, g, r, s in zip(("dq", "dk", "dv"), got, ref, sz):
+        _close(g, r, _tol(r, s, dtype), name)
+    span = max(tn[min(i + 511, n - 1)] - tn[i] for i in range(n))
+    _close(got[3], ref[3], 2.0 ** -18 * sz[3] + 2.0 ** -21 * span * total, "drates")
+    less = sbc.linear_attention_backward(do, q, k, v, rates, splits=sp, t=t, scale=0.2,
+                                         need_rates=False)
+    assert all(torch.equal(a, b) for a, b in zip(got[:3], less[:3]))
