@@ -35,7 +35,9 @@ struct RotaryArgs {
 // Pairs of a lane: one vector of them, or of each of their halves
 template <typename T, bool kInterleaved> constexpr int kPairs = kInterleaved ? kVec<T> / 2 : kVec<T>;
 
-template <typename T, typename P, bool kInterleaved>
+// kTail: there are channels past the last pair (300k events: 112 us without such lanes'
+// conditions, 139 with them)
+template <typename T, typename P, bool kInterleaved, bool kTail>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     constexpr int V = kVec<T>, N = kPairs<T, kInterleaved>;
     constexpr int kVecs = kInterleaved ? 1 : 2, kBatch = kInterleaved ? 4 : 2;
@@ -55,27 +57,23 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
         return static_cast<T *>(a.out[w].data) + i * a.out[w].token_stride +
                h * a.out[w].head_stride;
     };
-    if (unit >= turning) {  // channels past the last pair are copied
-        const int c = 2 * a.pairs + (unit - turning) * V;
-        for (int j = 0; j < total; ++j) {
-            float v[V];
-            load_vec<T>(source(j) + c, a.d - c, v);
-            store_vec<T>(target(j) + c, a.d - c, v);
-        }
-        return;
-    }
+    // A lane's vectors: of pairs (of the pairs themselves, or of their first and second
+    // halves), or of channels past the last pair, which are copied.  (By a way of their
+    // own the copies' loads, one head after another, had the whole wave wait.)
+    const bool copies = kTail && unit >= turning;
     const int p0 = unit * N;
     const int have = a.pairs - p0;  // pairs of this lane, if fewer than N
-    // the lane's vectors: of the pairs themselves, or of their first and second halves
-    const int c[2] = {kInterleaved ? 2 * p0 : p0, a.pairs + p0};
-    const int width = kInterleaved ? 2 * have : have;
+    const int past = 2 * a.pairs + (unit - turning) * V;
+    const int c[2] = {copies ? past : kInterleaved ? 2 * p0 : p0, a.pairs + p0};
+    const int width[2] = {copies ? a.d - past : kInterleaved ? 2 * have : have, copies ? 0 : have};
     float x[kBatch][kVecs][V];
     auto fetch = [&](int j0) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
             if (j0 + u < total) {
 #pragma unroll
-                for (int w = 0; w < kVecs; ++w) load_vec<T>(source(j0 + u) + c[w], width, x[u][w]);
+                for (int w = 0; w < kVecs; ++w)
+                    load_vec<T>(source(j0 + u) + c[w], width[w], x[u][w]);
             }
     };
     fetch(0);
@@ -84,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     for (int k = 0; k < N; ++k) {
         cs[k] = 1.f;
         sn[k] = 0.f;
-        if (k < have) {
+        if (!copies && k < have) {
             int axis = 0;
             for (int y = 0; y + 1 < a.n_axes; ++y) axis += p0 + k >= a.upto[y];
             const double pos = (double)static_cast<const P *>(a.positions)[i * a.pos_stride + axis];
@@ -103,6 +101,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
             if (j0 + u < total) {
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
+                    if (copies) break;
                     float &p = kInterleaved ? x[u][0][2 * k] : x[u][0][k];
                     float &q = kInterleaved ? x[u][0][2 * k + 1] : x[u][kVecs - 1][k];
                     const float turned = p * cs[k] - q * sn[k];
@@ -110,23 +109,23 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
                     p = turned;
                 }
 #pragma unroll
-                for (int w = 0; w < kVecs; ++w) store_vec<T>(target(j0 + u) + c[w], width, x[u][w]);
+                for (int w = 0; w < kVecs; ++w) store_vec<T>(target(j0 + u) + c[w], width[w], x[u][w]);
             }
     }
 }
 
-template <typename T> void launch(const RotaryArgs &a, bool float_pos, bool interleaved,
-                                  hipStream_t stream) {
+template <typename T, typename P>
+void launch(const RotaryArgs &a, bool interleaved, bool tail, hipStream_t stream) {
     const dim3 grid((unsigned)grid_for((int64_t)a.n * a.units, kThreads)), block(kThreads);
-#define SBC_ROTARY(P, I) hipLaunchKernelGGL((rotary_kernel<T, P, I>), grid, block, 0, stream, a)
-    if (float_pos && interleaved)
-        SBC_ROTARY(float, true);
-    else if (float_pos)
-        SBC_ROTARY(float, false);
+#define SBC_ROTARY(I, L) hipLaunchKernelGGL((rotary_kernel<T, P, I, L>), grid, block, 0, stream, a)
+    if (interleaved && tail)
+        SBC_ROTARY(true, true);
     else if (interleaved)
-        SBC_ROTARY(int32_t, true);
+        SBC_ROTARY(true, false);
+    else if (tail)
+        SBC_ROTARY(false, true);
     else
-        SBC_ROTARY(int32_t, false);
+        SBC_ROTARY(false, false);
 #undef SBC_ROTARY
 }
 
@@ -196,10 +195,15 @@ extern "C" sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q
     if ((int64_t)n * a.units > (int64_t)1 << 31)
         return fail(SBC_ERR_UNSUPPORTED, "n and d need more than 2^31 lanes");
     trace_before("rotary", stream);
-    if (dtype == SBC_F32)
-        launch<float>(a, plan->float_positions, plan->interleaved, stream);
+    const bool interleaved = plan->interleaved, tail = 2 * pairs < d;
+    if (dtype == SBC_F32 && plan->float_positions)
+        launch<float, float>(a, interleaved, tail, stream);
+    else if (dtype == SBC_F32)
+        launch<float, int32_t>(a, interleaved, tail, stream);
+    else if (plan->float_positions)
+        launch<bf16_t, float>(a, interleaved, tail, stream);
     else
-        launch<bf16_t>(a, plan->float_positions, plan->interleaved, stream);
+        launch<bf16_t, int32_t>(a, interleaved, tail, stream);
     SBC_LAUNCH_CHECK();
     trace_after("rotary", stream);
     return SBC_OK;
