@@ -263,11 +263,6 @@ __device__ __forceinline__ int wave_of_block() {
 }
 
 // ---------------------------------------------------------------- loads
-// The tokens of a chunk in the pass' order: the first is `first`, `count` exist.
-template <bool kRev> __device__ __forceinline__ int64_t token_of(int32_t first, int l) {
-    return kRev ? (int64_t)first - l : (int64_t)first + l;
-}
-
 // Loads of 16-byte pieces of rows.  Where the channels fill whole pieces (kWhole),
 // one that does not exist (past the channels, or of no token) is read from the
 // first row's start and zeroed on its way to LDS, so that no branch lies between the
