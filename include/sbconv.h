@@ -628,10 +628,9 @@ sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q, int32_t q
  *              sequence those of state_in, zero without one)
  * Products are taken on the matrix cores with operands split into bf16 parts
  * (float32: three; of bf16 inputs only what is computed from them: two, and
- * three for the state) and summed in float32; o is rounded once.  Sequences are
- * taken in chunks of 64 tokens: a NaN or infinity in v reaches no other sequence
- * and no earlier chunk, but may reach earlier tokens of its own chunk, and of
- * float32 inputs an infinity may come out as NaN.
+ * three for the state) and summed in float32; o is rounded once.  A NaN or
+ * infinity reaches no other sequence and no earlier token (of float32 inputs an
+ * infinity may come out as NaN).
  * No output may overlap an input.
  * ------------------------------------------------------------------------ */
 typedef struct {
@@ -656,6 +655,8 @@ sbc_status sbc_linear_attention_forward(const sbc_attention *a, const sbc_heads 
  *     dk_j = scale * sum over i >= j of D_ij (dO_i . v_j) q_i,
  *     dv_j = scale * sum over i >= j of D_ij (q_i . k_j) dO_i,
  *     drates[h] = -scale * sum of (t_i - t_j) D_ij (q_i . k_j) (dO_i . v_j).
+ * Sequences are taken in chunks of 64 tokens; a NaN or infinity in one spoils no
+ * other sequence, but may spoil all of its own chunk.
  *   dO [n, heads, dv]; dq, dk [n, heads, dk], dv [n, heads, dv]: of dtype
  *   drates [heads] float32, or NULL: not wanted */
 size_t sbc_linear_attention_backward_workspace_size(int32_t n, int32_t heads, int32_t dk,

@@ -330,6 +330,19 @@ template <typename T, int D, bool kWhole, bool kRev> struct Staged {
             }
         }
     }
+    // whether any of the lane's values is infinite or NaN (after store())
+    __device__ __forceinline__ bool not_finite() const {
+        uint32_t found = 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = raw[s][i];
+                found |= (w & 0x7F800000u) == 0x7F800000u;
+                if constexpr (sizeof(T) == 2) found |= (w & 0x7F80u) == 0x7F80u;
+            }
+        return found != 0;
+    }
     __device__ __forceinline__ void store(bf16_t *tile, int count, int width) {
         if (kWhole && (count < kChunk || width < D)) {
             const int tid = in_loop(threadIdx.x);

@@ -574,3 +574,33 @@ def test_attention_of_many_workgroups(h, dk, dv, dtype):
     less = sbc.linear_attention_backward(do, q, k, v, rates, splits=sp, t=t, scale=0.2,
                                          need_rates=False)
     assert all(torch.equal(a, b) for a, b in zip(got[:3], less[:3]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,dv", [(64, 64), (40, 72), (33, 31)])
+def test_attention_forward_keeps_broken_values_from_earlier_tokens(d, dv, dtype):
+    """Infinities and NaN in q, k and v: earlier tokens, earlier and later sequences are what
+    they are without them, bit by bit or within the chunk's rounding."""
+    n, splits = 500, [0, 120, 500]
+    q, k, v, _, _, _ = _attn_inputs(n, 1, d, dv, dtype, 3, False)
+    rates = torch.tensor([0.01], device=DEV)
+    sp = torch.tensor(splits, dtype=torch.int32, device=DEV)
+    want, S0, _ = sbc.linear_attention_forward(q, k, v, rates, splits=sp, return_state=True)
+    ro, _, _, size = R.attention(_np(q), _np(k), _np(v), _np(rates), splits, None, 1.0)
+    for which, at, value in ((v, 37, float("nan")), (v, 400, float("inf")), (v, 499, -float("inf")),
+                             (k, 201, float("nan")), (q, 300, float("nan"))):
+        kept = which[at, 0, 1].item()
+        which[at, 0, 1] = value
+        o, S, _ = sbc.linear_attention_forward(q, k, v, rates, splits=sp, return_state=True)
+        b = 0 if at < 120 else 1
+        clean = torch.ones(n, dtype=torch.bool, device=DEV)
+        clean[at:splits[b + 1]] = False
+        m = clean.cpu().numpy()
+        _close(o[clean], ro[m], _tol(ro, size, dtype)[m], "earlier tokens")
+        hit = o[at, 0] if which is not v else o[at, 0, 1:2]
+        assert not torch.isfinite(hit.float()).any()
+        assert torch.equal(S[1 - b], S0[1 - b])
+        if which is v:    # the other columns know nothing of it
+            assert torch.isfinite(o[at:, 0, 2:].float()).all()
+        which[at, 0, 1] = kept
+    assert torch.equal(sbc.linear_attention_forward(q, k, v, rates, splits=sp), want)
