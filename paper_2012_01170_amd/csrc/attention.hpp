@@ -56,10 +56,10 @@ struct AttnPass {
     const int32_t *state_time;
     float *state_out;
     int32_t *time_out;
-    // for the rates' gradient (Dots): rows whose products with y are wanted, the states
-    // that come into the segments along the sequence, and the sums, [tiles, n_seg, heads]
+    // for the rates' gradient (kDots): rows whose products with y are wanted, the states
+    // that come into the segments back along the sequence, and the sums, [tiles, n_seg, heads]
     sbc_heads x;
-    const float *before;
+    const float *behind;
     double *slope;
 };
 

@@ -7,32 +7,35 @@
 //
 // The rates' gradient.  With P_ij the term of a pair (its decay, both products and the
 // scale), drate = - sum of (t_i - t_j) P_ij.  A chunk's own pairs are summed as they
-// are.  Of the others, the sum of P_ij over the pairs that cross a point of the
-// sequence is a flow: it grows by k_j . dk_j (the part of dk_j from the state) behind
-// token j, falls by q_i . dq_i behind token i, and comes into a segment as the product
-// X of the states that meet there.  Over a piece of the segment up to the time t_end,
-//   sum of gap * flow = X (t_end - t_before) + sum of k . dk (t_end - t_j)
-//                       - sum of q . dq (t_end - t_i).
-// What rounding adds to the flow lasts to the end of the segment: 4.6e-7 of the rates'
-// gradient at 11003 tokens in float32.  (Without flows, by a second state that carries
-// the gaps, 2e-7, and the whole backward pass of 300k tokens took 723 us against 669.)
+// are.  The gap of any other is cut at the ends T of the chunks between:
+//   t_i - t_j = (T_c(j) - t_j) + (T_{c(i)-1} - T_c(j)) + (t_i - T_{c(i)-1}).
+// Of the first, dk's pass makes sum over j of (T - t_j) k_j . dk_j, with the part of dk_j
+// from the state, and dq's pass makes sum over i of (t_i - T) q_i . dq_i of the last.
+// The middle is carried by a second state of dq's pass along each segment,
+//   S1 <- D (S1 + dt S)  from chunk to chunk,
+// whose product with dO and q is summed for every token, and at the segment's end with
+// the state that comes in from behind; the next segment goes on with S alone, from the
+// time of this one's last token.  So every part of a gap is a factor of a term that its
+// own decay has weakened, and nothing is left to cancel: a pause, however long, adds
+// nothing to the error.  (300k tokens in bf16, 4 heads: 664 us for all gradients.  647 with
+// sums that cancel, of k . dk less q . dq times the time to the segment's end; but where 190
+// tokens with a rate of 0.05 hold pauses of 1.5e8, these are off by 4 to 11 %.)
 #include "attention_host.hpp"
 #include "attention_grad.hpp"
 
 namespace sbc {
 namespace {
 
-// drates[h] = what the tokens take from the flow less what is in it, sums of the
-// workgroups' parts [parts, heads] in order
-__global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restrict__ taken,
-                                                         int32_t n_taken,
-                                                         const double *__restrict__ given,
-                                                         int32_t n_given, int32_t heads,
+// drates[h] = - the sums of both passes' workgroups, [parts, heads], in order
+__global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restrict__ along,
+                                                         int32_t n_along,
+                                                         const double *__restrict__ back,
+                                                         int32_t n_back, int32_t heads,
                                                          float *__restrict__ drates) {
     __shared__ double buf[4];
     double s = 0.0;
-    for (int i = threadIdx.x; i < n_taken; i += 256) s += taken[(int64_t)i * heads + blockIdx.x];
-    for (int i = threadIdx.x; i < n_given; i += 256) s -= given[(int64_t)i * heads + blockIdx.x];
+    for (int i = threadIdx.x; i < n_along; i += 256) s -= along[(int64_t)i * heads + blockIdx.x];
+    for (int i = threadIdx.x; i < n_back; i += 256) s -= back[(int64_t)i * heads + blockIdx.x];
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
@@ -154,7 +157,7 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
         p.dc = keys ? a->dv : a->dk;
         p.carry = back ? s.behind : s.before;
         p.factor = back ? s.f_behind : s.f_before;
-        p.before = s.before;
+        p.behind = s.behind;
         // states lie as [dk, dv]
         p.carry_i = keys ? a->dv : 1;
         p.carry_j = keys ? 1 : a->dv;
@@ -169,7 +172,7 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     // so that it changes no other gradient); dv has nothing to do with it.
     trace_before("attn_bwd", stream);
     const int32_t parts = attn_tiles(a->dk) * base.n_seg;
-    double *behind = s.slope + (size_t)parts * base.heads;
+    double *back = s.slope + (size_t)parts * base.heads;
     AttnPass pq = make(dO, v, k, dq, false, false);
     AttnPass pv = make(k, q, dO, dv, true, true), pk = make(v, dO, q, dk, false, true);
     pq.tiles = pk.tiles = attn_tiles(a->dk);
@@ -177,11 +180,11 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     pq.x = q;
     pq.slope = s.slope;
     pk.x = k;
-    pk.slope = behind;
+    pk.slope = back;
     const bool narrow = a->dk <= 64 && a->dv <= 64;
     GradPass both{pv, k, v, dk, dv};
     both.p.tiles = 1;
-    both.p.slope = behind;
+    both.p.slope = back;
     // Together in one launch where dq's workgroups are at most three for two CUs: of 258
     // (11003 tokens, 3 heads) 59 us against 80 in bf16 and 148 against 154 at 40 and 72
     // channels in float32; of 64 41 against 61; of 512 229 against 175 at 128 channels in
@@ -209,7 +212,7 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     if (drates) {
         trace_before("attn_rates", stream);
         hipLaunchKernelGGL(attn_rates_kernel, dim3((unsigned)base.heads), dim3(256), 0, stream,
-                           s.slope, parts, behind, narrow ? base.n_seg : parts, base.heads,
+                           s.slope, parts, back, narrow ? base.n_seg : parts, base.heads,
                            drates);
         trace_after("attn_rates", stream);
     }

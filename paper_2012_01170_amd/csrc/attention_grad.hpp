@@ -19,7 +19,7 @@ struct GradPass {
     sbc_heads k, v, dk, dv;
 };
 
-// kDots: dk's part of the rates' gradient, as in attn_pass_kernel against k; the pairs
+// kDots: dk's part of the rates' gradient, as in attn_pass_kernel (2) against k; the pairs
 // of a chunk have both of their products here
 template <typename T, int DK, int DV, bool kWhole, bool kDots>
 __device__ __forceinline__ void grad_body(const GradPass &args, int block,
@@ -82,11 +82,9 @@ __device__ __forceinline__ void grad_body(const GradPass &args, int block,
         };
         fetch(0);
 
-        const int32_t t_end = time_at(p, hi - 1);  // (of kDots)
-        const bool flows_in = kDots && s < g0 && seg > 0;
         floatx4 acc[S::kTiles];
         bool some = came_in;  // whether there is a state
-        int32_t ref = came_in ? time_at(p, g1) : t_end;  // its time
+        int32_t ref = time_at(p, came_in ? g1 : hi - 1);  // its time
         {
             const float *from = p.carry + ((int64_t)seg * p.heads + head) * p.state_stride;
             const int col = S::col(), row0 = in_loop(S::row(0));
@@ -229,18 +227,17 @@ __device__ __forceinline__ void grad_body(const GradPass &args, int block,
                     }
                     out_k.put(ti, o);
                 }
-                if constexpr (kDots)
-                    slope += (double)dot * (double)elapsed<false>(t_end, t_mine) +
+                if constexpr (kDots)  // (the chunk's end comes first in the pass' order)
+                    slope += (double)dot * (double)elapsed<kRev>(t_mine, tj[0]) +
                              (double)pairs * (double)p.scale;
             }
-            if (more || flows_in) {
+            if (more) {
                 if (some) decay_state(step_factor(rate, elapsed<kRev>(t_last, ref)), acc);
                 add_chunk<T, DK, DV>(qt, gt, at_k, at_mine, wj, acc);
                 some = true;
                 ref = t_last;
             }
         }
-        if (flows_in) slope += flow_in<DK, DV>(p, acc, rate2, seg, head, 0, g0, t_end);
     }
     if constexpr (kDots) put_slope(p, slope, 0, seg, head);
 }
@@ -265,9 +262,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_grads_kernel(AttnPass dq, G
     else
         grad_body<T, D, D, true, kDots>(both, blockIdx.x - first, lds);
 }
+// (Two workgroups a CU where LDS holds them.)
 template <typename T, int D, bool kDots>
-__global__ __launch_bounds__(kAttnThreads) void attn_wide_grads_kernel(AttnPass dq, AttnPass dv,
-                                                                       AttnPass dk) {
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 && D <= 96 ? 2 : 1) void
+attn_wide_grads_kernel(AttnPass dq, AttnPass dv, AttnPass dk) {
     constexpr int NO = sizeof(T) == 4 ? 3 : 2;
     __shared__ PassShared<T, D, 64, 3> lds;
     const int first = dq.n_seg * dq.heads * dq.tiles, second = first + dv.n_seg * dv.heads * dv.tiles;

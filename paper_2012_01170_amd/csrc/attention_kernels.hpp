@@ -211,17 +211,16 @@ __global__ __launch_bounds__(256) void attn_scan_kernel(AttnPass along, AttnPass
         scan_body<true>(back);
 }
 
-// This lane's part of the flow into a segment from before its first token, times the
-// time from there to t_end: of the state in front of the segment, p.before, with the
-// one behind it, `acc` (laid out alike)
+// This lane's part of the product of two states at the end of a segment: `acc`, at the
+// time t_last of its last token, and the one that comes in from behind, p.behind (laid
+// out alike), at the time of the next token
 template <int DA, int DCT>
-__device__ __forceinline__ double flow_in(const AttnPass &p,
-                                          const floatx4 (&acc)[StateTiles<DA, DCT>::kTiles],
-                                          float rate2, int seg, int head, int dc0, int32_t g0,
-                                          int32_t t_end) {
+__device__ __forceinline__ double meet_behind(const AttnPass &p,
+                                              const floatx4 (&acc)[StateTiles<DA, DCT>::kTiles],
+                                              float rate2, int seg, int head, int dc0, int32_t g1,
+                                              int32_t t_last) {
     using S = StateTiles<DA, DCT>;
-    const float *before = p.before + ((int64_t)seg * p.heads + head) * p.state_stride;
-    const int32_t t_before = time_at(p, g0 - 1);
+    const float *behind = p.behind + ((int64_t)seg * p.heads + head) * p.state_stride;
     const int col = dc0 + S::col(), row0 = in_loop(S::row(0));
     float sum = 0.f;
 #pragma unroll
@@ -230,10 +229,9 @@ __device__ __forceinline__ double flow_in(const AttnPass &p,
         for (int r = 0; r < 4; ++r) {
             const int row = row0 + 16 * u + r;
             if (row < p.da && col < p.dc)
-                sum = fmaf(acc[u][r], before[row * p.carry_i + col * p.carry_j], sum);
+                sum = fmaf(acc[u][r], behind[row * p.carry_i + col * p.carry_j], sum);
         }
-    return (double)(sum * p.scale * decay(rate2, elapsed<false>(time_at(p, g0), t_before))) *
-           (double)elapsed<false>(t_end, t_before);
+    return (double)(sum * p.scale * decay(rate2, elapsed<false>(time_at(p, g1), t_last)));
 }
 
 // The sum of a workgroup's lanes to its place in p.slope
@@ -264,10 +262,13 @@ __device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int t
 // a token before its own; looking for them takes 1 % of the forward (300k tokens in bf16,
 // 4 heads: 236 us against 233).
 //
-// kDots: what the pass adds to the rates' gradient (attention_bwd.hip), products of
-// x with y's two parts: that from the state, times the time from the token to the
-// last of its piece, and, with kDots == 2, that within the chunk with every pair's
-// own gap, and the flow into the segment.
+// kDots: what the pass adds to the rates' gradient (attention_bwd.hip).  1, along the
+// sequence: products of x with y's part from the state S, times the time since S, and
+// with that of a second state, S1, whose terms are those of S times the time from their
+// chunk's end (or the segment's start) to the time of S; S1 takes the place of S in LDS
+// behind S's products.  2, back along it: products of x with y's part from the state,
+// times the time from the token to its chunk's end, and with that within the chunk, with
+// every pair's own gap.
 template <typename T, int DA, int DCT, int NS> struct PassShared {
     // (one array, so that all tiles are at constant distances from a lane's places)
     alignas(16) bf16_t tiles[kParts<T> * kChunk * (DA + DCT) + NS * DCT * DA];
@@ -343,10 +344,9 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
         const int32_t start = kRev ? lo + (length - 1) / kChunk * kChunk : lo;
         if (length > 0) fetch(start);
 
-        const int32_t t_end = length > 0 ? time_at(p, hi - 1) : 0;  // (of kDots)
-        const bool flows_in = kDots == 2 && s < g0 && seg > 0;
-        floatx4 acc[S::kTiles];
-        bool some = false;  // whether there is a state
+        const bool goes_on = kDots == 1 && e > g1 && seg < p.n_seg - 1;
+        floatx4 acc[S::kTiles], acc1[S::kTiles];  // S, and of kDots 1 S1
+        bool some = false, some1 = false;  // whether there is a state, and one in S1
         int32_t ref = 0;    // its time
         {
             const float *from = nullptr;
@@ -372,6 +372,7 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
                 for (int r = 0; r < 4; ++r) {
                     const int row = row0 + 16 * u + r;
                     acc[u][r] = some && row < p.da && col < p.dc ? from[row * si + col * sj] : 0.f;
+                    acc1[u][r] = 0.f;
                 }
         }
 
@@ -381,7 +382,7 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
             const int count = count_from(lowest);
             next = kRev ? lowest - kChunk : lowest + count;
             const bool more = kRev ? next >= lo : next < hi;
-            const bool update = more || (ends && p.state_out) || flows_in;
+            const bool update = more || (ends && p.state_out);
             const bool there = mine < count;
 
             __syncthreads();  // the last chunk's tiles are done with
@@ -496,9 +497,40 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
                     }
                 }
             }
-            if constexpr (kDots > 0)
-                slope += (double)dot * (double)elapsed<false>(t_end, t_mine) +
+            if constexpr (kDots == 2)  // (the chunk's end comes first in the pass' order)
+                slope += (double)dot * (double)elapsed<kRev>(t_mine, tj[0]) +
                          (double)dot1 * (double)p.scale;
+            if constexpr (kDots == 1) {
+                slope += (double)dot * (double)elapsed<kRev>(t_mine, ref);
+                if (some1) {
+                    __syncthreads();  // the products with S are done with
+                    store_state<DA, DCT, NS>(st, acc1);
+                    __syncthreads();
+#pragma unroll
+                    for (int ti = 0; ti < DCT / 16; ++ti) {
+                        floatx4 in{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = 0; k < DA / 32; ++k) {
+                            bf16x8 sf[NS];
+                            frag_row<DA, NS>(st, DCT * DA, ti, k, at_a, sf);
+                            mma<NS, NP>(sf, a[k], in);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            dot1 = fmaf(part_sum<NP>(xv[ti / 2], 4 * (ti % 2) + r), in[r], dot1);
+                    }
+                    slope += (double)(dot1 * since);
+                }
+                if (some && (more || goes_on)) {
+                    const float dt = elapsed<kRev>(t_last, ref), f = step_factor(rate, dt);
+#pragma unroll
+                    for (int u = 0; u < S::kTiles; ++u)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc1[u][r] = fmaf(dt, acc[u][r], acc1[u][r]);
+                    decay_state(f, acc1);
+                    some1 = true;
+                }
+            }
             if (update) {
                 if (some) decay_state(step_factor(rate, elapsed<kRev>(t_last, ref)), acc);
                 add_chunk<T, DA, DCT>(bt, ct, at_a, at_mine, wj, acc);
@@ -506,7 +538,10 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
                 ref = t_last;
             }
         }
-        if (flows_in) slope += flow_in<DA, DCT>(p, acc, rate2, seg, head, dc0, g0, t_end);
+        if constexpr (kDots == 1)
+            if (goes_on && some1)
+                slope += meet_behind<DA, DCT>(p, acc1, rate2, seg, head, dc0, g1,
+                                              time_at(p, g1 - 1));
         if (ends && p.state_out) {
             const int col = dc0 + S::col(), row0 = in_loop(S::row(0));
             float *to = p.state_out + ((int64_t)b * p.heads + head) * p.da * p.dc;
@@ -526,10 +561,15 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
     if constexpr (kDots > 0) put_slope(p, slope, tile, seg, head);
 }
 
-// (Three workgroups a CU in bf16 up to 64 channels, but for the products of kDots 2.)
+// Workgroups a CU that the registers are to hold: three in bf16 up to 64 channels, but for
+// the products of kDots 2; two where LDS holds two and S1 would take the second's registers.
+template <typename T, int DA, int kDots>
+constexpr int kPassBlocks = sizeof(T) == 2 && DA <= 64 && kDots < 2        ? 3
+                            : kDots == 1 && (DA <= 64 || sizeof(T) == 2) ? 2
+                                                                         : 1;
 template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 && DA <= 64 && kDots < 2 ? 3 : 1) void
-attn_pass_kernel(AttnPass p) {
+__global__ __launch_bounds__(kAttnThreads, (kPassBlocks<T, DA, kDots>)) void attn_pass_kernel(
+    AttnPass p) {
     __shared__ PassShared<T, DA, DCT, NS> lds;
     pass_body<T, DA, DCT, kWhole, kRev, NS, kDots>(p, blockIdx.x, lds);
 }

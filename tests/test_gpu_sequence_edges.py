@@ -1,0 +1,85 @@
+"""The sequence operators where rounding has the most to spoil: pauses in a stream's times.
+Against plain float64 (tests/sequence_ref.py), as tests/test_gpu_sequence.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2012_01170_amd as sbc
+from tests import sequence_ref as R
+
+pytestmark = pytest.mark.gpu
+
+DEV = torch.device("cuda:0")
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _np(x):
+    return x.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _positive(rng, n, d, dtype):
+    """One head of positive values: the gradient of a rate is then a sum of terms of one sign,
+    and its error is measured against the sum itself."""
+    return torch.from_numpy(rng.uniform(0.1, 1, (n, 1, d)).astype(np.float32)).to(DEV).to(dtype)
+
+
+# ---------------------------------------------------------------- the rates' gradient
+# Tolerance: float32 sums of products in three parts, some 2^8 roundings of 2^-24 a term, most
+# of which cancel: 2^-18 of the terms' magnitudes, each term with its own gap.
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (32, 32), (33, 31), (40, 72), (128, 128)])
+@pytest.mark.parametrize("pause", [0, 10 ** 7, 10 ** 9])
+@pytest.mark.parametrize("heads", [1, 800])
+def test_rates_gradient_with_a_pause(heads, pause, dk, dv, dtype):
+    """A stream that rests in the middle of a segment, inside a chunk.  With 800 heads (the
+    same values for all) a segment is the whole sequence, with one it is a few chunks."""
+    print(f"[rates] {heads} {pause} {dk} {dv} {dtype}", flush=True)
+    n, at = 1600, 801
+    rng = np.random.default_rng(dk + dv)
+    q, k, v, do = (_positive(rng, n, d, dtype) for d in (dk, dk, dv, dv))
+    tn = np.cumsum(rng.integers(0, 20, n))
+    tn[at:] += pause
+    t = torch.from_numpy(tn.astype(np.int32)).to(DEV)
+    rate = torch.tensor([1 / 500], device=DEV)
+    ref, size, _ = R.attention_grad(*(_np(x) for x in (do, q, k, v, rate)), [0, n], tn, 0.25)
+    got = sbc.linear_attention_backward(*(x.expand(n, heads, -1) for x in (do, q, k, v)),
+                                        rate.expand(heads).contiguous(), t=t, scale=0.25)[3]
+    assert np.abs(_np(got) - ref[3]).max() <= 2.0 ** -18 * size[3][0], (_np(got)[0], ref[3])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("splits,dk,dv", [
+    ([0, 65], 64, 64), ([0, 0, 130, 130, 200, 200], 64, 64), ([0, 1, 2, 70, 299, 300], 40, 72),
+    ([0, 256, 513], 33, 31), ([0, 700], 64, 48), ([0, 9001], 32, 32),
+    ([0, 3, 5, 4000, 4000, 6007], 128, 128),
+])
+def test_rates_gradient_of_sequences(splits, dk, dv, dtype):
+    """Rates from none at all to a memory of less than a token, by position."""
+    n, rng = splits[-1], np.random.default_rng(splits[-1])
+    rates = torch.tensor([0.0, 0.0005, 0.05, 3.0], device=DEV)
+    sp = torch.tensor(splits, dtype=torch.int32, device=DEV)
+    q, k, v, do = (_positive(rng, n, d, dtype) for d in (dk, dk, dv, dv))
+    got = sbc.linear_attention_backward(*(x.expand(n, 4, -1) for x in (do, q, k, v)), rates,
+                                        splits=sp, scale=0.25)[3]
+    for h in range(4):
+        ref, size, _ = R.attention_grad(*(_np(x) for x in (do, q, k, v, rates[h:h + 1])), splits,
+                                        None, 0.25)
+        assert abs(float(got[h]) - ref[3][0]) <= 2.0 ** -18 * size[3][0], (h, float(got[h]), ref[3])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rates_gradient_of_long_gaps_and_a_clock_that_wraps(dtype):
+    """Gaps that pass 2^24 and times that pass 2^31."""
+    n, d = 190, 32
+    rng = np.random.default_rng(0)
+    q, k, v, do = (_positive(rng, n, d, dtype) for _ in range(4))
+    t = np.cumsum(np.where(rng.random(n) < 0.05, 150_000_000, rng.integers(0, 5, n))).astype(np.int64)
+    t += 2_000_000_000 - t[90]
+    assert t[-1] > 2 ** 31 and t[-1] - t[0] < 2 ** 32
+    wrapped = torch.from_numpy(((t + 2 ** 31) % 2 ** 32 - 2 ** 31).astype(np.int32)).to(DEV)
+    for rate in (0.05, 1e-9):
+        r = torch.tensor([rate], device=DEV)
+        got = sbc.linear_attention_backward(do, q, k, v, r, t=wrapped)[3]
+        ref, size, _ = R.attention_grad(*(_np(x) for x in (do, q, k, v, r)), [0, n], t, 1.0)
+        assert abs(float(got) - ref[3][0]) <= 2.0 ** -18 * size[3][0], (rate, float(got), ref[3])
