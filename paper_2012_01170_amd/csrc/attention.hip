@@ -28,7 +28,7 @@ template <typename T> sbc_status forward(const AttnPass &p, bool whole_rows, hip
             trace_after("attn_scan", stream);
         }
         trace_before("attn_fwd", stream);
-        hipLaunchKernelGGL((attn_pass_kernel<T, DA, DCT, W, false, NS, 0>), pass_grid(p),
+        hipLaunchKernelGGL((attn_pass_kernel<T, DA, DCT, W, false, NS, 0, true>), pass_grid(p),
                            dim3(kAttnThreads), 0, stream, p);
         trace_after("attn_fwd", stream);
     });

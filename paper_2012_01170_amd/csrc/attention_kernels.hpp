@@ -257,10 +257,10 @@ __device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int t
 // into, two where they only reach bf16 outputs (2^-17 of them, beside the
 // output's rounding of 2^-8).
 //
-// A product with a masked weight is 0 times c, and NaN where c is infinite or NaN.  The
-// forward pass takes a chunk with such values in c token by token, so that none reaches
-// a token before its own; looking for them takes 1 % of the forward (300k tokens in bf16,
-// 4 heads: 236 us against 233).
+// A product with a masked weight is 0 times c, and NaN where c is infinite or NaN.
+// kCareful, the forward pass: a chunk with such values in c is taken token by token, so
+// that none reaches a token before its own; looking for them takes 1 % of the forward
+// (300k tokens in bf16, 4 heads: 236 us against 233).
 //
 // kDots: what the pass adds to the rates' gradient (attention_bwd.hip).  1, along the
 // sequence: products of x with y's part from the state S, times the time since S, and
@@ -276,7 +276,8 @@ template <typename T, int DA, int DCT, int NS> struct PassShared {
     alignas(16) float wj[kChunk];
     int32_t bad[2];  // of a chunk and the one before
 };
-template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
+template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots,
+          bool kCareful = false>
 __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
                                           PassShared<T, DA, DCT, NS> &lds) {
 #pragma clang fp contract(off)
@@ -307,7 +308,7 @@ __device__ __forceinline__ void pass_body(const AttnPass &p, int block,
     RowFrag<T, DCT, kWhole, kRev, true> sx;
     const Rows<T> rx(p.x, head, dc0);
     double slope = 0.0;
-    constexpr bool kCareful = !kRev && kDots == 0;
+    static_assert(!kCareful || (!kRev && kDots == 0), "single tokens: along the sequence, alone");
     int turn = 0;
     if (kCareful && threadIdx.x == 0) lds.bad[0] = lds.bad[1] = 0;  // (a barrier follows)
 
@@ -567,11 +568,12 @@ template <typename T, int DA, int kDots>
 constexpr int kPassBlocks = sizeof(T) == 2 && DA <= 64 && kDots < 2        ? 3
                             : kDots == 1 && (DA <= 64 || sizeof(T) == 2) ? 2
                                                                          : 1;
-template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots>
+template <typename T, int DA, int DCT, bool kWhole, bool kRev, int NS, int kDots,
+          bool kCareful = false>
 __global__ __launch_bounds__(kAttnThreads, (kPassBlocks<T, DA, kDots>)) void attn_pass_kernel(
     AttnPass p) {
     __shared__ PassShared<T, DA, DCT, NS> lds;
-    pass_body<T, DA, DCT, kWhole, kRev, NS, kDots>(p, blockIdx.x, lds);
+    pass_body<T, DA, DCT, kWhole, kRev, NS, kDots, kCareful>(p, blockIdx.x, lds);
 }
 
 // ---------------------------------------------------------------- launches

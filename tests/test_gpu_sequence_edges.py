@@ -1,4 +1,5 @@
-"""The sequence operators where rounding has the most to spoil: pauses in a stream's times.
+"""The sequence operators where rounding has the most to spoil, pauses in a stream's times,
+and infinities and NaN in the gradients.
 Against plain float64 (tests/sequence_ref.py), as tests/test_gpu_sequence.py.
 """
 import numpy as np
@@ -83,3 +84,22 @@ def test_rates_gradient_of_long_gaps_and_a_clock_that_wraps(dtype):
         got = sbc.linear_attention_backward(do, q, k, v, r, t=wrapped)[3]
         ref, size, _ = R.attention_grad(*(_np(x) for x in (do, q, k, v, r)), [0, n], t, 1.0)
         assert abs(float(got) - ref[3][0]) <= 2.0 ** -18 * size[3][0], (rate, float(got), ref[3])
+
+
+# ---------------------------------------------------------------- broken values
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,dv,h,n", [(64, 64, 1, 300), (33, 31, 1, 300), (40, 72, 1, 300),
+                                      (64, 64, 8, 7100)])
+def test_gradients_do_not_depend_on_the_rates_being_wanted(d, dv, h, n, dtype):
+    """Also where inputs hold infinities and NaN."""
+    rng = np.random.default_rng(n + d)
+    x = [torch.from_numpy(rng.standard_normal((n, h, c)).astype(np.float32)).to(DEV).to(dtype)
+         for c in (dv, d, d, dv)]
+    rates = torch.full((h,), 0.01, device=DEV)
+    for which, at, value in ((2, 40, "nan"), (2, 150, "inf"), (3, 41, "-inf"), (0, 7, "nan")):
+        x[which][at, 0, 1] = float(value)
+        with_, without = (sbc.linear_attention_backward(*x, rates, need_rates=b) for b in (True, False))
+        for a, b in zip(with_[:3], without[:3]):
+            assert torch.equal(torch.isnan(a), torch.isnan(b))
+            assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+        x[which][at, 0, 1] = 0.5
