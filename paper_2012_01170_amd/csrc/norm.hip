@@ -10,7 +10,8 @@
 // they are short; longer rows take K vectors a lane, then a whole workgroup);
 // it is read once and stays in registers, so the variance is that of the
 // differences from the mean.  Rows that do not fit a workgroup's registers are
-// read again from the cache instead (wide_* kernels).
+// read again from the cache instead (wide_* kernels), and summed in float64: a lane
+// adds up to 2^16 of their values, where float32 loses 6e-4 of the sum.
 //
 // dw and db: a lane keeps the sums of its channels over the rows that it takes,
 // the workgroup adds its groups in LDS, and norm_reduce_kernel adds the
@@ -115,6 +116,21 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(
     }
 }
 
+// The same sum over a workgroup in float64.
+struct WideSum {
+    double *buf;
+    int turn = 0;
+    __device__ __forceinline__ double operator()(double x) {
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+        double *b = buf + 4 * turn;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = x;
+        __syncthreads();
+        return (b[0] + b[1]) + (b[2] + b[3]);
+    }
+};
+
 // Rows longer than a workgroup's registers: a workgroup a row, read three times.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void wide_fwd_kernel(
@@ -122,24 +138,25 @@ __global__ __launch_bounds__(kThreads) void wide_fwd_kernel(
     const float *__restrict__ b, int32_t n, int32_t C, float eps, T *__restrict__ y,
     int64_t y_stride, float *__restrict__ mean, float *__restrict__ rstd) {
     constexpr int V = kVec<T>;
-    __shared__ float buf[8];
-    auto sum = row_sum<kThreads>(buf);
+    __shared__ double buf[8];
+    WideSum sum{buf};
     for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const T *xr = x + r * x_stride;
-        float v[V], s = 0.f;
+        float v[V];
+        double s = 0.0;
         for (int c = threadIdx.x * V; c < C; c += kThreads * V) {
             load_vec<T>(xr + c, C - c, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) s += v[i];
         }
-        const float mu = sum(s) / (float)C;
-        s = 0.f;
+        const float mu = (float)(sum(s) / C);
+        s = 0.0;
         for (int c = threadIdx.x * V; c < C; c += kThreads * V) {
             load_vec<T>(xr + c, C - c, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) s += c + i < C ? (v[i] - mu) * (v[i] - mu) : 0.f;
         }
-        const float rs = 1.0f / sqrtf(sum(s) / (float)C + eps);
+        const float rs = 1.0f / sqrtf((float)(sum(s) / C) + eps);
         if (threadIdx.x == 0) {
             if (mean) mean[r] = mu;
             if (rstd) rstd[r] = rs;
@@ -272,10 +289,11 @@ __global__ __launch_bounds__(kThreads) void wide_dx_kernel(
     const float *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
     int32_t n, int32_t C, T *__restrict__ dx, int64_t dx_stride) {
     constexpr int V = kVec<T>;
-    __shared__ float buf[8];
-    auto sum = row_sum<kThreads>(buf);
+    __shared__ double buf[8];
+    WideSum sum{buf};
     for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
-        const float mu = mean[r], rs = rstd[r], inv_c = 1.0f / (float)C;
+        const float mu = mean[r], rs = rstd[r];
+        double d1 = 0.0, d2 = 0.0;
         float s1 = 0.f, s2 = 0.f;
         for (int pass = 0; pass < 2; ++pass) {
             for (int c = threadIdx.x * V; c < C; c += kThreads * V) {
@@ -288,8 +306,8 @@ __global__ __launch_bounds__(kThreads) void wide_dx_kernel(
                     xn[i] = c + i < C ? (xn[i] - mu) * rs : 0.f;
                     if (w) g[i] *= wv[i];
                     if (pass == 0) {
-                        s1 += g[i];
-                        s2 += g[i] * xn[i];
+                        d1 += g[i];
+                        d2 += g[i] * xn[i];
                     } else {
                         g[i] = rs * (g[i] - s1 - xn[i] * s2);
                     }
@@ -297,8 +315,8 @@ __global__ __launch_bounds__(kThreads) void wide_dx_kernel(
                 if (pass == 1) store_vec<T>(dx + r * dx_stride + c, C - c, g);
             }
             if (pass == 0) {
-                s1 = sum(s1) * inv_c;
-                s2 = sum(s2) * inv_c;
+                s1 = (float)(sum(d1) / C);
+                s2 = (float)(sum(d2) / C);
             }
         }
     }

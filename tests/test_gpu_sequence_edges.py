@@ -1,5 +1,5 @@
-"""The sequence operators where rounding has the most to spoil, pauses in a stream's times,
-and infinities and NaN in the gradients.
+"""The sequence operators where rounding has the most to spoil, pauses in a stream's times
+and long rows, and infinities and NaN in the gradients.
 Against plain float64 (tests/sequence_ref.py), as tests/test_gpu_sequence.py.
 """
 import numpy as np
@@ -13,6 +13,7 @@ pytestmark = pytest.mark.gpu
 
 DEV = torch.device("cuda:0")
 F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -8       # half a unit of bf16
 
 
 def _np(x):
@@ -103,3 +104,43 @@ def test_gradients_do_not_depend_on_the_rates_being_wanted(d, dv, h, n, dtype):
             assert torch.equal(torch.isnan(a), torch.isnan(b))
             assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
         x[which][at, 0, 1] = 0.5
+
+
+# ---------------------------------------------------------------- layer norm
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("c", [20001, 1 << 20, 1 << 24])
+def test_norm_of_long_constant_rows(c, dtype):
+    """The mean of equal values is that value, and what is left of them is zero."""
+    print(f"[norm constant] {c} {dtype}", flush=True)
+    values = torch.tensor([100.1, 12345.678, -0.3, 5.0, 1e-3, 3.3e7], device=DEV).to(dtype)
+    if c >= 1 << 24:
+        values = values[:1]
+    x = values[:, None].expand(-1, c).contiguous()
+    y, mean, rstd = sbc.layer_norm_forward(x, eps=1e-5)
+    assert torch.equal(mean, values.float())
+    assert not y.any()
+    assert np.abs(_np(rstd) * 1e-5 ** 0.5 - 1).max() <= 2.0 ** -22
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("spread", [0.0, 0.1])
+@pytest.mark.parametrize("n,c", [(2, 1001), (2, 8192), (2, 20001), (2, 1 << 20), (1, 1 << 24)])
+def test_norm_gradient_of_long_rows(n, c, spread, dtype):
+    """dx of dy that lies far from zero, whose means over the row are what is taken off: some
+    2^5 roundings of 2^-24 in each of the three terms."""
+    print(f"[norm dx] {n} {c} {spread} {dtype}", flush=True)
+    rng = np.random.default_rng(c)
+    x = torch.from_numpy(rng.standard_normal((n, c)).astype(np.float32)).to(DEV).to(dtype)
+    dy = 1.1 + spread * (rng.standard_normal((n, c)) + 3 * _np(x))
+    dy = torch.from_numpy(dy.astype(np.float32)).to(DEV).to(dtype)
+    _, rm, rr = R.layer_norm(_np(x), None, None, 1e-5)
+    mean, rstd = (torch.from_numpy(a.astype(np.float32)).to(DEV) for a in (rm, rr))
+    dx, dw, db = sbc.layer_norm_backward(dy, x, None, mean, rstd)
+    rdx, rdw, rdb = R.layer_norm_grad(_np(dy), _np(x), None, _np(mean), _np(rstd))
+    xn = np.abs((_np(x) - _np(mean)[:, None]) * _np(rstd)[:, None])
+    g = np.abs(_np(dy))
+    size = _np(rstd)[:, None] * (g + g.mean(1, keepdims=True) + xn * (g * xn).mean(1, keepdims=True))
+    tol = 2.0 ** -19 * size + (U * np.abs(rdx) if dtype == BF16 else 0)
+    assert (np.abs(_np(dx) - rdx) <= tol).all(), np.abs(_np(dx) - rdx).max()
+    assert (np.abs(_np(dw) - rdw) <= 2.0 ** -19 * (g * (xn + 2.0 ** -3)).sum(0)).all()
+    assert (np.abs(_np(db) - rdb) <= 2.0 ** -19 * g.sum(0)).all()
