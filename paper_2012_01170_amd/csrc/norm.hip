@@ -9,7 +9,15 @@
 // as few as hold it at kVec elements a lane (several rows share a wave where
 // they are short; longer rows take K vectors a lane, then a whole workgroup);
 // it is read once and stays in registers, so the variance is that of the
-// differences from the mean.  Rows that do not fit a workgroup's registers are
+// differences from the mean.
+//
+// A float32 sum leaves the mean m off by some roundings, and with it all differences;
+// where the spread is small beside the mean this is most of y.  So the differences'
+// own mean, delta (they are exact where it matters), is taken off again:
+//   mean = m + delta,   var = <(x - m)^2> - delta^2,   x - mean = (x - m) - delta,
+// one sum more beside that of the squares.  Equal values leave exactly zero.
+//
+// Rows that do not fit a workgroup's registers are
 // read again from the cache instead (wide_* kernels), and summed in float64: a lane
 // adds up to 2^16 of their values, where float32 loses 6e-4 of the sum.
 //
@@ -50,6 +58,13 @@ template <int G> __device__ __forceinline__ RowSum<G> row_sum(float *buf) {
         return RowSum<G>{};
 }
 
+// rstd from the mean square of the differences from a mean that is off by delta.  (A NaN
+// stays one: fmaxf would drop it.)
+__device__ __forceinline__ float spread(float square, float delta, float eps) {
+    const float var = square - delta * delta;
+    return 1.0f / sqrtf((var < 0.f ? 0.f : var) + eps);
+}
+
 template <typename T, int G, int K>
 __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(
     const T *__restrict__ x, int64_t x_stride, const float *__restrict__ w,
@@ -81,20 +96,23 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(
             for (int i = 0; i < V; ++i) s += v[k][i];
         }
         if (r + step < n) fetch(r + step);
-        const float mu = sum(s) / (float)C;  // (exact where all values are equal)
+        const float mu = sum(s) / (float)C;
         s = 0.f;
+        float left = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * G + lane) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 v[k][i] -= mu;
+                left += c + i < C ? v[k][i] : 0.f;
                 s += c + i < C ? v[k][i] * v[k][i] : 0.f;
             }
         }
-        const float rs = 1.0f / sqrtf(sum(s) / (float)C + eps);
+        const float delta = sum(left) / (float)C;
+        const float rs = spread(sum(s) / (float)C, delta, eps);
         if (lane == 0) {
-            if (mean) mean[r] = mu;
+            if (mean) mean[r] = mu + delta;
             if (rstd) rstd[r] = rs;
         }
 #pragma unroll
@@ -106,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_kernel(
             if (b) load_f32<V>(b + c, C - c, bv);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float o = v[k][i] * rs;
+                float o = (v[k][i] - delta) * rs;
                 if (w) o *= wv[i];
                 if (b) o += bv[i];
                 v[k][i] = o;
@@ -149,14 +167,15 @@ __global__ __launch_bounds__(kThreads) void wide_fwd_kernel(
 #pragma unroll
             for (int i = 0; i < V; ++i) s += v[i];
         }
-        const float mu = (float)(sum(s) / C);
+        s = sum(s) / C;
+        const float mu = (float)s, delta = (float)(s - mu);
         s = 0.0;
         for (int c = threadIdx.x * V; c < C; c += kThreads * V) {
             load_vec<T>(xr + c, C - c, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) s += c + i < C ? (v[i] - mu) * (v[i] - mu) : 0.f;
         }
-        const float rs = 1.0f / sqrtf((float)(sum(s) / C) + eps);
+        const float rs = spread((float)(sum(s) / C), delta, eps);
         if (threadIdx.x == 0) {
             if (mean) mean[r] = mu;
             if (rstd) rstd[r] = rs;
@@ -168,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void wide_fwd_kernel(
             if (b) load_f32<V>(b + c, C - c, bv);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float o = (v[i] - mu) * rs;
+                float o = ((v[i] - mu) - delta) * rs;
                 if (w) o *= wv[i];
                 if (b) o += bv[i];
                 v[i] = o;

@@ -1,5 +1,5 @@
-"""The sequence operators where rounding has the most to spoil, pauses in a stream's times
-and long rows, and infinities and NaN in the gradients.
+"""The sequence operators where rounding has the most to spoil, pauses in a stream's times,
+long rows and rows far from zero, and infinities and NaN in the gradients.
 Against plain float64 (tests/sequence_ref.py), as tests/test_gpu_sequence.py.
 """
 import numpy as np
@@ -144,3 +144,36 @@ def test_norm_gradient_of_long_rows(n, c, spread, dtype):
     assert (np.abs(_np(dx) - rdx) <= tol).all(), np.abs(_np(dx) - rdx).max()
     assert (np.abs(_np(dw) - rdw) <= 2.0 ** -19 * (g * (xn + 2.0 ** -3)).sum(0)).all()
     assert (np.abs(_np(db) - rdb) <= 2.0 ** -19 * g.sum(0)).all()
+
+
+LENGTHS = [1, 7, 24, 513, 1001, 2049, 4096, 8192]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("c", LENGTHS)
+def test_norm_of_constant_rows(c, dtype):
+    """As the long ones."""
+    print(f"[norm constant] {c} {dtype}", flush=True)
+    values = torch.tensor([100.1, 12345.678, -0.3, 5.0, 1e-3, 3.3e7], device=DEV).to(dtype)
+    y, mean, rstd = sbc.layer_norm_forward(values[:, None].expand(-1, c).contiguous(), eps=1e-5)
+    assert torch.equal(mean, values.float())
+    assert not y.any()
+    assert np.abs(_np(rstd) * 1e-5 ** 0.5 - 1).max() <= 2.0 ** -22
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("c", LENGTHS[1:] + [20001, 1 << 20])
+def test_norm_of_rows_far_from_zero(c, dtype):
+    """Rows whose spread is small beside their mean.  The mean is rounded once (2^-24 of it)
+    from one that is exact to 2^-18 of the spread; differences from it are exact, so that y
+    knows nothing of the mean's size: 2^-18 of itself and of the spread."""
+    print(f"[norm far] {c} {dtype}", flush=True)
+    rng = np.random.default_rng(c)
+    far = 1e4 if dtype == F32 else 100.0
+    x = torch.from_numpy((far + rng.standard_normal((3, c))).astype(np.float32)).to(DEV).to(dtype)
+    y, mean, rstd = sbc.layer_norm_forward(x, eps=1e-5)
+    ry, rm, rr = R.layer_norm(_np(x), None, None, 1e-5)
+    assert (np.abs(_np(mean) - rm) <= 2.0 ** -24 * rm + 2.0 ** -18 / rr).all()
+    assert (np.abs(_np(rstd) - rr) <= 2.0 ** -18 * rr).all()
+    tol = 2.0 ** -18 * (1 + np.abs(ry)) + (U * np.abs(ry) if dtype == BF16 else 0)
+    assert (np.abs(_np(y) - ry) <= tol).all(), np.abs(_np(y) - ry).max()
