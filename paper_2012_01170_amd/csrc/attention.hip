@@ -71,15 +71,14 @@ extern "C" sbc_status sbc_linear_attention_forward(const sbc_attention *a, const
     if (a->t && (state_out != nullptr) != (time_out != nullptr))
         return fail(SBC_ERR_INVALID_ARG, "with t, state_out and time_out go together");
     if (n == 0 && (a->n_batch == 0 || !state_out)) return SBC_OK;
-    const size_t state_bytes = (size_t)a->n_batch * H * a->dk * a->dv * 4;
-    if (overlap(state_in, state_bytes, state_out, state_bytes))
-        return fail(SBC_ERR_INVALID_ARG, "state_out overlaps state_in");
-    if (overlap(state_time, (size_t)a->n_batch * 4, time_out, (size_t)a->n_batch * 4))
-        return fail(SBC_ERR_INVALID_ARG, "time_out overlaps state_time");
-    if (n > 0 && (heads_overlap(*o, H, a->dv, *q, H, a->dk, n, a->dtype) ||
-                  heads_overlap(*o, H, a->dv, *k, H, a->dk, n, a->dtype) ||
-                  heads_overlap(*o, H, a->dv, *v, H, a->dv, n, a->dtype)))
-        return fail(SBC_ERR_INVALID_ARG, "o overlaps an input");
+    const int64_t states = (int64_t)a->n_batch * H * a->dk * a->dv;
+    if (!a->t) state_time = time_out = nullptr;
+    SBC_TRY(check_apart({region_heads(o, H, n, a->dv, a->dtype), region(state_out, states, 4),
+                         region(time_out, a->n_batch, 4)},
+                        {region_heads(q, H, n, a->dk, a->dtype), region_heads(k, H, n, a->dk, a->dtype),
+                         region_heads(v, H, n, a->dv, a->dtype), region(state_in, states, 4),
+                         region(state_time, a->n_batch, 4), region(a->rates, H, 4),
+                         region(a->splits, (int64_t)a->n_batch + 1, 4), region(a->t, n, 4)}));
     if (!a->rates) return fail(SBC_ERR_INVALID_ARG, "rates is null");
     if (!workspace || workspace_bytes < sbc_linear_attention_workspace_size(n, H, a->dk, a->dv))
         return fail(SBC_ERR_WORKSPACE,
@@ -111,7 +110,7 @@ extern "C" sbc_status sbc_linear_attention_forward(const sbc_attention *a, const
     p.state_in = state_in;
     p.state_time = state_time;
     p.state_out = state_out;
-    p.time_out = a->t ? time_out : nullptr;
+    p.time_out = time_out;
     const bool whole = n > 0 && whole_rows(a, {q, k, v});
     return a->dtype == SBC_F32 ? forward<float>(p, whole, stream)
                                : forward<bf16_t>(p, whole, stream);

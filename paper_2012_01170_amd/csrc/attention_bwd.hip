@@ -251,16 +251,11 @@ extern "C" sbc_status sbc_linear_attention_backward(const sbc_attention *a, cons
     SBC_TRY(check_out_heads(dv, H, n, a->dv, a->dtype, "dv"));
     if (n == 0)
         return drates ? fill_i32(reinterpret_cast<int32_t *>(drates), 0, H, stream) : SBC_OK;
-    const sbc_heads *in[4] = {dO, q, k, v}, *out[3] = {dq, dk, dv};
-    const int32_t in_d[4] = {a->dv, a->dk, a->dk, a->dv}, out_d[3] = {a->dk, a->dk, a->dv};
-    for (int i = 0; i < 3; ++i) {
-        for (int j = 0; j < 4; ++j)
-            if (heads_overlap(*out[i], H, out_d[i], *in[j], H, in_d[j], n, a->dtype))
-                return fail(SBC_ERR_INVALID_ARG, "a gradient overlaps an input");
-        for (int j = 0; j < i; ++j)
-            if (heads_overlap(*out[i], H, out_d[i], *out[j], H, out_d[j], n, a->dtype))
-                return fail(SBC_ERR_INVALID_ARG, "two gradients overlap");
-    }
+    auto heads = [&](const sbc_heads *x, int32_t d) { return region_heads(x, H, n, d, a->dtype); };
+    SBC_TRY(check_apart({heads(dq, a->dk), heads(dk, a->dk), heads(dv, a->dv), region(drates, H, 4)},
+                        {heads(dO, a->dv), heads(q, a->dk), heads(k, a->dk), heads(v, a->dv),
+                         region(a->rates, H, 4), region(a->splits, (int64_t)a->n_batch + 1, 4),
+                         region(a->t, n, 4)}));
     if (!workspace ||
         workspace_bytes < sbc_linear_attention_backward_workspace_size(n, H, a->dk, a->dv))
         return fail(SBC_ERR_WORKSPACE,

@@ -92,16 +92,17 @@ extern "C" sbc_status sbc_linear_attention_step(const sbc_attention *a, const sb
     if (!state_in || !state_out) return fail(SBC_ERR_INVALID_ARG, "state_in or state_out is null");
     if (a->t && (!state_time || !time_out))
         return fail(SBC_ERR_INVALID_ARG, "with t, state_time and time_out are needed");
-    const size_t state_bytes = (size_t)n * H * a->dk * a->dv * 4;
-    if (state_in != state_out && overlap(state_in, state_bytes, state_out, state_bytes))
+    const Region tokens = region_heads(o, H, n, a->dv, a->dtype);
+    const Region state = region(state_out, (int64_t)n * H * a->dk * a->dv, 4);
+    const Region times = region(a->t ? time_out : nullptr, n, 4);
+    const Region before = region(state_in, (int64_t)n * H * a->dk * a->dv, 4);
+    if (state_in != state_out && meet(state, before))
         return fail(SBC_ERR_INVALID_ARG, "state_out overlaps state_in and is not state_in itself");
-    if (a->t && (overlap(state_time, (size_t)n * 4, time_out, (size_t)n * 4) ||
-                 overlap(a->t, (size_t)n * 4, time_out, (size_t)n * 4)))
-        return fail(SBC_ERR_INVALID_ARG, "time_out overlaps state_time or t");
-    if (heads_overlap(*o, H, a->dv, *q, H, a->dk, n, a->dtype) ||
-        heads_overlap(*o, H, a->dv, *k, H, a->dk, n, a->dtype) ||
-        heads_overlap(*o, H, a->dv, *v, H, a->dv, n, a->dtype))
-        return fail(SBC_ERR_INVALID_ARG, "o overlaps an input");
+    SBC_TRY(check_apart({tokens, state, times},
+                        {region_heads(q, H, n, a->dk, a->dtype), region_heads(k, H, n, a->dk, a->dtype),
+                         region_heads(v, H, n, a->dv, a->dtype), region(a->rates, H, 4),
+                         region(a->t, n, 4), region(a->t ? state_time : nullptr, n, 4)}));
+    SBC_TRY(check_apart({tokens, times}, {before}));
     StepArgs p{n, H, a->dk, a->dv, (a->dv + kCols - 1) / kCols, a->scale, a->rates, a->t,
                state_time, *q, *k, *v, *o, state_in, state_out, a->t ? time_out : nullptr};
     const int64_t blocks = (int64_t)n * H * p.tiles;

@@ -498,10 +498,6 @@ sbc_status backward(const void *dy, int64_t dys, const void *x, int64_t xs, cons
     return SBC_OK;
 }
 
-size_t rows_bytes(int32_t n, int32_t C, int64_t stride, sbc_dtype d) {
-    return n > 0 ? ((size_t)(n - 1) * (size_t)stride + (size_t)C) * dtype_bytes(d) : 0;
-}
-
 }  // namespace
 }  // namespace sbc
 
@@ -518,8 +514,9 @@ extern "C" sbc_status sbc_layer_norm_forward(const void *x, int64_t x_stride, co
         return fail(SBC_ERR_INVALID_ARG, "a row stride is smaller than C");
     if (n == 0) return SBC_OK;
     if (!x || !y) return fail(SBC_ERR_INVALID_ARG, "x or y is null");
-    if (overlap(x, rows_bytes(n, C, x_stride, dtype), y, rows_bytes(n, C, y_stride, dtype)))
-        return fail(SBC_ERR_INVALID_ARG, "y overlaps x");
+    SBC_TRY(check_apart({region_rows(y, n, C, y_stride, dtype), region(mean, n, 4), region(rstd, n, 4)},
+                        {region_rows(x, n, C, x_stride, dtype), region(weight, C, 4),
+                         region(bias, C, 4)}));
     trace_before("norm_fwd", stream);
     SBC_TRY(dtype == SBC_F32 ? forward<float>(x, x_stride, weight, bias, n, C, eps, y, y_stride,
                                               mean, rstd, stream)
@@ -554,10 +551,10 @@ extern "C" sbc_status sbc_layer_norm_backward(const void *dy, int64_t dy_stride,
     }
     if (!dy || !x || !mean || !rstd)
         return fail(SBC_ERR_INVALID_ARG, "dy, x, mean or rstd is null");
-    const size_t dx_bytes = dx ? rows_bytes(n, C, dx_stride, dtype) : 0;
-    if (overlap(dx, dx_bytes, x, rows_bytes(n, C, x_stride, dtype)) ||
-        overlap(dx, dx_bytes, dy, rows_bytes(n, C, dy_stride, dtype)))
-        return fail(SBC_ERR_INVALID_ARG, "dx overlaps x or dy");
+    SBC_TRY(check_apart({region_rows(dx, n, C, dx_stride, dtype), region(dweight, C, 4),
+                         region(dbias, C, 4)},
+                        {region_rows(dy, n, C, dy_stride, dtype), region_rows(x, n, C, x_stride, dtype),
+                         region(weight, C, 4), region(mean, n, 4), region(rstd, n, 4)}));
     if (sums && (!workspace || workspace_bytes < sbc_layer_norm_workspace_size(n, C)))
         return fail(SBC_ERR_WORKSPACE, "workspace smaller than sbc_layer_norm_workspace_size()");
     float *part = sums ? static_cast<float *>(workspace) : nullptr;

@@ -172,15 +172,18 @@ extern "C" sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q
             const bool same = w == u && in[u]->data == out[w]->data &&
                               in[u]->token_stride == out[w]->token_stride &&
                               in[u]->head_stride == out[w]->head_stride;
-            if (!same && heads_overlap(*out[w], heads[w], d, *in[u], heads[u], d, n, dtype))
+            if (!same && meet(region_heads(out[w], heads[w], n, d, dtype),
+                              region_heads(in[u], heads[u], n, d, dtype)))
                 return fail(SBC_ERR_INVALID_ARG, "an output overlaps an input that is not its own");
         }
         a.in[w] = *in[w];
         a.out[w] = *out[w];
         a.heads[w] = heads[w];
     }
-    if (heads_overlap(*out[0], heads[0], d, *out[1], heads[1], d, n, dtype))
-        return fail(SBC_ERR_INVALID_ARG, "q_out and k_out overlap");
+    SBC_TRY(check_apart({region_heads(out[0], heads[0], n, d, dtype),
+                         region_heads(out[1], heads[1], n, d, dtype)},
+                        {region_rows(plan->positions, n, plan->n_axes, plan->position_stride, SBC_F32),
+                         region(plan->freqs, pairs, 4)}));
     const int V = dtype == SBC_F32 ? 4 : 8;
     const int N = plan->interleaved ? V / 2 : V;  // (kPairs)
     a.n = n;

@@ -6,6 +6,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 
 #include "common.hpp"
 
@@ -95,23 +96,57 @@ template <int G> __device__ __forceinline__ float group_sum(float x) {
     return x;
 }
 
-// Whether [a, a + na) and [b, b + nb) bytes share any.
-inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && na && nb && x < y + nb && y < x + na;
-}
-
 inline bool known_dtype(sbc_dtype d) { return d == SBC_F32 || d == SBC_BF16; }
 inline size_t dtype_bytes(sbc_dtype d) { return d == SBC_F32 ? 4 : 2; }
 
-// ---------------------------------------------------------------- sbc_heads
-// Bytes from the first element of n tokens' heads to past their last one.
-inline size_t heads_bytes(const sbc_heads &x, int32_t heads, int32_t n, int32_t d, sbc_dtype dt) {
-    if (!x.data || heads <= 0 || n <= 0) return 0;
-    return ((size_t)(n - 1) * (size_t)x.token_stride + (size_t)(heads - 1) * (size_t)x.head_stride +
-            (size_t)d) * dtype_bytes(dt);
+// ---------------------------------------------------------------- overlaps
+// Where an argument lies: `blocks` blocks of `span` bytes, `stride` bytes apart.
+struct Region {
+    const void *data;
+    int64_t span, stride, blocks;
+    int64_t extent() const { return data && blocks > 0 ? stride * (blocks - 1) + span : 0; }
+};
+inline Region region(const void *data, int64_t count, int64_t element) {
+    return {data, count * element, 0, 1};
+}
+inline Region region_rows(const void *data, int64_t n, int64_t width, int64_t stride, sbc_dtype dt) {
+    const int64_t e = (int64_t)dtype_bytes(dt);
+    return {data, width * e, stride * e, n};
+}
+inline Region region_heads(const sbc_heads *x, int64_t heads, int64_t n, int64_t d, sbc_dtype dt) {
+    if (!x || heads <= 0 || n <= 0) return {nullptr, 0, 0, 0};
+    const int64_t e = (int64_t)dtype_bytes(dt), ts = x->token_stride * e, hs = x->head_stride * e;
+    if (heads == 1 || (n > 1 && ts >= hs))
+        return {x->data, (heads - 1) * hs + d * e, ts, ts == 0 ? 1 : n};
+    return {x->data, (n - 1) * ts + d * e, hs, heads};
 }
 
+// Whether two of them share memory.  Rows of the same stride may lie in each other's gaps
+// (parts of one projection), and so may a block in those of rows.
+inline bool meet(const Region &a, const Region &b) {
+    const int64_t na = a.extent(), nb = b.extent();
+    const int64_t off = (int64_t)((uintptr_t)b.data - (uintptr_t)a.data);
+    if (na <= 0 || nb <= 0 || off >= na || -off >= nb) return false;
+    if (a.blocks == 1 && b.blocks > 1) return meet(b, a);
+    if (a.blocks == 1 || a.stride < a.span) return true;
+    if (b.blocks > 1 ? a.stride != b.stride : off < 0) return true;
+    const int64_t at = ((off % a.stride) + a.stride) % a.stride;
+    return !(at >= a.span && at + b.span <= a.stride);
+}
+
+// Outputs share memory with no input and with no other output.
+inline sbc_status check_apart(std::initializer_list<Region> outputs,
+                              std::initializer_list<Region> inputs) {
+    for (const Region *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Region &i : inputs)
+            if (meet(*o, i)) return fail(SBC_ERR_INVALID_ARG, "an output overlaps an input");
+        for (const Region *p = outputs.begin(); p != o; ++p)
+            if (meet(*o, *p)) return fail(SBC_ERR_INVALID_ARG, "two outputs overlap");
+    }
+    return SBC_OK;
+}
+
+// ---------------------------------------------------------------- sbc_heads
 // An input: any strides that do not go backwards (0: the same for all).
 inline sbc_status check_heads(const sbc_heads *x, int32_t heads, int32_t n, int32_t d,
                               sbc_dtype dt, const char *name) {
@@ -135,24 +170,6 @@ inline sbc_status check_out_heads(const sbc_heads *x, int32_t heads, int32_t n, 
     if (!tokens_outside && !heads_outside)
         return fail(SBC_ERR_INVALID_ARG, std::string(name) + "'s elements overlap");
     return SBC_OK;
-}
-
-// Whether two such arrays may share elements.  Heads of different arrays in the
-// same rows (parts of one projection) do not, where the rows' strides are equal.
-inline bool heads_overlap(const sbc_heads &a, int32_t a_heads, int32_t a_d, const sbc_heads &b,
-                          int32_t b_heads, int32_t b_d, int32_t n, sbc_dtype dt) {
-    if (!overlap(a.data, heads_bytes(a, a_heads, n, a_d, dt), b.data,
-                 heads_bytes(b, b_heads, n, b_d, dt)))
-        return false;
-    const int64_t ts = a.token_stride;
-    if (ts != b.token_stride || ts <= 0) return true;
-    const int64_t e = (int64_t)dtype_bytes(dt);
-    const int64_t off = (int64_t)((uintptr_t)b.data - (uintptr_t)a.data);
-    const int64_t span_a = (a_heads - 1) * a.head_stride + a_d;
-    const int64_t span_b = (b_heads - 1) * b.head_stride + b_d;
-    int64_t m = off % (ts * e);
-    if (m < 0) m += ts * e;
-    return !(m >= span_a * e && m + span_b * e <= ts * e);
 }
 
 }  // namespace sbc

@@ -177,3 +177,26 @@ def test_norm_of_rows_far_from_zero(c, dtype):
     assert (np.abs(_np(rstd) - rr) <= 2.0 ** -18 * rr).all()
     tol = 2.0 ** -18 * (1 + np.abs(ry)) + (U * np.abs(ry) if dtype == BF16 else 0)
     assert (np.abs(_np(y) - ry) <= tol).all(), np.abs(_np(y) - ry).max()
+
+
+# ---------------------------------------------------------------- shared memory
+def test_arrays_in_the_same_rows():
+    """Queries, keys and positions that lie beside each other in rows are no overlap, and
+    neither is a state that is updated in place beside its token."""
+    n, h, d = 70, 2, 16
+    rows = torch.randn(n, 2 * h * d + 3, device=DEV)
+    q, k = (rows[:, i * h * d:(i + 1) * h * d].view(n, h, d) for i in (0, 1))
+    pos, freqs = rows[:, 2 * h * d:], torch.rand(6, device=DEV)
+    before = pos.clone()
+    want = sbc.rotary_forward(q.contiguous(), k.contiguous(), before, freqs, (2, 2, 2))
+    got = sbc.rotary_forward(q, k, pos, freqs, (2, 2, 2), inplace=True)
+    assert all(torch.equal(a, b) for a, b in zip((*got, pos), (*want, before)))
+    one = torch.randn(3 * h * d + h * d * d, device=DEV)
+    x = [one[i * h * d:(i + 1) * h * d].view(1, h, d) for i in range(3)]
+    state = one[3 * h * d:].view(1, h, d, d)
+    rates = torch.full((h,), 0.1, device=DEV)
+    want = sbc.linear_attention_step(*(y.clone() for y in x), rates, state.clone())
+    got = sbc.linear_attention_step(*x, rates, state, out_state=state)
+    assert torch.equal(got[0], want[0]) and torch.equal(state, want[1])
+    with pytest.raises(sbc.ops.L.SbcError, match="INVALID_ARG"):
+        sbc.rotary_forward(q, None, rows[:, h * d - 3:h * d], freqs, (2, 2, 2), inplace=True)
