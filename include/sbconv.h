@@ -585,7 +585,8 @@ typedef struct {
  * lose nothing.
  *   q, k     [n, q_heads, d] and [n, k_heads, d] (either may have 0 heads and be
  *            NULL), float32 or bf16; q_out and k_out alike: they may be q and k
- *            themselves, and overlap nothing else
+ *            themselves, and overlap nothing else.  n * (d + 8) <= 2^33 is
+ *            always taken, more only where the channels need fewer lanes
  * ------------------------------------------------------------------------ */
 #define SBC_MAX_AXES 8
 typedef struct {
@@ -672,7 +673,7 @@ sbc_status sbc_linear_attention_backward(const sbc_attention *a, const sbc_heads
  * stream i's next.  Arguments as above with state_in and state_out [n, heads, dk,
  * dv] given (and with t state_time and time_out); without t every step is one
  * position.  state_out may be state_in itself; time_out must not overlap
- * state_time or t.  No workspace. */
+ * state_time or t.  n * heads * ceil(dv / 64) < 2^24.  No workspace. */
 sbc_status sbc_linear_attention_step(const sbc_attention *a, const sbc_heads *q,
                                      const sbc_heads *k, const sbc_heads *v,
                                      const float *state_in, const int32_t *state_time,

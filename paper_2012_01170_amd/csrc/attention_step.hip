@@ -106,8 +106,8 @@ extern "C" sbc_status sbc_linear_attention_step(const sbc_attention *a, const sb
     StepArgs p{n, H, a->dk, a->dv, (a->dv + kCols - 1) / kCols, a->scale, a->rates, a->t,
                state_time, *q, *k, *v, *o, state_in, state_out, a->t ? time_out : nullptr};
     const int64_t blocks = (int64_t)n * H * p.tiles;
-    if (blocks >= (int64_t)1 << 24)
-        return fail(SBC_ERR_UNSUPPORTED, "n * heads must be below 2^23");
+    if (blocks >= (int64_t)1 << 24)  // (a launch holds fewer than 2^32 work-items)
+        return fail(SBC_ERR_UNSUPPORTED, "n * heads * ceil(dv / 64) must be below 2^24");
     trace_before("attn_step", stream);
     if (a->dtype == SBC_F32)
         hipLaunchKernelGGL(attn_step_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
