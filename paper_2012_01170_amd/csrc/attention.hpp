@@ -136,10 +136,11 @@ __device__ __forceinline__ void mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB]
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], acc, 0, 0, 0);
 }
 
-// 8 values -> N parts: their first 8, 16 or 24 bits
+// 8 values -> N parts: their first 16 or 24 bits
 template <int N>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[N]) {
 #pragma clang fp contract(off)
+    static_assert(N == 2 || N == 3, "parts");
     u32x4v h, m, l;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -152,13 +153,12 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[N]) {
             l[i] = w;
         } else {
             h[i] = pack_bf16(a, b);
-            if constexpr (N == 2)
-                m[i] = pack_bf16(a - __uint_as_float(h[i] << 16),
-                                 b - __uint_as_float(h[i] & 0xFFFF0000u));
+            m[i] = pack_bf16(a - __uint_as_float(h[i] << 16),
+                             b - __uint_as_float(h[i] & 0xFFFF0000u));
         }
     }
     out[0] = __builtin_bit_cast(bf16x8, h);
-    if constexpr (N > 1) out[1] = __builtin_bit_cast(bf16x8, m);
+    out[1] = __builtin_bit_cast(bf16x8, m);
     if constexpr (N > 2) out[2] = __builtin_bit_cast(bf16x8, l);
 }
 
