@@ -262,10 +262,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_grads_kernel(AttnPass dq, G
     else
         grad_body<T, D, D, true, kDots>(both, blockIdx.x - first, lds);
 }
-// (Two workgroups a CU where LDS holds them.)
 template <typename T, int D, bool kDots>
-__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 && D <= 96 ? 2 : 1) void
-attn_wide_grads_kernel(AttnPass dq, AttnPass dv, AttnPass dk) {
+__global__ __launch_bounds__(kAttnThreads) void attn_wide_grads_kernel(AttnPass dq, AttnPass dv,
+                                                                       AttnPass dk) {
     constexpr int NO = sizeof(T) == 4 ? 3 : 2;
     __shared__ PassShared<T, D, 64, 3> lds;
     const int first = dq.n_seg * dq.heads * dq.tiles, second = first + dv.n_seg * dv.heads * dv.tiles;
