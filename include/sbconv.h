@@ -627,11 +627,13 @@ sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q, int32_t q
  *   state_out  the same after each sequence's last token, or NULL; with t,
  *              time_out [n_batch] its time (both NULL or none; of an empty
  *              sequence those of state_in, zero without one)
- * Products are taken on the matrix cores with operands split into bf16 parts
- * (float32: three; of bf16 inputs only what is computed from them: two, and
- * three for the state) and summed in float32; o is rounded once.  A NaN or
- * infinity reaches no other sequence and no earlier token (of float32 inputs an
- * infinity may come out as NaN).
+ * Products are taken on the matrix cores with operands split into bf16 parts and
+ * summed in float32.  Float32 operands have three parts, whose smallest products
+ * (up to 2^-22 of the whole) are left out.  Of bf16 inputs the masked products and the
+ * state have two (2^-17) where they meet nothing but o, dk and dv, which are then
+ * rounded once to bf16 (2^-8), and three in dq, the states and the rates' gradient.
+ * A NaN or infinity reaches no other sequence and no earlier token; an infinity may
+ * come out as NaN.
  * No output may overlap an input.
  * ------------------------------------------------------------------------ */
 typedef struct {
@@ -655,7 +657,8 @@ sbc_status sbc_linear_attention_forward(const sbc_attention *a, const sbc_heads 
  *     dq_i = scale * sum over j <= i of D_ij (dO_i . v_j) k_j,
  *     dk_j = scale * sum over i >= j of D_ij (dO_i . v_j) q_i,
  *     dv_j = scale * sum over i >= j of D_ij (q_i . k_j) dO_i,
- *     drates[h] = -scale * sum of (t_i - t_j) D_ij (q_i . k_j) (dO_i . v_j).
+ *     drates[h] = -scale * sum of (t_i - t_j) D_ij (q_i . k_j) (dO_i . v_j),
+ * the last with every term weighed by its own gap, so that pauses cost no digits.
  * Sequences are taken in chunks of 64 tokens; a NaN or infinity in one spoils no
  * other sequence, but may spoil all of its own chunk.
  *   dO [n, heads, dv]; dq, dk [n, heads, dk], dv [n, heads, dv]: of dtype

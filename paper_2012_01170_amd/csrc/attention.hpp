@@ -124,7 +124,9 @@ __device__ __forceinline__ float join_factors(float f, float g) {
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
 
 // acc += a b, all products of parts that reach above the smallest part's own
-// rounding, smallest first
+// rounding, smallest first.  (Of three parts each, m l, l m and l l are left out, up to
+// 2^-22 of the product; the sum of all is one float32, where split.hpp's mma_split keeps the largest
+// apart, at twice the registers.)
 template <int NA, int NB>
 __device__ __forceinline__ void mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], floatx4 &acc) {
     constexpr int kMost = NA > NB ? NA : NB;

@@ -17,7 +17,7 @@
 // the state that comes in from behind; the next segment goes on with S alone, from the
 // time of this one's last token.  So every part of a gap is a factor of a term that its
 // own decay has weakened, and nothing is left to cancel: a pause, however long, adds
-// nothing to the error.  (300k tokens in bf16, 4 heads: 664 us for all gradients.  647 with
+// nothing to the error.  (300k tokens in bf16, 4 heads: 666 us for all gradients.  647 with
 // sums that cancel, of k . dk less q . dq times the time to the segment's end; but where 190
 // tokens with a rate of 0.05 hold pauses of 1.5e8, these are off by 4 to 11 %.)
 #include "attention_host.hpp"
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void attn_rates_kernel(const double *__restric
 }
 
 // Workgroups a CU: what its registers hold of the passes up to 64 channels in bf16 (300k
-// tokens, 4 heads: 645 us at 3, 655 at 2 with the registers for 2), else two.
+// tokens, 4 heads: 666 us at 3, 683 at 2 with the registers for 2), else two.
 void backward_segments(int32_t n, int32_t heads, int32_t dk, int32_t dv, sbc_dtype dtype,
                        int32_t *seg_len, int32_t *n_seg) {
     const bool three = dtype == SBC_BF16 && dk <= 64 && dv <= 64;
@@ -186,8 +186,8 @@ sbc_status backward(const sbc_attention *a, const sbc_heads &dO, const sbc_heads
     both.p.tiles = 1;
     both.p.slope = back;
     // Together in one launch where dq's workgroups are at most three for two CUs: of 258
-    // (11003 tokens, 3 heads) 59 us against 80 in bf16 and 148 against 154 at 40 and 72
-    // channels in float32; of 64 41 against 61; of 512 229 against 175 at 128 channels in
+    // (11003 tokens, 3 heads) 51 us against 77 in bf16 and 145 against 150 at 40 and 72
+    // channels in float32; of 64 31 against 47; of 512 150 against 133 at 128 channels in
     // bf16, where the joint kernel's registers leave fewer workgroups on a CU.
     const bool together = whole && 2 * (int64_t)parts * base.heads <= 3 * (int64_t)device_cus();
     auto run = [&](auto dots) {

@@ -432,16 +432,17 @@ template <int V, typename F> bool row_dispatch(int32_t C, F &&f) {
 
 // Workgroups of the forward pass (and of dx in wide rows), one for the rows that it
 // takes at once; rows past 2^22 workgroups' are taken in turn.  (A launch holds fewer
-// than 2^32 work-items.  1M rows of 64 bf16 take 66 us so, 70 in 8192 workgroups.)
+// than 2^32 work-items.  1M rows of 64 bf16 take 72.6 us so, 73.2 in 8192 workgroups.)
 constexpr int64_t kMostBlocks = 1 << 22;
 unsigned row_blocks(int64_t n, int rows) {
     const int64_t b = (n + rows - 1) / rows;
     return (unsigned)(b < kMostBlocks ? b : kMostBlocks);
 }
 
-// Workgroups of the backward pass: at most 2 a CU, and one for 16 rows, since each
-// leaves 2 C sums to be read again (12007 rows of 1001 bf16: 25.5 us so, 31 at one a
-// CU, 31 to 34 at 8 rows).
+// Workgroups of the backward pass: at most 2 a CU (12007 rows of 1001 bf16: 29 us, 39 at
+// one a CU), and one for 16 rows, since each leaves 2 C sums to be read again (4000 rows of
+// 4096 float32: 44 us, 47 at 8 rows, 58 at 32; 4000 of 1001 bf16: 18, 18, 23).  Few wide
+// rows would rather have more: 256 of 4096 take 30 us, 20 at 8 rows.
 int32_t bwd_blocks(int32_t n) {
     const int64_t most = 2 * (int64_t)device_cus();
     int64_t b = ((int64_t)n + 15) / 16;
