@@ -255,7 +255,8 @@ __device__ __forceinline__ void put_slope(const AttnPass &p, double slope, int t
 // masked products P go from one product's result to the next one's operand
 // without LDS), and its tiles of the state.  NS: parts that P and S are split
 // into, two where they only reach bf16 outputs (2^-17 of them, beside the
-// output's rounding of 2^-8).
+// output's rounding of 2^-8; with three the forward of 300k tokens, 4 heads takes 249 us
+// against 236, and is as far from float64).
 //
 // A product with a masked weight is 0 times c, and NaN where c is infinite or NaN.
 // kCareful, the forward pass: a chunk with such values in c is taken token by token, so
