@@ -684,6 +684,146 @@ sbc_status sbc_linear_attention_step(const sbc_attention *a, const sbc_heads *q,
                                      hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * 14. Norms of queries and keys for each head, with the rotation by their positions in the
+ * same pass.  Head h of token i (x, of d channels) becomes
+ *     y = R(positions[i]) (w * x / sqrt(mean(x^2) + eps)),
+ * the mean over the head's channels, w the weights of q or of k, the same for all heads,
+ * and R the rotation of section 12.
+ *   q, k     [n, q_heads, d] and [n, k_heads, d] (either may have 0 heads and be
+ *            NULL), float32 or bf16; q_out and k_out alike: they may be q and k
+ *            themselves, and overlap nothing else
+ *   q_weight, k_weight  [d] float32, or NULL: ones
+ *   d <= 256; past 240 only where the pairs and the channels past them fill 64 pieces of 16
+ *   bytes at most
+ * The backward pass: from dq and dk, the gradients of q_out and k_out, those of q and k
+ * (dq_out, dk_out, which overlap no input), and of the weights (float32 [d], summed over
+ * tokens and heads in an order that the sizes alone decide; NULL: not wanted).
+ * ------------------------------------------------------------------------ */
+sbc_status sbc_qk_norm_rotary_forward(const sbc_rotary_plan *plan, const sbc_heads *q,
+                                      int32_t q_heads, const sbc_heads *k, int32_t k_heads,
+                                      const float *q_weight, const float *k_weight,
+                                      sbc_dtype dtype, int32_t n, int32_t d, float eps,
+                                      const sbc_heads *q_out, const sbc_heads *k_out,
+                                      hipStream_t stream);
+size_t sbc_qk_norm_rotary_workspace_size(int32_t n, int32_t d);
+sbc_status sbc_qk_norm_rotary_backward(const sbc_rotary_plan *plan, const sbc_heads *dq,
+                                       const sbc_heads *dk, const sbc_heads *q, int32_t q_heads,
+                                       const sbc_heads *k, int32_t k_heads, const float *q_weight,
+                                       const float *k_weight, sbc_dtype dtype, int32_t n,
+                                       int32_t d, float eps, const sbc_heads *dq_out,
+                                       const sbc_heads *dk_out, float *dq_weight,
+                                       float *dk_weight, void *workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * 15. Softmax attention over packed sequences.  Head h of the queries reads head
+ * h / (heads / kv_heads) of the keys.  For token i of a sequence
+ *     s_ij = scale q_i . k_j,   lse_i = log sum over visible j of exp(s_ij),
+ *     o_i = sum over visible j of exp(s_ij - lse_i) v_j;
+ * where no key is visible, o is 0 and lse -infinity.  All keys of the sequence are visible,
+ * or with causal != 0 those up to the token, the last token seeing the last key (token i of
+ * lq sees keys j <= i + lk - lq).
+ *   splits     [n_batch + 1] int32, 0 .. n: sequence b owns the tokens
+ *              splits[b] .. splits[b+1]-1, perhaps none; NULL: one sequence
+ *   k_splits   the same for the m keys; NULL: those of splits (m = n), or one sequence
+ *              of all m keys where splits is NULL too.  Rows of outputs that lie in no
+ *              sequence are left as they were
+ *   q [n, heads, dk], k [m, kv_heads, dk], v [m, kv_heads, dv], o [n, heads, dv]:
+ *              float32 or bf16 (dtype), 1 <= dk, dv <= 128, heads <= 65535,
+ *              n heads and m kv_heads below 2^31
+ *   lse        [n, heads] float32, or NULL: not wanted
+ *   scale      > 0 and finite
+ * Scores, maxima and sums are float32.  Products are taken on the matrix cores, of float32
+ * inputs with operands split into three bf16 parts (products up to 2^-22 of the whole left
+ * out); of bf16 inputs, the weights are rounded to bf16 (2^-8 each) on their way to the
+ * product with v, as are the terms of the gradients' products.
+ * A NaN or infinity reaches no other sequence and no row that does not see it; an infinity
+ * may come out as NaN.  (The gradients: no other sequence; within one, rows and keys of the
+ * same 128 may share it.)
+ * No output may overlap an input.  Results do not depend on anything but the inputs.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    int32_t n, m, n_batch, heads, kv_heads, dk, dv;
+    sbc_dtype dtype;
+    float scale;
+    int32_t causal;
+    const int32_t *splits;
+    const int32_t *k_splits;
+} sbc_softmax_attention;
+size_t sbc_softmax_attention_workspace_size(const sbc_softmax_attention *a);
+sbc_status sbc_softmax_attention_forward(const sbc_softmax_attention *a, const sbc_heads *q,
+                                         const sbc_heads *k, const sbc_heads *v,
+                                         const sbc_heads *o, float *lse, void *workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
+/* The gradients of <o, dO>, from the forward pass' o and lse:
+ *     P_ij = exp(s_ij - lse_i),   dS_ij = P_ij (dO_i . v_j - dO_i . o_i),
+ *     dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij dO_i,
+ * the sums over i over all the heads that read a key's head as well.
+ *   dq like q, dk like k, dv like v, of dtype */
+size_t sbc_softmax_attention_backward_workspace_size(const sbc_softmax_attention *a);
+sbc_status sbc_softmax_attention_backward(const sbc_softmax_attention *a, const sbc_heads *dO,
+                                          const sbc_heads *q, const sbc_heads *k,
+                                          const sbc_heads *v, const sbc_heads *o,
+                                          const float *lse, const sbc_heads *dq,
+                                          const sbc_heads *dk, const sbc_heads *dv,
+                                          void *workspace, size_t workspace_bytes,
+                                          hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * 16. A cache of keys and values in pages, for sequences that grow.  A cache is
+ * [n_pages, page, kv_heads, d] with any strides of its first three axes; token j of stream b
+ * lies at place j % page of the page table[b, j / page].
+ *
+ * sbc_softmax_attention_paged: section 15's attention, causal, of n new tokens over the
+ * streams' kept tokens, the new ones among them (m, k_splits and causal are not read).
+ *   table      [n_batch, width] int32, lengths [n_batch] int32: tokens that a stream has,
+ *              with the new ones (taken as 0 .. width * page)
+ *   splits     of the new tokens; NULL: one for each stream (n = n_batch)
+ * Keys on a page outside 0 .. n_pages-1 are left out.
+ *
+ * sbc_cache_slots: pages and places for new tokens, before they are appended.  Stream b has
+ * lengths[b] tokens and gets splits[b+1] - splits[b] more (NULL: one), for which it needs
+ *     ceil(after / page) - ceil(before / page)
+ * pages more (no more than its row of the table has room for).  They are handed out from
+ * free [n_free] in the order of the streams.
+ *   table_out  [n_batch, width] the table with them, -1 where free had no more; it may be
+ *              table itself
+ *   slots      [n] int64: page * (the page's number) + place of each new token, -1 without
+ *              a page or in no stream
+ *   lengths_out [n_batch] the lengths with the new tokens, needed [1] the number of pages
+ *              that all streams need (more than n_free: some tokens have no place)
+ * n_batch * width below 2^31.
+ *
+ * sbc_cache_append: rows of k [n, kv_heads, dk] and v [n, kv_heads, dv] to their slots;
+ * slots outside 0 .. n_pages * page - 1 are left out, the others must be distinct.  Either
+ * of k and v may be NULL with its pages.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    void *data;
+    int64_t page_stride;   /* strides in elements, the channels dense */
+    int64_t token_stride;
+    int64_t head_stride;
+} sbc_pages;
+size_t sbc_softmax_attention_paged_workspace_size(const sbc_softmax_attention *a, int32_t page,
+                                                  int32_t width);
+sbc_status sbc_softmax_attention_paged(const sbc_softmax_attention *a, const sbc_heads *q,
+                                       const sbc_pages *k, const sbc_pages *v, int32_t n_pages,
+                                       int32_t page, const int32_t *table, int32_t width,
+                                       const int32_t *lengths, const sbc_heads *o, float *lse,
+                                       void *workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+size_t sbc_cache_slots_workspace_size(int32_t n_batch);
+sbc_status sbc_cache_slots(const int32_t *lengths, const int32_t *splits, int32_t n,
+                           int32_t n_batch, const int32_t *table, int32_t width, int32_t page,
+                           const int32_t *free_pages, int32_t n_free, int32_t *table_out,
+                           int64_t *slots, int32_t *lengths_out, int32_t *needed,
+                           void *workspace, size_t workspace_bytes, hipStream_t stream);
+sbc_status sbc_cache_append(const sbc_heads *k, const sbc_heads *v, int32_t n, int32_t kv_heads,
+                            int32_t dk, int32_t dv, sbc_dtype dtype, const int64_t *slots,
+                            const sbc_pages *k_pages, const sbc_pages *v_pages, int32_t n_pages,
+                            int32_t page, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Tracing, for measurement tools.  After sbc_trace_kernel(name, start, stop)
  * every launch of the kernel called `name` made by the calling thread records
  * `start` immediately before and `stop` immediately after itself on its

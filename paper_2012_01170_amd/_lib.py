@@ -39,7 +39,12 @@ EXPORTS = [
     "sbc_layer_norm_forward", "sbc_layer_norm_workspace_size", "sbc_layer_norm_backward",
     "sbc_rotary", "sbc_linear_attention_workspace_size", "sbc_linear_attention_forward",
     "sbc_linear_attention_backward_workspace_size", "sbc_linear_attention_backward",
-    "sbc_linear_attention_step",
+    "sbc_linear_attention_step", "sbc_qk_norm_rotary_forward",
+    "sbc_qk_norm_rotary_workspace_size", "sbc_qk_norm_rotary_backward",
+    "sbc_softmax_attention_workspace_size", "sbc_softmax_attention_forward",
+    "sbc_softmax_attention_backward_workspace_size", "sbc_softmax_attention_backward",
+    "sbc_softmax_attention_paged_workspace_size", "sbc_softmax_attention_paged",
+    "sbc_cache_slots_workspace_size", "sbc_cache_slots", "sbc_cache_append",
 ]
 
 
@@ -88,6 +93,19 @@ class SbcAttention(ctypes.Structure):
                 ("splits", ctypes.c_void_p), ("t", ctypes.c_void_p)]
 
 
+class SbcSoftmaxAttention(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("m", ctypes.c_int32), ("n_batch", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dk", ctypes.c_int32),
+                ("dv", ctypes.c_int32), ("dtype", ctypes.c_int), ("scale", ctypes.c_float),
+                ("causal", ctypes.c_int32), ("splits", ctypes.c_void_p),
+                ("k_splits", ctypes.c_void_p)]
+
+
+class SbcPages(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class SbcError(RuntimeError):
     def __init__(self, status: int, message: str):
         self.status = status
@@ -104,6 +122,8 @@ _geo_p = ctypes.POINTER(SbcGeometry)
 _i64_p = ctypes.POINTER(ctypes.c_int64)
 _heads_p = ctypes.POINTER(SbcHeads)
 _attn_p = ctypes.POINTER(SbcAttention)
+_soft_p = ctypes.POINTER(SbcSoftmaxAttention)
+_pages_p = ctypes.POINTER(SbcPages)
 
 _SIGS = {
     "sbc_last_error": (ctypes.c_char_p, []),
@@ -175,6 +195,29 @@ _SIGS = {
                                       [_vp, _vp, _sz, _vp]),
     "sbc_linear_attention_step": (ctypes.c_int, [_attn_p, _heads_p, _heads_p, _heads_p, _vp, _vp,
                                                  _heads_p, _vp, _vp, _vp]),
+    "sbc_qk_norm_rotary_forward": (ctypes.c_int, [ctypes.POINTER(SbcRotaryPlan), _heads_p, _i32,
+                                                  _heads_p, _i32, _vp, _vp, ctypes.c_int, _i32,
+                                                  _i32, _f32, _heads_p, _heads_p, _vp]),
+    "sbc_qk_norm_rotary_workspace_size": (_sz, [_i32, _i32]),
+    "sbc_qk_norm_rotary_backward": (ctypes.c_int, [ctypes.POINTER(SbcRotaryPlan), _heads_p,
+                                                   _heads_p, _heads_p, _i32, _heads_p, _i32, _vp,
+                                                   _vp, ctypes.c_int, _i32, _i32, _f32, _heads_p,
+                                                   _heads_p, _vp, _vp, _vp, _sz, _vp]),
+    "sbc_softmax_attention_workspace_size": (_sz, [_soft_p]),
+    "sbc_softmax_attention_forward": (ctypes.c_int, [_soft_p] + [_heads_p] * 4 +
+                                      [_vp, _vp, _sz, _vp]),
+    "sbc_softmax_attention_backward_workspace_size": (_sz, [_soft_p]),
+    "sbc_softmax_attention_backward": (ctypes.c_int, [_soft_p] + [_heads_p] * 5 + [_vp] +
+                                       [_heads_p] * 3 + [_vp, _sz, _vp]),
+    "sbc_softmax_attention_paged_workspace_size": (_sz, [_soft_p, _i32, _i32]),
+    "sbc_softmax_attention_paged": (ctypes.c_int, [_soft_p, _heads_p, _pages_p, _pages_p, _i32,
+                                                   _i32, _vp, _i32, _vp, _heads_p, _vp, _vp, _sz,
+                                                   _vp]),
+    "sbc_cache_slots_workspace_size": (_sz, [_i32]),
+    "sbc_cache_slots": (ctypes.c_int, [_vp, _vp, _i32, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _vp,
+                                       _vp, _vp, _vp, _sz, _vp]),
+    "sbc_cache_append": (ctypes.c_int, [_heads_p, _heads_p, _i32, _i32, _i32, _i32, ctypes.c_int,
+                                        _vp, _pages_p, _pages_p, _i32, _i32, _vp]),
 }
 
 

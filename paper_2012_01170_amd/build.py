@@ -30,7 +30,8 @@ COMMON_FLAGS = [
 # Flags of single sources.  The attention kernels keep their sums in the registers that
 # the vector ALU reads: as accumulation registers, each use of one was a move besides
 # (96 of some 900 vector instructions a chunk).
-FILE_FLAGS = {f"attention{s}.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"] for s in ("", "_bwd")}
+FILE_FLAGS = {f"{s}.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+              for s in ("attention", "attention_bwd", "softmax", "softmax_paged", "softmax_bwd")}
 
 
 def _sources():

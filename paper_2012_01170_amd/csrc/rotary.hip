@@ -8,12 +8,7 @@
 // not made for every head: a lane makes those of some pairs of a token once and
 // takes the token's heads, of both arrays, kBatch at a time, so that their loads are
 // in flight together (and the first ones while it makes them).
-//
-// The angle is taken in revolutions in float64, where the product of two float32
-// is exact and 1 / 2 pi costs 2^-53 of it, and reduced before sine and cosine in
-// float32: angles of 1e6 (timestamps) are as good as small ones.
-#include "common.hpp"
-#include "seq.hpp"
+#include "rotary.hpp"
 
 namespace sbc {
 namespace {
@@ -31,9 +26,6 @@ struct RotaryArgs {
     int32_t upto[SBC_MAX_AXES];  // pairs of the axes so far
     float sign;
 };
-
-// Pairs of a lane: one vector of them, or of each of their halves
-template <typename T, bool kInterleaved> constexpr int kPairs = kInterleaved ? kVec<T> / 2 : kVec<T>;
 
 // kTail: there are channels past the last pair (300k events: 112 us without such lanes'
 // conditions, 139 with them)
@@ -86,11 +78,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
             int axis = 0;
             for (int y = 0; y + 1 < a.n_axes; ++y) axis += p0 + k >= a.upto[y];
             const double pos = (double)static_cast<const P *>(a.positions)[i * a.pos_stride + axis];
-            double rev = pos * (double)a.freqs[p0 + k] * 0.15915494309189533577;
-            rev -= rint(rev);
-            float s, co;
-            sincospif((float)(2.0 * rev), &s, &co);
-            cs[k] = co;
+            float s;
+            turn_of(pos, a.freqs[p0 + k], cs[k], s);
             sn[k] = a.sign * s;
         }
     }
@@ -142,19 +131,9 @@ extern "C" sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q
     if (!plan) return fail(SBC_ERR_INVALID_ARG, "plan is null");
     if (n < 0 || d <= 0) return fail(SBC_ERR_INVALID_ARG, "n must be >= 0 and d > 0");
     if (!known_dtype(dtype)) return fail(SBC_ERR_INVALID_ARG, "unknown dtype");
-    if (plan->n_axes < 1 || plan->n_axes > SBC_MAX_AXES)
-        return fail(SBC_ERR_INVALID_ARG, "n_axes must be 1 .. SBC_MAX_AXES");
     RotaryArgs a{};
     int64_t pairs = 0;
-    for (int x = 0; x < plan->n_axes; ++x) {
-        if (plan->sections[x] < 0) return fail(SBC_ERR_INVALID_ARG, "a section is negative");
-        pairs += plan->sections[x];
-        a.upto[x] = (int32_t)(pairs <= d ? pairs : d);
-    }
-    if (pairs < 1 || 2 * pairs > d)
-        return fail(SBC_ERR_INVALID_ARG, "the sections must sum to 1 .. d / 2 pairs");
-    if (plan->position_stride < plan->n_axes)
-        return fail(SBC_ERR_INVALID_ARG, "position_stride is smaller than n_axes");
+    SBC_TRY(check_rotary(plan, d, &pairs, a.upto));
     if (q_heads < 0 || k_heads < 0) return fail(SBC_ERR_INVALID_ARG, "negative number of heads");
     if (n == 0 || (q_heads == 0 && k_heads == 0)) return SBC_OK;
     if (!plan->positions || !plan->freqs)
@@ -184,12 +163,10 @@ extern "C" sbc_status sbc_rotary(const sbc_rotary_plan *plan, const sbc_heads *q
                          region_heads(out[1], heads[1], n, d, dtype)},
                         {region_rows(plan->positions, n, plan->n_axes, plan->position_stride, SBC_F32),
                          region(plan->freqs, pairs, 4)}));
-    const int V = dtype == SBC_F32 ? 4 : 8;
-    const int N = plan->interleaved ? V / 2 : V;  // (kPairs)
     a.n = n;
     a.d = d;
     a.pairs = (int32_t)pairs;
-    a.units = (int32_t)((pairs + N - 1) / N + (d - 2 * pairs + V - 1) / V);
+    a.units = (int32_t)rotary_units(dtype, plan->interleaved, pairs, d);
     a.positions = plan->positions;
     a.pos_stride = plan->position_stride;
     a.freqs = plan->freqs;

@@ -7,6 +7,7 @@
 #include <cstdint>
 #include <cstring>
 #include <initializer_list>
+#include <utility>
 
 #include "common.hpp"
 
@@ -170,6 +171,43 @@ inline sbc_status check_out_heads(const sbc_heads *x, int32_t heads, int32_t n, 
     if (!tokens_outside && !heads_outside)
         return fail(SBC_ERR_INVALID_ARG, std::string(name) + "'s elements overlap");
     return SBC_OK;
+}
+
+// ---------------------------------------------------------------- sbc_pages
+inline sbc_status check_pages(const sbc_pages *x, int32_t n_pages, int32_t page, int32_t heads,
+                              int32_t d, sbc_dtype dt, const char *name) {
+    if (n_pages == 0) return SBC_OK;
+    if (!x || !x->data) return fail(SBC_ERR_INVALID_ARG, std::string(name) + " is null");
+    if (x->page_stride < 0 || x->token_stride < 0 || x->head_stride < 0)
+        return fail(SBC_ERR_INVALID_ARG, std::string(name) + " has a negative stride");
+    if (((uintptr_t)x->data) % dtype_bytes(dt))
+        return fail(SBC_ERR_INVALID_ARG, std::string(name) + " is not aligned to its elements");
+    return SBC_OK;
+}
+inline sbc_status check_out_pages(const sbc_pages *x, int32_t n_pages, int32_t page, int32_t heads,
+                                  int32_t d, sbc_dtype dt, const char *name) {
+    SBC_TRY(check_pages(x, n_pages, page, heads, d, dt, name));
+    if (n_pages == 0) return SBC_OK;
+    int64_t dims[3][2] = {{n_pages, x->page_stride}, {page, x->token_stride}, {heads, x->head_stride}};
+    int64_t extent = d;
+    for (int i = 0; i < 3; ++i) {  // from the smallest stride out
+        for (int j = i + 1; j < 3; ++j)
+            if (dims[j][0] > 1 && (dims[i][0] <= 1 || dims[j][1] < dims[i][1])) std::swap(dims[i], dims[j]);
+        if (dims[i][0] <= 1) break;
+        if (dims[i][1] < extent)
+            return fail(SBC_ERR_INVALID_ARG, std::string(name) + "'s elements overlap");
+        extent += dims[i][1] * (dims[i][0] - 1);
+    }
+    return SBC_OK;
+}
+inline Region region_pages(const sbc_pages *x, int32_t n_pages, int32_t page, int32_t heads,
+                           int32_t d, sbc_dtype dt) {
+    if (!x || n_pages <= 0) return {nullptr, 0, 0, 0};
+    const int64_t e = (int64_t)dtype_bytes(dt);
+    const int64_t span = (x->token_stride * (page - 1) + x->head_stride * (heads - 1) + d) * e;
+    const int64_t stride = x->page_stride * e;
+    if (n_pages > 1 && stride < span) return {x->data, stride * (n_pages - 1) + span, 0, 1};
+    return {x->data, span, stride, n_pages};
 }
 
 }  // namespace sbc

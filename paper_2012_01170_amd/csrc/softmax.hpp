@@ -1,0 +1,500 @@
+// Softmax attention: what the forward pass, its form over a paged cache and the
+// gradients share.
+//
+// Head h of the queries reads head h / group of the keys (group = heads / kv_heads).
+// The rows of one sequence and key head are its tokens' queries of the whole group,
+// row r = token r / group, head r % group of the group: keys are read once for all of
+// them, a single token still fills `group` rows, and the gradients of a shared head are
+// sums along the rows.
+//
+// Products are v_mfma_f32_32x32x16_bf16 on operands split into parts (split.hpp, one part
+// of a bf16 input, three of a float32 one).  They are taken so that a lane holds one row's
+// scores: S^T = K Q^T has row l = lane & 31 in the lanes l and l + 32, and of its 32 keys
+// those of 8 (r / 4) + 4 (lane >> 5) + r % 4 in register r.  Maximum and sum are then along
+// a lane's registers (one exchange between the halves for the maximum), and the registers are
+// the next product's operand as they are, O^T = V^T P^T, if V's rows come in the same
+// order, as the transposing reads of LDS give them.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "attention.hpp"
+#include "common.hpp"
+#include "seq.hpp"
+#include "split.hpp"
+
+namespace sbc {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// ---------------------------------------------------------------- division
+// n / d for n < 2^31 by a multiplication (round-up method): q = (hi(m n) + n) >> s
+struct Divisor {
+    uint32_t m, d;
+    int32_t s;
+};
+inline Divisor divisor(int32_t d) {
+    int32_t s = 0;
+    while (((int64_t)1 << s) < d) ++s;
+    const uint64_t m = ((((uint64_t)1 << s) - (uint64_t)d) << 32) / (uint64_t)d + 1;
+    return {(uint32_t)m, (uint32_t)d, s};
+}
+__device__ __forceinline__ int32_t divide(int32_t n, const Divisor &by) {
+    return (int32_t)((__umulhi((uint32_t)n, by.m) + (uint32_t)n) >> by.s);
+}
+
+// ---------------------------------------------------------------- arguments
+struct SoftmaxPages {  // a paged cache, in place of k, v and k_splits
+    sbc_pages k, v;
+    int32_t n_pages, width;
+    Divisor page;
+    const int32_t *table, *lengths;
+};
+struct SoftmaxArgs {
+    int32_t n, m, n_batch, heads, kv_heads, dk, dv;
+    int32_t causal;
+    Divisor group;
+    float scale, scale2;  // scale2 = scale log2 e
+    const int32_t *splits, *k_splits;
+    sbc_heads q, k, v, o;
+    float *lse;
+    int32_t slots;  // places of tiles (tile_place)
+    SoftmaxPages pages;
+    // keys of a sequence in parts (softmax_rows_kernel): what each part gives, float32
+    int32_t parts;
+    float *part_o, *part_lse;
+    // gradients
+    sbc_heads d_o, dq, dk_out, dv_out;
+    const float *lse_in;
+    float *delta;
+    float *part_dk, *part_dv;
+};
+
+__device__ __forceinline__ int32_t clamp_i(int32_t x, int32_t lo, int32_t hi) {
+    return x < lo ? lo : x > hi ? hi : x;
+}
+// (whatever the splits hold, rows are read and written inside the arrays)
+__device__ __forceinline__ int32_t q_split(const SoftmaxArgs &p, int32_t b) {
+    return p.splits ? clamp_i(p.splits[b], 0, p.n) : p.pages.table ? b : b == 0 ? 0 : p.n;
+}
+__device__ __forceinline__ int32_t k_split(const SoftmaxArgs &p, int32_t b) {
+    return p.k_splits ? clamp_i(p.k_splits[b], 0, p.m) : b == 0 ? 0 : p.m;
+}
+
+// Tiles of kRows rows are laid out by places: those of sequence b begin at place
+// (rows before it) / kRows + b, which leaves room for its last, partly filled one, so that
+// no sum over the sequences' tiles is needed to launch or to find them.  The last b in
+// [0, n_batch) whose places begin at or before x, -1 if none; 64 lanes look at 64 places
+// of the range at once.
+template <typename F>
+__device__ __forceinline__ int32_t sequence_of(int32_t n_batch, int32_t x, F begin) {
+    int32_t lo = 0, hi = n_batch;
+    while (lo < hi) {
+        const int32_t step = (hi - lo + 63) / 64;
+        const int64_t b = lo + (int64_t)(threadIdx.x & 63) * step;
+        const bool before = b < hi && begin((int32_t)b) <= x;
+        const int32_t c = __popcll(__ballot(before));
+        if (c == 0) break;
+        const int64_t up = lo + (int64_t)c * step;
+        lo += (c - 1) * step + 1;
+        hi = up < hi ? (int32_t)up : hi;
+    }
+    return lo - 1;
+}
+
+// One sequence's tokens and keys
+struct Sequence {
+    int32_t b, q0, lq, k0, lk;
+    // keys that the token sees: causal, the last token sees the last key
+    __device__ __forceinline__ int32_t limit(int32_t token, int32_t causal) const {
+        return causal ? clamp_i(token + lk - lq + 1, 0, lk) : lk;
+    }
+};
+template <bool kPaged>
+__device__ __forceinline__ Sequence sequence_at(const SoftmaxArgs &p, int32_t b) {
+    Sequence s;
+    s.b = b;
+    s.q0 = q_split(p, b);
+    s.lq = q_split(p, b + 1) - s.q0;
+    if (s.lq < 0) s.lq = 0;
+    if constexpr (kPaged) {
+        const int64_t room = (int64_t)p.pages.width * p.pages.page.d;
+        s.k0 = 0;
+        s.lk = clamp_i(p.pages.lengths[b], 0, room > INT32_MAX ? INT32_MAX : (int32_t)room);
+    } else {
+        s.k0 = k_split(p, b);
+        s.lk = k_split(p, b + 1) - s.k0;
+        if (s.lk < 0) s.lk = 0;
+    }
+    return s;
+}
+
+// ---------------------------------------------------------------- fragments
+template <int NA, int NB>
+__device__ __forceinline__ void mma32(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB],
+                                      floatx16 &acc) {
+    constexpr int kMost = NA > NB ? NA : NB;
+#pragma unroll
+    for (int s = kMost - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB)
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[s - i], acc, 0, 0, 0);
+}
+template <int N> __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[i][r] = 0.f;
+}
+
+// A lane's places in a tile of D columns (tile_at) for 32 x 32 products
+template <int D> struct LaneAt32 {
+    static constexpr int kMask = ((D / 8) & -(D / 8)) - 1;  // (tile_at)
+    int row0, col0, col8;
+    __device__ __forceinline__ LaneAt32() {
+        const int lane = threadIdx.x & 63, quarter = lane >> 4, i = lane & 15;
+        const int r = 4 * (quarter >> 1) + (i >> 2), c = 16 * (quarter & 1) + 4 * (i & 3);
+        row0 = in_loop(tile_at<D>(lane & 31, 8 * (lane >> 5)));
+        col0 = in_loop(tile_at<D>(r, c));
+        col8 = in_loop(tile_at<D>(r + 8, c));
+    }
+    __device__ __forceinline__ static int along(int at, int pieces) {
+        return (at ^ ((pieces & kMask) << 3)) + ((pieces & ~kMask) << 3);
+    }
+};
+// Row 32 u + l, columns 16 k + 8 g .. + 7 (g = lane >> 5)
+template <int D, int N>
+__device__ __forceinline__ void frag_row32(const bf16_t *tile, int plane, int u, int k,
+                                           const LaneAt32<D> &at, bf16x8 (&out)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        out[i] = *reinterpret_cast<const bf16x8 *>(tile + (i * plane + 32 * u * D) +
+                                                   LaneAt32<D>::along(at.row0, 2 * k));
+}
+// Rows 16 s + 4 g .. + 3 and 16 s + 8 + 4 g .. + 3 of column 32 t + l
+template <int D, int N>
+__device__ __forceinline__ void frag_col32(const bf16_t *tile, int plane, int s, int t,
+                                           const LaneAt32<D> &at, bf16x8 (&out)[N]) {
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef short s8 __attribute__((ext_vector_type(8)));
+    typedef __attribute__((address_space(3))) s4 *lds_s4;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        bf16_t *base = const_cast<bf16_t *>(tile) + (i * plane + 16 * s * D);
+        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s4)(base + LaneAt32<D>::along(at.col0, 4 * t)));
+        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s4)(base + LaneAt32<D>::along(at.col8, 4 * t)));
+        out[i] = __builtin_bit_cast(bf16x8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
+}
+// Registers 8 h .. + 7 of a product as an operand of the next: keys 16 h + 4 g .. + 3 and
+// 16 h + 8 + 4 g .. + 3 of its 32.  A bf16 call's weights are rounded to bf16 here (2^-8 of
+// each, independent ones, beside the output's own 2^-8).
+template <typename T>
+__device__ __forceinline__ void frag_regs(const floatx16 &x, int h, bf16x8 (&out)[kParts<T>]) {
+    if constexpr (sizeof(T) == 2) {
+        u32x4v w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
+        out[0] = __builtin_bit_cast(bf16x8, w);
+    } else {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[8 * h + i];
+        split8<3>(y, out);
+    }
+}
+
+// A lane's row of an input as an operand of D columns, 16 k + 8 g .. + 7 of k-step k; `row` may
+// be read also without `there`.
+template <typename T, int D, bool kWhole>
+__device__ __forceinline__ void load_row(const T *row, bool there, int width,
+                                         u32x4v (&raw)[D / 16][8 / kVec<T>]) {
+    const int c0 = 8 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 8 / kVec<T>; ++i) {
+            const int c = 16 * k + c0 + i * kVec<T>;
+            if constexpr (kWhole)
+                __builtin_memcpy(&raw[k][i], row + (c < width ? c : 0), 16);
+            else
+                raw[k][i] = load_elements<T>(row, c, width, there);
+        }
+}
+// What load_row read past the columns, and all of a row that is not there, to zero
+template <typename T, int D, bool kWhole>
+__device__ __forceinline__ void settle_row(bool there, int width,
+                                           u32x4v (&raw)[D / 16][8 / kVec<T>]) {
+    if (!kWhole || (width == D && __all(there))) return;
+    const int c0 = in_loop(8 * ((threadIdx.x & 63) >> 5));
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 8 / kVec<T>; ++i) {
+            const bool ok = there && 16 * k + c0 + i * kVec<T> < width;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) raw[k][i][e] = ok ? raw[k][i][e] : 0u;
+        }
+}
+template <typename T>
+__device__ __forceinline__ void raw_parts(const u32x4v (&raw)[8 / kVec<T>],
+                                          bf16x8 (&out)[kParts<T>]) {
+    if constexpr (sizeof(T) == 2) {
+        out[0] = __builtin_bit_cast(bf16x8, raw[0]);
+    } else {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw[i / 4][i % 4]);
+        split8<3>(x, out);
+    }
+}
+template <typename T, int D, bool kWhole>
+__device__ __forceinline__ void row_operand(const T *row, bool there, int width,
+                                            bf16x8 (&out)[D / 16][kParts<T>]) {
+    u32x4v raw[D / 16][8 / kVec<T>];
+    load_row<T, D, kWhole>(row, there, width, raw);
+    settle_row<T, D, kWhole>(there, width, raw);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) raw_parts<T>(raw[k], out[k]);
+}
+
+__device__ __forceinline__ bool finite_bits(uint32_t w, bool pair) {
+    return (w & 0x7F800000u) != 0x7F800000u && !(pair && (w & 0x7F80u) == 0x7F80u);
+}
+
+// kRows x D values on their way to LDS by kThreads threads, kSteps 16-byte pieces each
+template <typename T, int D, int kRows, int kThreads, bool kWhole> struct TileLoad {
+    static constexpr int kPerRow = D / kVec<T>;
+    static constexpr int kSteps = kRows * kPerRow / kThreads;
+    static_assert(kRows * kPerRow % kThreads == 0, "pieces");
+    u32x4v raw[kSteps];
+    uint32_t there;  // a bit for each piece that exists (the others are zeroed in settle())
+    __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
+    __device__ __forceinline__ static int row_of(int s) { return (s * kThreads + tid()) / kPerRow; }
+    __device__ __forceinline__ static int col_of(int s) {
+        return (s * kThreads + tid()) % kPerRow * kVec<T>;
+    }
+    // row_at(row): where the tile's row begins, nullptr if it does not exist; `any` is an address
+    // that may be read
+    template <typename F>
+    __device__ __forceinline__ void load(F row_at, const T *any, int width) {
+        there = 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const T *row = row_at(row_of(s));
+            const int c = col_of(s);
+            if constexpr (kWhole) {
+                const bool ok = row != nullptr && c < width;
+                __builtin_memcpy(&raw[s], ok ? row + c : any, 16);
+                there |= (uint32_t)ok << s;
+            } else {
+                raw[s] = load_elements<T>(row ? row : any, c, width, row != nullptr);
+            }
+        }
+    }
+    // after the loads' wait, before store()
+    __device__ __forceinline__ void settle() {
+        if (!kWhole || there == (1u << kSteps) - 1u) return;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[s][i] = there >> s & 1u ? raw[s][i] : 0u;
+    }
+    __device__ __forceinline__ bool not_finite() const {
+        bool found = false;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) found |= !finite_bits(raw[s][i], sizeof(T) == 2);
+        return found;
+    }
+    __device__ __forceinline__ void store(bf16_t *tile) const {
+        constexpr int kPlane = kRows * D;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int at = tile_at<D>(row_of(s), col_of(s));
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<u32x4v *>(tile + at) = raw[s];
+            } else {
+                uint32_t h[2], m[2], lo[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    split2(__uint_as_float(raw[s][2 * i]), __uint_as_float(raw[s][2 * i + 1]),
+                           h[i], m[i], lo[i]);
+                *reinterpret_cast<uint2 *>(tile + at) = uint2{h[0], h[1]};
+                *reinterpret_cast<uint2 *>(tile + kPlane + at) = uint2{m[0], m[1]};
+                *reinterpret_cast<uint2 *>(tile + 2 * kPlane + at) = uint2{lo[0], lo[1]};
+            }
+        }
+    }
+};
+
+// The other half's value of the same row
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Where the keys of a tile lie: lane j looks up key first + j (j below kKeys).
+struct KeyPlaces {
+    int32_t page, at;  // -1: no such key
+    uint64_t there;    // a bit for each key of the tile
+    template <int kKeys>
+    __device__ __forceinline__ void find(const SoftmaxArgs &p, const Sequence &s, int32_t first,
+                                         int32_t end) {
+        const int32_t j = threadIdx.x & (kKeys - 1), key = first + j;
+        page = -1;
+        at = 0;
+        if (key < end) {
+            const int32_t i = divide(key, p.pages.page);
+            at = key - i * (int32_t)p.pages.page.d;
+            page = p.pages.table[(int64_t)s.b * p.pages.width + i];
+            if (page < 0 || page >= p.pages.n_pages) page = -1;
+        }
+        there = __ballot(page >= 0);
+        if constexpr (kKeys == 32) there &= 0xFFFFFFFFull;
+    }
+    template <typename T>
+    __device__ __forceinline__ const T *row(const sbc_pages &x, int32_t head, int32_t j) const {
+        const int32_t g = __shfl(page, j), a = __shfl(at, j);
+        return g < 0 ? nullptr
+                     : static_cast<const T *>(x.data) + g * x.page_stride + a * x.token_stride +
+                           head * x.head_stride;
+    }
+};
+
+// ---------------------------------------------------------------- softmax
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// Rows' running softmax: a lane's row has its maximum m (in units of log 2, scaled), its
+// own keys' part of the sum l, and its channels 32 t + 8 (r / 4) + 4 g + r % 4 of the sum of
+// products.
+template <int D> struct RowSums {
+    floatx16 o[D / 32];
+    float m, l;
+    __device__ __forceinline__ RowSums() : m(-INFINITY), l(0.f) { clear(o); }
+};
+
+// The keys that a lane's row sees of 32 (bit 8 (r / 4) + r % 4 of the result is register r)
+__device__ __forceinline__ uint32_t seen_bits(uint64_t there, int u, int32_t visible) {
+    const int32_t n = clamp_i(visible - 32 * u, 0, 32);
+    const uint32_t low = n == 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
+    return ((uint32_t)(there >> (32 * u)) & low) >> (4 * ((threadIdx.x & 63) >> 5));
+}
+
+// Scores x of kSub x 32 keys -> their weights, in place; the sums follow the maximum.  The
+// maximum that weights refer to moves only where a score lies 2^8 above it (a weight then is
+// at most 2^8, and rounded as a smaller one is), so that most tiles leave the sums alone.
+template <int D, int kSub>
+__device__ __forceinline__ void softmax_weights(floatx16 (&x)[kSub], float scale2, RowSums<D> &s) {
+    float top = x[0][0];
+#pragma unroll
+    for (int u = 0; u < kSub; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, x[u][r]);
+    top = fmaxf(top, other_half(top)) * scale2;
+    if (__any(top > s.m + 8.f)) {
+        const float m = fmaxf(s.m, top);
+        const float f = m == s.m ? 1.f : __builtin_amdgcn_exp2f(s.m - m);
+        s.m = m;
+        s.l *= f;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s.o[t][r] *= f;
+    }
+    const float m = s.m == -INFINITY ? 0.f : s.m;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < kSub; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            x[u][r] = __builtin_amdgcn_exp2f(fmaf(x[u][r], scale2, -m));
+            sum[r % 4] += x[u][r];
+        }
+    s.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// o += weights x values of the tile vt
+template <typename T, int D, int kSub>
+__device__ __forceinline__ void add_values(const floatx16 (&x)[kSub], const bf16_t *vt,
+                                           const LaneAt32<D> &at, RowSums<D> &s) {
+#pragma clang fp contract(off)
+    constexpr int NP = kParts<T>;
+#pragma unroll
+    for (int h = 0; h < 2 * kSub; ++h) {
+        bf16x8 w[NP];
+        frag_regs<T>(x[h / 2], h % 2, w);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+            bf16x8 v[NP];
+            frag_col32<D, NP>(vt, 32 * kSub * D, h, t, at, v);
+            mma32<NP, NP>(v, w, s.o[t]);
+        }
+    }
+}
+// The same key by key: values that are infinite or NaN meet only the rows that see them
+// (a product with the weight 0 of a hidden one would be NaN).
+template <typename T, int D, int kSub>
+__device__ __forceinline__ void add_values_singly(const floatx16 (&x)[kSub], const uint32_t (&seen)[kSub],
+                                               const bf16_t *vt, RowSums<D> &s) {
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+    for (int j = 0; j < 32 * kSub; ++j) {
+        const int reg = 4 * (j % 32 / 8) + j % 4, owner = (j / 4) % 2;
+        float mine = 0.f;
+        uint32_t sees = 0;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (u == j / 32 && r == reg) {
+                    mine = x[u][r];
+                    sees = seen[u] >> (8 * (r / 4) + r % 4) & 1u;
+                }
+        const float w = __shfl(mine, (lane & 31) + 32 * owner);
+        const bool ok = __shfl((int)sees, (lane & 31) + 32 * owner) != 0;
+        if (ok) {
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int at = tile_at<D>(j, 32 * t + 8 * (r / 4) + 4 * g + r % 4);
+                    float v = 0.f;
+#pragma unroll
+                    for (int i = kParts<T> - 1; i >= 0; --i) v += to_f32(vt[i * 32 * kSub * D + at]);
+                    s.o[t][r] = fmaf(w, v, s.o[t][r]);
+                }
+        }
+    }
+}
+
+// Four channels of an output's row: columns c .. + 3 of `width`
+template <typename T, bool kWhole>
+__device__ __forceinline__ void put4(T *row, int c, int width, const float (&x)[4]) {
+    T raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = from_f32<T>(x[i]);
+    if constexpr (kWhole) {
+        if (c < width) __builtin_memcpy(row + c, raw, sizeof(raw));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < width) row[c + i] = raw[i];
+    }
+}
+
+// f(D) with D the channels' tile as a constant
+template <typename F> void softmax_dispatch(int32_t d, F f) {
+    if (d <= 32)
+        f(std::integral_constant<int, 32>{});
+    else if (d <= 64)
+        f(std::integral_constant<int, 64>{});
+    else if (d <= 96)
+        f(std::integral_constant<int, 96>{});
+    else
+        f(std::integral_constant<int, 128>{});
+}
+
+}  // namespace sbc

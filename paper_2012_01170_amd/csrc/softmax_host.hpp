@@ -1,0 +1,103 @@
+// Host side of softmax attention's entry points: checks, and how rows and keys are divided.
+#pragma once
+
+#include <cmath>
+
+#include "softmax.hpp"
+
+namespace sbc {
+
+inline sbc_status check_softmax(const sbc_softmax_attention *a) {
+    if (!a) return fail(SBC_ERR_INVALID_ARG, "attention is null");
+    if (a->n < 0 || a->m < 0 || a->n_batch < 0)
+        return fail(SBC_ERR_INVALID_ARG, "n, m and n_batch must be >= 0");
+    if (a->heads <= 0 || a->kv_heads <= 0 || a->dk <= 0 || a->dv <= 0)
+        return fail(SBC_ERR_INVALID_ARG, "heads, kv_heads, dk and dv must be > 0");
+    if (a->heads % a->kv_heads)
+        return fail(SBC_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
+    if (!known_dtype(a->dtype)) return fail(SBC_ERR_INVALID_ARG, "unknown dtype");
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale))
+        return fail(SBC_ERR_INVALID_ARG, "scale must be > 0 and finite");
+    if (a->dk > 128 || a->dv > 128)
+        return fail(SBC_ERR_UNSUPPORTED, "dk and dv must be <= 128");
+    if (a->heads > 65535) return fail(SBC_ERR_UNSUPPORTED, "heads must be <= 65535");
+    if ((int64_t)a->n * a->heads >= (int64_t)1 << 31 ||
+        (int64_t)a->m * a->kv_heads >= (int64_t)1 << 31)
+        return fail(SBC_ERR_UNSUPPORTED, "n * heads and m * kv_heads must be below 2^31");
+    return SBC_OK;
+}
+// Sequences of keys that lie in one array
+inline sbc_status check_softmax_sequences(const sbc_softmax_attention *a) {
+    SBC_TRY(check_softmax(a));
+    if (!a->splits && a->n_batch != 1)
+        return fail(SBC_ERR_INVALID_ARG, "without splits there is one sequence (n_batch 1)");
+    if (a->n > 0 && a->n_batch == 0)
+        return fail(SBC_ERR_INVALID_ARG, "tokens without a sequence (n_batch 0)");
+    if (!a->k_splits && a->splits && a->m != a->n)
+        return fail(SBC_ERR_INVALID_ARG, "without k_splits there are as many keys as queries");
+    return SBC_OK;
+}
+
+inline int64_t softmax_places(const sbc_softmax_attention *a, int32_t rows) {
+    return (int64_t)a->n * (a->heads / a->kv_heads) / rows + a->n_batch;
+}
+
+// Whole 16-byte pieces of rows
+inline bool softmax_whole(const sbc_softmax_attention *a) {
+    const int v = a->dtype == SBC_F32 ? 4 : 8;
+    return a->dk % v == 0 && a->dv % v == 0;
+}
+
+// The kernels' arguments that every call has
+inline SoftmaxArgs softmax_args(const sbc_softmax_attention *a) {
+    SoftmaxArgs p{};
+    p.n = a->n;
+    p.m = a->m;
+    p.n_batch = a->n_batch;
+    p.heads = a->heads;
+    p.kv_heads = a->kv_heads;
+    p.dk = a->dk;
+    p.dv = a->dv;
+    p.causal = a->causal != 0;
+    p.group = divisor(a->heads / a->kv_heads);
+    p.scale = a->scale;
+    p.scale2 = (float)((double)a->scale * 1.4426950408889634);
+    p.splits = a->splits;
+    p.k_splits = a->k_splits ? a->k_splits : a->splits;
+    p.parts = 1;
+    return p;
+}
+
+// The forward pass takes few rows (32 to a workgroup, keys in parts) where many, 128 to a
+// workgroup, would leave CUs without work or most of their rows empty.
+struct SoftmaxPlan {
+    bool few;
+    int32_t parts;
+    int64_t blocks;
+};
+// most_keys: of one sequence
+inline SoftmaxPlan softmax_plan(const sbc_softmax_attention *a, int64_t most_keys) {
+    SoftmaxPlan s{false, 1, softmax_places(a, 128) * a->kv_heads};
+    const int64_t rows = (int64_t)a->n * (a->heads / a->kv_heads);
+    const int cus = device_cus();
+    s.few = rows <= (int64_t)64 * a->n_batch || s.blocks < cus / 2;
+    if (!s.few) return s;
+    const int64_t tiles = softmax_places(a, 32) * a->kv_heads;
+    int64_t parts = ((int64_t)8 * cus + tiles - 1) / tiles;
+    const int64_t most = (most_keys + 127) / 128;  // a round of keys for each
+    if (parts > most) parts = most;
+    if (parts > 64) parts = 64;
+    if (parts < 1) parts = 1;
+    s.parts = (int32_t)parts;
+    s.blocks = tiles * parts;
+    return s;
+}
+inline size_t softmax_workspace(const sbc_softmax_attention *a, const SoftmaxPlan &s) {
+    if (s.parts <= 1) return 256;
+    Carver c(nullptr);
+    c.take<float>((size_t)s.parts * a->n * a->heads * a->dv);
+    c.take<float>((size_t)s.parts * a->n * a->heads);
+    return c.used;
+}
+
+}  // namespace sbc

@@ -1,0 +1,370 @@
+// The kernels of softmax attention's forward pass (softmax.hpp), over packed sequences or a
+// paged cache.
+#pragma once
+
+#include "softmax.hpp"
+
+namespace sbc {
+
+constexpr int kSoftmaxThreads = 256;
+
+// The keys of a tile in LDS: 64, or 32 of wide float32 heads, whose three parts
+// would fill more than the 64 KB that let two workgroups share a CU's LDS.
+template <typename T, int D> constexpr int kTileKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
+
+constexpr int kTileRows = 128;  // of softmax_tile_kernel: 32 a wave
+constexpr int kFewRows = 32;    // of softmax_rows_kernel
+
+// A sequence's keys in p.parts parts for softmax_rows_kernel: as even ones as multiples of 128
+// keys (a round of a workgroup's four waves) allow
+__device__ __forceinline__ int32_t part_keys(int32_t lk, int32_t parts) {
+    return (int32_t)(((int64_t)lk + parts - 1) / parts + 127) / 128 * 128;
+}
+
+// ---------------------------------------------------------------- many rows
+// A workgroup has 128 rows, 32 a wave, and goes through the keys that they see in tiles,
+// which its waves share in LDS; the next tile is on its way into registers meanwhile.
+template <typename T, int D, bool kWhole, bool kPaged>
+__global__ __launch_bounds__(kSoftmaxThreads, 2) void softmax_tile_kernel(SoftmaxArgs p) {
+    constexpr int NP = kParts<T>, KB = kTileKeys<T, D>, kSub = KB / 32, kPlane = KB * D;
+    __shared__ __attribute__((aligned(16))) bf16_t kt[NP * kPlane], vt[NP * kPlane];
+    __shared__ int32_t bad[2];
+    const int32_t head_k = blockIdx.x % p.kv_heads;
+    // (from the back: a causal sequence's last tiles are its longest)
+    const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads;
+    const int32_t group = p.group.d;
+    auto begin = [&](int32_t b) {
+        return (int32_t)((int64_t)q_split(p, b) * group / kTileRows) + b;
+    };
+    const int32_t b = sequence_of(p.n_batch, x, begin);
+    if (b < 0) return;
+    const Sequence s = sequence_at<kPaged>(p, b);
+    const int32_t r0 = (x - begin(b)) * kTileRows, rows = s.lq * group;
+    if (r0 >= rows) return;
+    const int wave = wave_of_block(), lane = threadIdx.x & 63;
+    // this lane's row (the last one in place of those that do not exist)
+    const int32_t wave_row = r0 + 32 * wave, row = wave_row + (lane & 31);
+    const bool there = row < rows;
+    const int32_t token = divide(there ? row : rows - 1, p.group);
+    const int32_t head = head_k * group + (there ? row - token * group : 0);
+    const int32_t limit = s.limit(token, p.causal);
+    auto limit_of = [&](int32_t r) {
+        return s.limit(divide(r < rows ? r : rows - 1, p.group), p.causal);
+    };
+    const int32_t least = __builtin_amdgcn_readfirstlane(limit_of(r0));
+    const int32_t most = __builtin_amdgcn_readfirstlane(limit_of(r0 + kTileRows - 1));
+    const int32_t wave_least = __builtin_amdgcn_readfirstlane(limit_of(wave_row));
+    const int32_t wave_most =
+        wave_row < rows ? __builtin_amdgcn_readfirstlane(limit_of(wave_row + 31)) : 0;
+
+    bf16x8 q[D / 16][NP];
+    {
+        const T *at = static_cast<const T *>(p.q.data) + (int64_t)(s.q0 + token) * p.q.token_stride +
+                      (int64_t)head * p.q.head_stride;
+        row_operand<T, D, kWhole>(at, there, p.dk, q);
+    }
+    const T *kbase, *vbase;
+    if constexpr (kPaged) {
+        kbase = static_cast<const T *>(p.pages.k.data);
+        vbase = static_cast<const T *>(p.pages.v.data);
+    } else {
+        kbase = static_cast<const T *>(p.k.data) + s.k0 * p.k.token_stride + head_k * p.k.head_stride;
+        vbase = static_cast<const T *>(p.v.data) + s.k0 * p.v.token_stride + head_k * p.v.head_stride;
+    }
+    TileLoad<T, D, KB, kSoftmaxThreads, kWhole> sk, sv;
+    KeyPlaces places, next_places;
+    auto fetch = [&](int32_t k0) {
+        if constexpr (kPaged) {
+            sk.load([&](int r) { return next_places.row<T>(p.pages.k, head_k, r); }, kbase, p.dk);
+            sv.load([&](int r) { return next_places.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
+        } else {
+            sk.load([&](int r) { return k0 + r < s.lk ? kbase + (k0 + r) * p.k.token_stride : nullptr; },
+                    kbase, p.dk);
+            sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
+                    vbase, p.dv);
+        }
+    };
+    const LaneAt32<D> at;
+    RowSums<D> sums;
+    if (threadIdx.x < 2) bad[threadIdx.x] = 0;
+    int turn = 0;
+    constexpr uint64_t kAll = KB == 64 ? ~0ull : 0xFFFFFFFFull;
+    if (most > 0) {
+        if constexpr (kPaged) next_places.template find<KB>(p, s, 0, s.lk);
+        fetch(0);
+    }
+    for (int32_t k0 = 0; k0 < most; k0 += KB, turn ^= 1) {
+        __syncthreads();  // the last tile has been read
+        sk.settle();
+        sv.settle();
+        sk.store(kt);
+        sv.store(vt);
+        if (k0 + KB > least && sv.not_finite()) bad[turn] = 1;
+        if (threadIdx.x == 0) bad[turn ^ 1] = 0;
+        if constexpr (kPaged) places = next_places;
+        __syncthreads();
+        if (k0 + KB < most) {
+            if constexpr (kPaged) next_places.template find<KB>(p, s, k0 + KB, s.lk);
+            fetch(k0 + KB);
+        }
+        if (k0 >= wave_most) continue;
+        floatx16 x[kSub];
+        clear(x);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) {
+                bf16x8 f[NP];
+                frag_row32<D, NP>(kt, kPlane, u, k, at, f);
+                mma32<NP, NP>(f, q[k], x[u]);
+            }
+        const uint64_t known = kPaged ? places.there : kAll;
+        if (k0 + KB > wave_least || known != kAll) {
+            uint32_t seen[kSub];
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) {
+                seen[u] = seen_bits(known, u, limit - k0);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    x[u][r] = seen[u] >> (8 * (r / 4) + r % 4) & 1u ? x[u][r] : -INFINITY;
+            }
+            softmax_weights<D, kSub>(x, p.scale2, sums);
+            if (bad[turn])
+                add_values_singly<T, D, kSub>(x, seen, vt, sums);
+            else
+                add_values<T, D, kSub>(x, vt, at, sums);
+        } else {
+            softmax_weights<D, kSub>(x, p.scale2, sums);
+            add_values<T, D, kSub>(x, vt, at, sums);
+        }
+    }
+    if (!there) return;
+    const float l = sums.l + other_half(sums.l);
+    const int64_t place = s.q0 + token;
+    if (p.lse && lane < 32)
+        p.lse[place * p.heads + head] = l == 0.f ? -INFINITY : (sums.m + log2f(l)) * kLn2;
+    T *out = static_cast<T *>(p.o.data) + place * p.o.token_stride + (int64_t)head * p.o.head_stride;
+    const float part = 1.f / l;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = l == 0.f ? 0.f : sums.o[t][4 * j + i] * part;
+            put4<T, kWhole>(out, 32 * t + 8 * j + 4 * (lane >> 5), p.dv, y);
+        }
+}
+
+// ---------------------------------------------------------------- few rows
+// A workgroup has 32 rows and one part of the keys; each wave takes every fourth 32 of
+// these keys by itself (keys from memory to registers, values through LDS of its own),
+// and the waves' sums are joined at the end.  Memory bounds it where a row or few meet a long cache:
+// the next 32 keys and values are always on their way.
+template <typename T, int D, bool kWhole, bool kPaged>
+__global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxArgs p) {
+    constexpr int NP = kParts<T>, kPlane = 32 * D;
+    constexpr int kJoin = 4 * 32 * 36 * 2;  // (bf16 elements of [4][32][36] float32)
+    constexpr int kTiles = 4 * NP * kPlane;
+    __shared__ __attribute__((aligned(16))) bf16_t lds[kTiles > kJoin ? kTiles : kJoin];
+    __shared__ float wave_m[4][32], wave_l[4][32];
+    const int32_t head_k = blockIdx.x % p.kv_heads;
+    const int32_t part = blockIdx.x / p.kv_heads % p.parts;
+    const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads / p.parts;
+    const int32_t group = p.group.d;
+    auto begin = [&](int32_t b) {
+        return (int32_t)((int64_t)q_split(p, b) * group / kFewRows) + b;
+    };
+    const int32_t b = sequence_of(p.n_batch, x, begin);
+    if (b < 0) return;
+    const Sequence s = sequence_at<kPaged>(p, b);
+    const int32_t r0 = (x - begin(b)) * kFewRows, rows = s.lq * group;
+    if (r0 >= rows) return;
+    const int wave = wave_of_block(), lane = threadIdx.x & 63;
+    const int32_t row = r0 + (lane & 31);
+    const bool there = row < rows;
+    const int32_t token = divide(there ? row : rows - 1, p.group);
+    const int32_t head = head_k * group + (there ? row - token * group : 0);
+    const int32_t limit = s.limit(token, p.causal);
+    auto limit_of = [&](int32_t r) {
+        return s.limit(divide(r < rows ? r : rows - 1, p.group), p.causal);
+    };
+    const int32_t least = __builtin_amdgcn_readfirstlane(limit_of(r0));
+    const int32_t most = __builtin_amdgcn_readfirstlane(limit_of(r0 + kFewRows - 1));
+    const int32_t size = p.parts > 1 ? part_keys(s.lk, p.parts) : s.lk;
+    const int32_t first = part * size;
+    const int32_t end = p.parts > 1 && most > first + size ? first + size : most;
+    if (part > 0 && first >= most) return;  // (softmax_join_kernel knows)
+
+    bf16x8 q[D / 16][NP];
+    {
+        const T *at = static_cast<const T *>(p.q.data) + (int64_t)(s.q0 + token) * p.q.token_stride +
+                      (int64_t)head * p.q.head_stride;
+        row_operand<T, D, kWhole>(at, there, p.dk, q);
+    }
+    const T *kbase, *vbase;
+    if constexpr (kPaged) {
+        kbase = static_cast<const T *>(p.pages.k.data);
+        vbase = static_cast<const T *>(p.pages.v.data);
+    } else {
+        kbase = static_cast<const T *>(p.k.data) + s.k0 * p.k.token_stride + head_k * p.k.head_stride;
+        vbase = static_cast<const T *>(p.v.data) + s.k0 * p.v.token_stride + head_k * p.v.head_stride;
+    }
+    u32x4v kraw[D / 16][8 / kVec<T>];
+    TileLoad<T, D, 32, 64, kWhole> sv;
+    KeyPlaces places, next_places;
+    auto fetch = [&](int32_t k0) {
+        if constexpr (kPaged) {
+            const T *at = next_places.row<T>(p.pages.k, head_k, lane & 31);
+            load_row<T, D, kWhole>(at ? at : kbase, at != nullptr, p.dk, kraw);
+            sv.load([&](int r) { return next_places.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
+        } else {
+            const int32_t key = k0 + (lane & 31);
+            const bool ok = key < s.lk;
+            load_row<T, D, kWhole>(kbase + (ok ? key : 0) * p.k.token_stride, ok, p.dk, kraw);
+            sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
+                    vbase, p.dv);
+        }
+    };
+    const LaneAt32<D> at;
+    RowSums<D> sums;
+    bf16_t *const vt = lds + wave * NP * kPlane;
+    int32_t k0 = first + 32 * wave;
+    if (k0 < end) {
+        if constexpr (kPaged) next_places.template find<32>(p, s, k0, s.lk);
+        fetch(k0);
+    }
+    for (; k0 < end; k0 += 128) {
+        bf16x8 kf[D / 16][NP];
+        settle_row<T, D, kWhole>(true, p.dk, kraw);  // (scores of keys that are not there are hidden)
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) raw_parts<T>(kraw[k], kf[k]);
+        sv.settle();
+        sv.store(vt);
+        const bool bad = k0 + 32 > least && __any(sv.not_finite());
+        if constexpr (kPaged) places = next_places;
+        if (k0 + 128 < end) {
+            if constexpr (kPaged) next_places.template find<32>(p, s, k0 + 128, s.lk);
+            fetch(k0 + 128);
+        }
+        floatx16 w[1];
+        clear(w);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) mma32<NP, NP>(kf[k], q[k], w[0]);
+        const uint64_t known = kPaged ? places.there : 0xFFFFFFFFull;
+        const int32_t visible = limit < end ? limit : end;
+        const uint32_t seen[1] = {seen_bits(known, 0, visible - k0)};
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            w[0][r] = seen[0] >> (8 * (r / 4) + r % 4) & 1u ? w[0][r] : -INFINITY;
+        softmax_weights<D, 1>(w, p.scale2, sums);
+        // (the wave's own LDS, which it reads in the order of its writes)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (bad)
+            add_values_singly<T, D, 1>(w, seen, vt, sums);
+        else
+            add_values<T, D, 1>(w, vt, at, sums);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    // joined: the waves' sums as weights of the largest maximum
+    const float l = sums.l + other_half(sums.l);
+    if (lane < 32) {
+        wave_m[wave][lane] = sums.m;
+        wave_l[wave][lane] = l;
+    }
+    __syncthreads();  // (all tiles have been read besides)
+    const int r = lane & 31;
+    const float top = fmaxf(fmaxf(wave_m[0][r], wave_m[1][r]), fmaxf(wave_m[2][r], wave_m[3][r]));
+    // (without a maximum the sums are zero, or NaN of scores that are NaN)
+    auto weight = [](float m, float top) {
+        return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    };
+    const float f = weight(sums.m, top);
+    float *const join = reinterpret_cast<float *>(lds);
+    // this thread's part of the sums: a row and four channels of each tile
+    const int32_t jr = threadIdx.x / 8, jc = threadIdx.x % 8 * 4;
+    const int32_t out_row = r0 + jr;
+    const int32_t out_token = divide(out_row < rows ? out_row : rows - 1, p.group);
+    const int64_t place = s.q0 + out_token;
+    const int32_t out_head = head_k * group + (out_row < rows ? out_row - out_token * group : 0);
+    const float out_top = fmaxf(fmaxf(wave_m[0][jr], wave_m[1][jr]), fmaxf(wave_m[2][jr], wave_m[3][jr]));
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        total += wave_l[i][jr] * weight(wave_m[i][jr], out_top);
+    const float inverse = 1.f / total;
+    const int64_t flat = place * p.heads + out_head;
+    if (out_row < rows && jc == 0) {
+        const float lse2 = total == 0.f ? -INFINITY : out_top + log2f(total);
+        if (p.parts > 1)
+            p.part_lse[(int64_t)part * p.n * p.heads + flat] = lse2;
+        else if (p.lse)
+            p.lse[flat] = lse2 * kLn2;
+    }
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+        if (t > 0) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            floatx4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = sums.o[t][4 * j + i] * f;
+            *reinterpret_cast<floatx4 *>(join + (wave * 32 + r) * 36 + 8 * j + 4 * (lane >> 5)) = y;
+        }
+        __syncthreads();
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const floatx4 z = *reinterpret_cast<const floatx4 *>(join + (w * 32 + jr) * 36 + jc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += z[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * inverse;
+        if (out_row < rows) {
+            if (p.parts > 1)
+                put4<float, false>(p.part_o + ((int64_t)part * p.n * p.heads + flat) * p.dv, 32 * t + jc,
+                                   p.dv, y);
+            else
+                put4<T, kWhole>(static_cast<T *>(p.o.data) + place * p.o.token_stride +
+                                    (int64_t)out_head * p.o.head_stride,
+                                32 * t + jc, p.dv, y);
+        }
+    }
+}
+
+// The parts' sums joined, a wave a token and head: each part's own softmax weighs by its sum.
+// Only parts that begin before the row's limit have been written.
+template <typename T, bool kPaged>
+__global__ __launch_bounds__(256) void softmax_join_kernel(SoftmaxArgs p) {
+    const int64_t flat = (int64_t)blockIdx.x * 4 + wave_of_block();
+    if (flat >= (int64_t)p.n * p.heads) return;
+    const int32_t token = (int32_t)(flat / p.heads), head = (int32_t)(flat - (int64_t)token * p.heads);
+    const int lane = threadIdx.x & 63;
+    const int32_t b = sequence_of(p.n_batch, token, [&](int32_t i) { return q_split(p, i); });
+    if (b < 0) return;
+    const Sequence s = sequence_at<kPaged>(p, b);
+    if (token - s.q0 >= s.lq) return;  // behind the last sequence
+    const int32_t limit = s.limit(token - s.q0, p.causal), size = part_keys(s.lk, p.parts);
+    const int64_t stride = (int64_t)p.n * p.heads;
+    const bool there = lane < p.parts && (int64_t)lane * size < limit;  // (parts <= 64)
+    const float lse2 = there ? p.part_lse[lane * stride + flat] : -INFINITY;
+    float top = lse2;
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    const float w = lse2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lse2 - top);
+    const float total = group_sum<64>(w);
+    const int32_t parts = size > 0 ? (limit + size - 1) / size : 0;
+    T *out = static_cast<T *>(p.o.data) + token * p.o.token_stride + (int64_t)head * p.o.head_stride;
+    for (int c0 = 0; c0 < p.dv; c0 += 64) {
+        const int c = c0 + lane < p.dv ? c0 + lane : p.dv - 1;
+        float y = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < parts; ++i)
+            y = fmaf(__shfl(w, i), p.part_o[(i * stride + flat) * p.dv + c], y);
+        if (c0 + lane < p.dv) out[c] = from_f32<T>(total == 0.f ? 0.f : y / total);
+    }
+    if (p.lse && lane == 0) p.lse[flat] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+}
+
+}  // namespace sbc

@@ -1,5 +1,6 @@
 """Binding of the sequence operators: layer norm, rotary positions with several
-axes, linear attention with a decay for each head.
+axes, linear attention with a decay for each head, norms of queries and keys with
+their rotation, softmax attention, and a cache in pages.
 
 As in ops.py, argument marshalling only.  Token arrays [n, heads, d] may be
 views with any strides, as long as their last axis is dense (parts of one
@@ -125,12 +126,13 @@ def layer_norm_backward(dy, x, weight, mean, rstd, need_dx: bool = True,
 
 
 # ---------------------------------------------------------------- rotary positions
-def _rotary(q, k, positions, freqs, sections, interleaved, backward, inplace):
+def _rotary_plan(q, k, positions, freqs, sections, interleaved):
+    """The checked q and k, one of them, and their plan."""
     one = q if q is not None else k
     if one is None:
         raise ValueError("q or k is needed")
     _first(one, "q" if q is not None else "k", 3)
-    index, dev, (n, _, d) = one.get_device(), one.device, one.shape
+    index, (n, _, d) = one.get_device(), one.shape
     for name, x in (("q", q), ("k", k)):
         if x is not None:
             _view(x, name, one.dtype, 3, index)
@@ -151,6 +153,12 @@ def _rotary(q, k, positions, freqs, sections, interleaved, backward, inplace):
     plan = L.SbcRotaryPlan(positions.data_ptr(), _row_stride(positions),
                            int(is_float), freqs.data_ptr(), len(sections),
                            (ctypes.c_int32 * L.SBC_MAX_AXES)(*sections), int(interleaved))
+    return one, index, plan
+
+
+def _rotary(q, k, positions, freqs, sections, interleaved, backward, inplace):
+    one, index, plan = _rotary_plan(q, k, positions, freqs, sections, interleaved)
+    dev, (n, _, d) = one.device, one.shape
     out = [None if x is None else (x if inplace else torch.empty(x.shape, dtype=x.dtype, device=dev))
            for x in (q, k)]
     L.check(L.lib().sbc_rotary(ctypes.byref(plan), _heads(q), 0 if q is None else q.shape[1],
@@ -299,3 +307,266 @@ def linear_attention_step(q, k, v, rates, state, t: Optional[torch.Tensor] = Non
         ctypes.byref(a), _heads(q), _heads(k), _heads(v), state.data_ptr(), _ptr(state_time),
         _heads(o), out_state.data_ptr(), _ptr(out_time), _stream(index)))
     return o, out_state, out_time
+
+
+# ---------------------------------------------------------------- norms and rotation
+def _head_weight(w, name, d, index):
+    if w is not None:
+        _dense(w, name, torch.float32, 1, index)
+        if w.numel() != d:
+            raise ValueError(f"{name} must be [{d}], got {tuple(w.shape)}")
+
+
+def qk_norm_rotary_forward(q, k, q_weight, k_weight, positions, freqs, sections: Sequence[int],
+                           interleaved: bool = False, eps: float = 1e-5, inplace: bool = False):
+    """q [n, heads, d] and k [n, k_heads, d] (either may be None), each head
+    divided by its root mean square, times its weights ([d] float32, or None), and
+    turned by the tokens' positions as rotary_forward does
+    (sbc_qk_norm_rotary_forward); returns both."""
+    one, index, plan = _rotary_plan(q, k, positions, freqs, sections, interleaved)
+    dev, (n, _, d) = one.device, one.shape
+    _head_weight(q_weight, "q_weight", d, index)
+    _head_weight(k_weight, "k_weight", d, index)
+    out = [None if x is None else (x if inplace else torch.empty(x.shape, dtype=x.dtype, device=dev))
+           for x in (q, k)]
+    L.check(L.lib().sbc_qk_norm_rotary_forward(
+        ctypes.byref(plan), _heads(q), 0 if q is None else q.shape[1], _heads(k),
+        0 if k is None else k.shape[1], _ptr(q_weight), _ptr(k_weight), _dtype_code(one), n, d,
+        float(eps), _heads(out[0]), _heads(out[1]), _stream(index)))
+    return tuple(out)
+
+
+def qk_norm_rotary_backward(dq, dk, q, k, q_weight, k_weight, positions, freqs,
+                            sections: Sequence[int], interleaved: bool = False, eps: float = 1e-5,
+                            need_weights: bool = True):
+    """(dq, dk, dq_weight, dk_weight): the gradients of qk_norm_rotary_forward's q
+    and k from those of its outputs, and of the weights ([d] float32; None for an
+    absent q or k, and where not wanted) (sbc_qk_norm_rotary_backward)."""
+    one, index, plan = _rotary_plan(q, k, positions, freqs, sections, interleaved)
+    dev, (n, _, d) = one.device, one.shape
+    _head_weight(q_weight, "q_weight", d, index)
+    _head_weight(k_weight, "k_weight", d, index)
+    for name, g, x in (("dq", dq, q), ("dk", dk, k)):
+        if (g is None) != (x is None):
+            raise ValueError(f"{name} and its input go together")
+        if x is not None:
+            _view(g, name, x.dtype, 3, index)
+            if g.shape != x.shape:
+                raise ValueError(f"{name} must be {tuple(x.shape)}, got {tuple(g.shape)}")
+    out = [None if x is None else torch.empty(x.shape, dtype=x.dtype, device=dev) for x in (q, k)]
+    dw = [torch.empty(d, dtype=torch.float32, device=dev) if need_weights and x is not None
+          else None for x in (q, k)]
+    lib = L.lib()
+    ws = _Workspace(lib.sbc_qk_norm_rotary_workspace_size(n, d) if need_weights else 0, dev)
+    L.check(lib.sbc_qk_norm_rotary_backward(
+        ctypes.byref(plan), _heads(dq), _heads(dk), _heads(q), 0 if q is None else q.shape[1],
+        _heads(k), 0 if k is None else k.shape[1], _ptr(q_weight), _ptr(k_weight),
+        _dtype_code(one), n, d, float(eps), _heads(out[0]), _heads(out[1]), _ptr(dw[0]),
+        _ptr(dw[1]), ws.ptr, ws.nbytes, _stream(index)))
+    return out[0], out[1], dw[0], dw[1]
+
+
+# ---------------------------------------------------------------- softmax attention
+def _softmax(q, k, v, splits, k_splits, scale, causal):
+    _first(q, "q", 3)
+    index, (n, H, dk) = q.get_device(), q.shape
+    _view(k, "k", q.dtype, 3, index)
+    _view(v, "v", q.dtype, 3, index)
+    m, G = k.shape[:2]
+    if k.shape[2] != dk:
+        raise ValueError(f"k must be [m, kv_heads, {dk}], got {tuple(k.shape)}")
+    if v.shape[:2] != k.shape[:2]:
+        raise ValueError(f"v must be [{m}, {G}, dv], got {tuple(v.shape)}")
+    n_batch = 1
+    if splits is not None:
+        _dense(splits, "splits", torch.int32, 1, index)
+        if splits.numel() < 1:
+            raise ValueError("splits must be [n_batch + 1]")
+        n_batch = splits.numel() - 1
+    if k_splits is not None:
+        _dense(k_splits, "k_splits", torch.int32, 1, index)
+        if splits is None:
+            raise ValueError("k_splits needs splits")
+        if k_splits.numel() != n_batch + 1:
+            raise ValueError(f"k_splits must be [{n_batch + 1}], got {tuple(k_splits.shape)}")
+    scale = dk ** -0.5 if scale is None else float(scale)
+    return index, q.device, L.SbcSoftmaxAttention(n, m, n_batch, H, G, dk, v.shape[2],
+                                                  _dtype_code(q), scale, int(causal),
+                                                  _ptr(splits), _ptr(k_splits))
+
+
+def softmax_attention_forward(q, k, v, splits: Optional[torch.Tensor] = None,
+                              k_splits: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, causal: bool = False):
+    """(o [n, heads, dv], lse [n, heads] float32) of q [n, heads, dk], k [m,
+    kv_heads, dk] and v [m, kv_heads, dv] (sbc_softmax_attention_forward):
+
+        o_i = sum_j exp(s_ij - lse_i) v_j,   s_ij = scale q_i . k_j,
+
+    over the keys of the token's sequence, with causal those up to the token (the
+    last token sees the last key).  heads is a multiple of kv_heads, head h reads
+    head h // (heads // kv_heads).  splits [n_batch + 1] int32 cuts the tokens into
+    sequences (None: one) and k_splits the keys (None: as splits).  scale: 1 /
+    sqrt(dk) by default."""
+    index, dev, a = _softmax(q, k, v, splits, k_splits, scale, causal)
+    o = torch.empty((a.n, a.heads, a.dv), dtype=q.dtype, device=dev)
+    lse = torch.empty((a.n, a.heads), dtype=torch.float32, device=dev)
+    lib, ref = L.lib(), ctypes.byref(a)
+    ws = _Workspace(lib.sbc_softmax_attention_workspace_size(ref), dev)
+    L.check(lib.sbc_softmax_attention_forward(ref, _heads(q), _heads(k), _heads(v), _heads(o),
+                                              lse.data_ptr(), ws.ptr, ws.nbytes, _stream(index)))
+    return o, lse
+
+
+def softmax_attention_backward(do, q, k, v, o, lse, splits: Optional[torch.Tensor] = None,
+                               k_splits: Optional[torch.Tensor] = None,
+                               scale: Optional[float] = None, causal: bool = False):
+    """(dq, dk, dv) from the forward pass' o and lse
+    (sbc_softmax_attention_backward)."""
+    index, dev, a = _softmax(q, k, v, splits, k_splits, scale, causal)
+    shape = (a.n, a.heads, a.dv)
+    for name, x in (("do", do), ("o", o)):
+        _view(x, name, q.dtype, 3, index)
+        if x.shape != shape:
+            raise ValueError(f"{name} must be {shape}, got {tuple(x.shape)}")
+    _dense(lse, "lse", torch.float32, 2, index)
+    if lse.shape != shape[:2]:
+        raise ValueError(f"lse must be {shape[:2]}, got {tuple(lse.shape)}")
+    dq, dk, dv = (torch.empty(x.shape, dtype=q.dtype, device=dev) for x in (q, k, v))
+    lib, ref = L.lib(), ctypes.byref(a)
+    ws = _Workspace(lib.sbc_softmax_attention_backward_workspace_size(ref), dev)
+    L.check(lib.sbc_softmax_attention_backward(
+        ref, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), lse.data_ptr(), _heads(dq),
+        _heads(dk), _heads(dv), ws.ptr, ws.nbytes, _stream(index)))
+    return dq, dk, dv
+
+
+# ---------------------------------------------------------------- a cache in pages
+def _pages(t: Optional[torch.Tensor]):
+    if t is None:
+        return None
+    s = t.stride()
+    return ctypes.byref(L.SbcPages(t.data_ptr(), s[0], s[1], s[2]))
+
+
+def _streams(splits, n, n_batch, index):
+    if splits is not None:
+        _dense(splits, "splits", torch.int32, 1, index)
+        if splits.numel() != n_batch + 1:
+            raise ValueError(f"splits must be [{n_batch + 1}], got {tuple(splits.shape)}")
+    elif n != n_batch:
+        raise ValueError(f"without splits each of the {n_batch} streams has one new token, got {n}")
+
+
+def softmax_attention_paged(q, k_pages, v_pages, table, lengths,
+                            splits: Optional[torch.Tensor] = None, scale: Optional[float] = None):
+    """o [n, heads, dv] of n new tokens over the streams' kept ones, themselves
+    among them (sbc_softmax_attention_paged): softmax_attention_forward, causal,
+    with the keys and values in pages.
+
+    k_pages [n_pages, page, kv_heads, dk] and v_pages [n_pages, page, kv_heads, dv]
+    (any strides, the last axis dense); table [n_batch, width] int32: the pages of
+    each stream's tokens; lengths [n_batch] int32: its tokens, with the new ones;
+    splits [n_batch + 1] int32: its new tokens (None: one)."""
+    _first(q, "q", 3)
+    index, dev, (n, H, dk) = q.get_device(), q.device, q.shape
+    _view(k_pages, "k_pages", q.dtype, 4, index)
+    _view(v_pages, "v_pages", q.dtype, 4, index)
+    n_pages, page, G = k_pages.shape[:3]
+    if k_pages.shape[3] != dk:
+        raise ValueError(f"k_pages must be [n_pages, page, kv_heads, {dk}], "
+                         f"got {tuple(k_pages.shape)}")
+    if v_pages.shape[:3] != k_pages.shape[:3]:
+        raise ValueError(f"v_pages must be [{n_pages}, {page}, {G}, dv], got {tuple(v_pages.shape)}")
+    _dense(table, "table", torch.int32, 2, index)
+    _dense(lengths, "lengths", torch.int32, 1, index)
+    n_batch, width = table.shape
+    if lengths.numel() != n_batch:
+        raise ValueError(f"lengths must be [{n_batch}], got {tuple(lengths.shape)}")
+    _streams(splits, n, n_batch, index)
+    dv = v_pages.shape[3]
+    a = L.SbcSoftmaxAttention(n, 0, n_batch, H, G, dk, dv, _dtype_code(q),
+                              dk ** -0.5 if scale is None else float(scale), 1, _ptr(splits), None)
+    o = torch.empty((n, H, dv), dtype=q.dtype, device=dev)
+    lib, ref = L.lib(), ctypes.byref(a)
+    ws = _Workspace(lib.sbc_softmax_attention_paged_workspace_size(ref, page, width), dev)
+    L.check(lib.sbc_softmax_attention_paged(
+        ref, _heads(q), _pages(k_pages), _pages(v_pages), n_pages, page, table.data_ptr(), width,
+        lengths.data_ptr(), _heads(o), None, ws.ptr, ws.nbytes, _stream(index)))
+    return o
+
+
+def cache_slots(lengths, table, free, page: int, splits: Optional[torch.Tensor] = None,
+                n: Optional[int] = None, out_table: Optional[torch.Tensor] = None):
+    """(table, slots, lengths, needed) for the next tokens of n_batch streams
+    (sbc_cache_slots): the table [n_batch, width] int32 with the pages that they
+    need, taken from free [n_free] int32 in the streams' order (-1 where free has
+    no more); slots [n] int64, the new tokens' places in the pages (-1: none); the
+    streams' lengths with them; and needed [1] int32, how many pages of free all
+    streams need.
+
+    splits [n_batch + 1] int32: the streams' new tokens, n in all (None: one
+    each).  out_table: where the table is written, table itself if wanted (default:
+    a new one)."""
+    index = lengths.get_device() if isinstance(lengths, torch.Tensor) else -1
+    if index < 0:
+        _require(lengths, "lengths", torch.int32, 1)
+    _dense(lengths, "lengths", torch.int32, 1, index)
+    _dense(table, "table", torch.int32, 2, index)
+    _dense(free, "free", torch.int32, 1, index)
+    dev, (n_batch, width) = lengths.device, table.shape
+    if lengths.numel() != n_batch:
+        raise ValueError(f"lengths must be [{n_batch}], got {tuple(lengths.shape)}")
+    if n is None:
+        if splits is not None:
+            raise ValueError("n, the number of new tokens, is needed beside splits")
+        n = n_batch
+    _streams(splits, n, n_batch, index)
+    if out_table is None:
+        out_table = torch.empty_like(table)
+    else:
+        _dense(out_table, "out_table", torch.int32, 2, index)
+        if out_table.shape != table.shape:
+            raise ValueError(f"out_table must be {tuple(table.shape)}, got {tuple(out_table.shape)}")
+    slots = torch.empty(n, dtype=torch.int64, device=dev)
+    after = torch.empty_like(lengths)
+    needed = torch.empty(1, dtype=torch.int32, device=dev)
+    lib = L.lib()
+    ws = _Workspace(lib.sbc_cache_slots_workspace_size(n_batch), dev)
+    L.check(lib.sbc_cache_slots(lengths.data_ptr(), _ptr(splits), n, n_batch, table.data_ptr(),
+                                width, int(page), free.data_ptr(), free.numel(),
+                                out_table.data_ptr(), slots.data_ptr(), after.data_ptr(),
+                                needed.data_ptr(), ws.ptr, ws.nbytes, _stream(index)))
+    return out_table, slots, after, needed
+
+
+def cache_append(k, v, k_pages, v_pages, slots):
+    """The rows of k [n, kv_heads, dk] and v [n, kv_heads, dv] written to their
+    slots ([n] int64, from cache_slots; outside the pages: left out, else
+    distinct) of k_pages [n_pages, page, kv_heads, dk] and v_pages
+    (sbc_cache_append).  k may be None with k_pages, v with v_pages."""
+    one, pages = (k, k_pages) if k is not None else (v, v_pages)
+    if one is None:
+        raise ValueError("k or v is needed")
+    _first(one, "k" if k is not None else "v", 3)
+    index, (n, G) = one.get_device(), one.shape[:2]
+    d = [0, 0]
+    for i, (name, x, to) in enumerate((("k", k, k_pages), ("v", v, v_pages))):
+        if (x is None) != (to is None):
+            raise ValueError(f"{name} and {name}_pages go together")
+        if x is None:
+            continue
+        _view(x, name, one.dtype, 3, index)
+        _view(to, name + "_pages", one.dtype, 4, index)
+        d[i] = x.shape[2]
+        if x.shape[:2] != (n, G):
+            raise ValueError(f"{name} must be [{n}, {G}, d], got {tuple(x.shape)}")
+        if to.shape != (*pages.shape[:2], G, d[i]):
+            raise ValueError(f"{name}_pages must be [{pages.shape[0]}, {pages.shape[1]}, {G}, {d[i]}], "
+                             f"got {tuple(to.shape)}")
+    _dense(slots, "slots", torch.int64, 1, index)
+    if slots.numel() != n:
+        raise ValueError(f"slots must be [{n}], got {tuple(slots.shape)}")
+    L.check(L.lib().sbc_cache_append(_heads(k), _heads(v), n, G, d[0], d[1], _dtype_code(one),
+                                     slots.data_ptr(), _pages(k_pages), _pages(v_pages),
+                                     pages.shape[0], pages.shape[1], _stream(index)))
