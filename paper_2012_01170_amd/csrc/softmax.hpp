@@ -70,6 +70,7 @@ struct SoftmaxArgs {
     const float *lse_in;
     float *delta;
     float *part_dk, *part_dv;
+    int32_t even_rows;  // whether tiles of rows begin with a token's first head, at 32-bit offsets
 };
 
 __device__ __forceinline__ int32_t clamp_i(int32_t x, int32_t lo, int32_t hi) {
@@ -274,10 +275,31 @@ template <typename T, int D, int kRows, int kThreads, bool kWhole> struct TileLo
     static_assert(kRows * kPerRow % kThreads == 0, "pieces");
     u32x4v raw[kSteps];
     uint32_t there;  // a bit for each piece that exists (the others are zeroed in settle())
+    uint32_t off[kSteps], columns;  // of load_all(): the pieces' bytes, and those that exist
     __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
     __device__ __forceinline__ static int row_of(int s) { return (s * kThreads + tid()) / kPerRow; }
     __device__ __forceinline__ static int col_of(int s) {
         return (s * kThreads + tid()) % kPerRow * kVec<T>;
+    }
+    // For tiles whose rows all exist, `stride` elements apart (kWhole; below 2^22)
+    __device__ __forceinline__ void places(int64_t stride, int width) {
+        places([&](int r) { return (uint32_t)r * (uint32_t)stride; }, width);
+    }
+    // or whose row r is at(r) elements from the first
+    template <typename F> __device__ __forceinline__ void places(F at, int width) {
+        columns = 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const bool ok = col_of(s) < width;
+            off[s] = (at(row_of(s)) + (ok ? col_of(s) : 0)) * (uint32_t)sizeof(T);
+            columns |= (uint32_t)ok << s;
+        }
+    }
+    __device__ __forceinline__ void load_all(const T *base) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            __builtin_memcpy(&raw[s], reinterpret_cast<const char *>(base) + off[s], 16);
+        there = columns;
     }
     // row_at(row): where the tile's row begins, nullptr if it does not exist; `any` is an address
     // that may be read
@@ -305,13 +327,39 @@ template <typename T, int D, int kRows, int kThreads, bool kWhole> struct TileLo
 #pragma unroll
             for (int i = 0; i < 4; ++i) raw[s][i] = there >> s & 1u ? raw[s][i] : 0u;
     }
-    __device__ __forceinline__ bool not_finite() const {
+    // Values that are infinite or NaN to zero, and the first such row of each column, counted from
+    // `first` on, to first_bad[column].  Where some rows of a product see a tile only in part, the
+    // others' weight 0 times such a value would be NaN; what they are to those that do see them is
+    // made up for at the end (FirstBad).
+    __device__ __forceinline__ void put_bad_apart(int32_t first, int32_t *first_bad) {
         bool found = false;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i) found |= !finite_bits(raw[s][i], sizeof(T) == 2);
-        return found;
+        if (!found) return;
+        for (int s = 0; s < kSteps; ++s) {
+            uint32_t w[4];
+            T e[kVec<T>];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = 0;
+#pragma unroll
+                for (int r = 0; r < kSteps; ++r) w[i] = r == s ? raw[r][i] : w[i];
+            }
+            __builtin_memcpy(e, w, 16);
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i)
+                if ((__float_as_uint(to_f32(e[i])) & 0x7F800000u) == 0x7F800000u) {
+                    e[i] = T(0);
+                    atomicMin(first_bad + col_of(s) + i, first + row_of(s));
+                }
+            __builtin_memcpy(w, e, 16);
+#pragma unroll
+            for (int r = 0; r < kSteps; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[r][i] = r == s ? w[i] : raw[r][i];
+        }
     }
     __device__ __forceinline__ void store(bf16_t *tile) const {
         constexpr int kPlane = kRows * D;
@@ -334,8 +382,15 @@ template <typename T, int D, int kRows, int kThreads, bool kWhole> struct TileLo
     }
 };
 
-// The other half's value of the same row
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// A row's two halves joined, in both
+__device__ __forceinline__ float halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // Where the keys of a tile lie: lane j looks up key first + j (j below kKeys).
 struct KeyPlaces {
@@ -389,12 +444,12 @@ __device__ __forceinline__ uint32_t seen_bits(uint64_t there, int u, int32_t vis
 // at most 2^8, and rounded as a smaller one is), so that most tiles leave the sums alone.
 template <int D, int kSub>
 __device__ __forceinline__ void softmax_weights(floatx16 (&x)[kSub], float scale2, RowSums<D> &s) {
-    float top = x[0][0];
+    float top = fmaxf(x[0][0], x[kSub - 1][15]);
 #pragma unroll
     for (int u = 0; u < kSub; ++u)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, x[u][r]);
-    top = fmaxf(top, other_half(top)) * scale2;
+        for (int r = 0; r < 16; r += 2) top = fmaxf(fmaxf(top, x[u][r]), x[u][r + 1]);
+    top = halves_max(top) * scale2;
     if (__any(top > s.m + 8.f)) {
         const float m = fmaxf(s.m, top);
         const float f = m == s.m ? 1.f : __builtin_amdgcn_exp2f(s.m - m);
@@ -417,58 +472,66 @@ __device__ __forceinline__ void softmax_weights(floatx16 (&x)[kSub], float scale
     s.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
-// o += weights x values of the tile vt
-template <typename T, int D, int kSub>
-__device__ __forceinline__ void add_values(const floatx16 (&x)[kSub], const bf16_t *vt,
-                                           const LaneAt32<D> &at, RowSums<D> &s) {
+// What may move past a point of the schedule: anything but matrix products and LDS reads,
+// which are to stay in the order that the loops below give them.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6 | 0x70); }
+
+// x[j] += the rows that read(k, j) gives of step k times operand j, kJobs products side by side.
+// The rows of kAhead steps are on their way from LDS while a step's products run: read where
+// they are used, a wave waited out LDS' latency every two products.
+template <typename T, int D, int kJobs, typename Read, typename Operand>
+__device__ __forceinline__ void row_products(Read read, Operand operand, floatx16 (&x)[kJobs]) {
+    constexpr int NP = kParts<T>, kSteps = D / 16, kAhead = NP == 1 && kJobs == 1 ? 4 : 2;
+    bf16x8 f[kAhead][kJobs][NP];
+#pragma unroll
+    for (int k = 0; k < kAhead && k < kSteps; ++k)
+#pragma unroll
+        for (int j = 0; j < kJobs; ++j) read(k, j, f[k][j]);
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        keep_order();
+#pragma unroll
+        for (int j = 0; j < kJobs; ++j) mma32<NP, NP>(f[k % kAhead][j], operand(k, j), x[j]);
+        if (k + kAhead < kSteps) {
+            keep_order();
+#pragma unroll
+            for (int j = 0; j < kJobs; ++j) read(k + kAhead, j, f[k % kAhead][j]);
+        }
+    }
+}
+
+// acc[t] += columns 32 t .. + 31 of the tile, transposed, times weights by rows: k-step h takes
+// rows 16 h .. + 15.  First read(), which may lie well before, then add().
+template <typename T, int D, int kRows> struct ColumnProducts {
+    static constexpr int NP = kParts<T>, kSteps = kRows / 16;
+    bf16x8 f[2][D / 32][NP];
+    // step h of the rows that begin `first` (a multiple of 32) into a tile
+    __device__ __forceinline__ void fetch(const bf16_t *tile, int plane, int first,
+                                          const LaneAt32<D> &at, int h) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) frag_col32<D, NP>(tile, plane, first / 16 + h, t, at, f[h % 2][t]);
+    }
+    __device__ __forceinline__ void read(const bf16_t *tile, int plane, int first,
+                                         const LaneAt32<D> &at) {
+        fetch(tile, plane, first, at, 0);
+        keep_order();
+    }
+    __device__ __forceinline__ void add(const floatx16 (&x)[kRows / 32], const bf16_t *tile,
+                                        int plane, int first, const LaneAt32<D> &at,
+                                        floatx16 (&acc)[D / 32]) {
 #pragma clang fp contract(off)
-    constexpr int NP = kParts<T>;
 #pragma unroll
-    for (int h = 0; h < 2 * kSub; ++h) {
-        bf16x8 w[NP];
-        frag_regs<T>(x[h / 2], h % 2, w);
+        for (int h = 0; h < kSteps; ++h) {
+            if (h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
+            bf16x8 w[NP];
+            frag_regs<T>(x[h / 2], h % 2, w);
+            keep_order();
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) {
-            bf16x8 v[NP];
-            frag_col32<D, NP>(vt, 32 * kSub * D, h, t, at, v);
-            mma32<NP, NP>(v, w, s.o[t]);
+            for (int t = 0; t < D / 32; ++t) mma32<NP, NP>(f[h % 2][t], w, acc[t]);
+            keep_order();
         }
     }
-}
-// The same key by key: values that are infinite or NaN meet only the rows that see them
-// (a product with the weight 0 of a hidden one would be NaN).
-template <typename T, int D, int kSub>
-__device__ __forceinline__ void add_values_singly(const floatx16 (&x)[kSub], const uint32_t (&seen)[kSub],
-                                               const bf16_t *vt, RowSums<D> &s) {
-    const int lane = threadIdx.x & 63, g = lane >> 5;
-    for (int j = 0; j < 32 * kSub; ++j) {
-        const int reg = 4 * (j % 32 / 8) + j % 4, owner = (j / 4) % 2;
-        float mine = 0.f;
-        uint32_t sees = 0;
-#pragma unroll
-        for (int u = 0; u < kSub; ++u)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (u == j / 32 && r == reg) {
-                    mine = x[u][r];
-                    sees = seen[u] >> (8 * (r / 4) + r % 4) & 1u;
-                }
-        const float w = __shfl(mine, (lane & 31) + 32 * owner);
-        const bool ok = __shfl((int)sees, (lane & 31) + 32 * owner) != 0;
-        if (ok) {
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int at = tile_at<D>(j, 32 * t + 8 * (r / 4) + 4 * g + r % 4);
-                    float v = 0.f;
-#pragma unroll
-                    for (int i = kParts<T> - 1; i >= 0; --i) v += to_f32(vt[i * 32 * kSub * D + at]);
-                    s.o[t][r] = fmaf(w, v, s.o[t][r]);
-                }
-        }
-    }
-}
+};
 
 // Four channels of an output's row: columns c .. + 3 of `width`
 template <typename T, bool kWhole>

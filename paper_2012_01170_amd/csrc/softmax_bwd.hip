@@ -45,6 +45,12 @@ sbc_status backward(SoftmaxArgs p, const sbc_softmax_attention *a, hipStream_t s
         }
         if (a->m > 0) {
             p.slots = (int32_t)cols;
+            constexpr int kRows = kGradRows<T, D>;
+            const int32_t group = a->heads / a->kv_heads;
+            p.even_rows = kRows % group == 0;
+            for (const sbc_heads *x : {&p.q, &p.d_o})
+                if (x->token_stride >= 1 << 22 || x->head_stride > ((int64_t)1 << 28) / group)
+                    p.even_rows = 0;
             trace_before("softmax_dkv", stream);
             hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole>), dim3((unsigned)dkv_blocks),
                                dim3(kGradThreads), 0, stream, p);
@@ -119,7 +125,7 @@ extern "C" sbc_status sbc_softmax_attention_backward(
         p.dv_out = *dv;
     }
     p.lse_in = lse;
-    const bool whole = softmax_whole(a);
+    const bool whole = softmax_whole(a, {&p.k, &p.v});
     if (dt == SBC_F32)
         return whole ? backward<float, true>(p, a, stream) : backward<float, false>(p, a, stream);
     return whole ? backward<bf16_t, true>(p, a, stream) : backward<bf16_t, false>(p, a, stream);

@@ -16,6 +16,7 @@ constexpr int kGradThreads = 256;
 template <typename T, int D> constexpr int kGradKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
 // Waves a SIMD: the rows' operands and sums of wide heads in float32 fill its registers alone
 template <typename T, int D> constexpr int kGradWaves = sizeof(T) == 4 && D > 32 ? 1 : 2;
+template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) * D > 128 ? 1 : 2;
 
 template <typename T, int D, bool kWhole>
 __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_kernel(SoftmaxArgs p) {
@@ -42,8 +43,6 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
     };
     const int32_t most = __builtin_amdgcn_readfirstlane(limit_of(r0 + 127));
     const int32_t wave_least = __builtin_amdgcn_readfirstlane(limit_of(wave_row));
-    const int32_t wave_most =
-        wave_row < rows ? __builtin_amdgcn_readfirstlane(limit_of(wave_row + 31)) : 0;
 
     const int64_t place = s.q0 + token;
     bf16x8 q[D / 16][NP], g[D / 16][NP];
@@ -73,7 +72,7 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
                 for (int e = 0; e < kVec<T>; ++e) delta = fmaf(a[e], c[e], delta);
             }
         }
-        delta += other_half(delta);
+        delta = halves_sum(delta);
     }
     const int64_t flat = place * p.heads + head;
     if (there && lane < 32) p.delta[flat] = delta;
@@ -86,7 +85,16 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
     const T *const vbase =
         static_cast<const T *>(p.v.data) + s.k0 * p.v.token_stride + head_k * p.v.head_stride;
     TileLoad<T, D, KB, kGradThreads, kWhole> sk, sv;
+    if (kWhole) {
+        sk.places(p.k.token_stride, p.dk);
+        sv.places(p.v.token_stride, p.dv);
+    }
     auto fetch = [&](int32_t k0) {
+        if (kWhole && k0 + KB <= s.lk) {
+            sk.load_all(kbase + k0 * p.k.token_stride);
+            sv.load_all(vbase + k0 * p.v.token_stride);
+            return;
+        }
         sk.load([&](int r) { return k0 + r < s.lk ? kbase + (k0 + r) * p.k.token_stride : nullptr; },
                 kbase, p.dk);
         sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
@@ -104,19 +112,17 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
         sv.store(vt);
         __syncthreads();
         if (k0 + KB < most) fetch(k0 + KB);
-        if (k0 >= wave_most) continue;
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
             floatx16 w[2];  // scores, and dO v
             clear(w);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                bf16x8 f[NP], h[NP];
-                frag_row32<D, NP>(kt, kPlane, u, k, at, f);
-                frag_row32<D, NP>(vt, kPlane, u, k, at, h);
-                mma32<NP, NP>(f, q[k], w[0]);
-                mma32<NP, NP>(h, g[k], w[1]);
-            }
+            row_products<T, D, 2>(
+                [&](int k, int j, bf16x8(&f)[NP]) {
+                    frag_row32<D, NP>(j ? vt : kt, kPlane, u, k, at, f);
+                },
+                [&](int k, int j) -> const bf16x8(&)[NP] { return j ? g[k] : q[k]; }, w);
+            ColumnProducts<T, D, 32> keys;
+            keys.read(kt, kPlane, 32 * u, at);
             const bool masked = k0 + 32 * u + 32 > wave_least;
             const uint32_t seen = masked ? seen_bits(~0ull, 0, limit - k0 - 32 * u) : ~0u;
 #pragma unroll
@@ -125,17 +131,7 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
                 const float d = e * (w[1][r] - delta);
                 w[0][r] = !masked || (seen >> (8 * (r / 4) + r % 4) & 1u) ? d : 0.f;
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 ds[NP];
-                frag_regs<T>(w[0], h, ds);
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    bf16x8 f[NP];
-                    frag_col32<D, NP>(kt, kPlane, 2 * u + h, t, at, f);
-                    mma32<NP, NP>(f, ds, acc[t]);
-                }
-            }
+            keys.add(reinterpret_cast<const floatx16(&)[1]>(w[0]), kt, kPlane, 32 * u, at, acc);
         }
     }
     if (!there) return;
@@ -158,7 +154,7 @@ constexpr int kGradCols = 128;
 template <typename T, int D> constexpr int kGradRows = sizeof(T) == 4 && D > 64 ? 32 : 64;
 
 template <typename T, int D, bool kWhole>
-__global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
+__global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
 #pragma clang fp contract(off)
     constexpr int NP = kParts<T>, RB = kGradRows<T, D>, kSub = RB / 32, kPlane = RB * D;
     __shared__ __attribute__((aligned(16))) bf16_t qt[NP * kPlane], gt[NP * kPlane];
@@ -202,14 +198,31 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dkv_
     TileLoad<T, D, RB, kGradThreads, kWhole> sq, sg;
     float next_lse = 0.f, next_delta = 0.f;
     int32_t next_limit = 0;
+    if (kWhole && p.even_rows) {
+        auto place = [&](const sbc_heads &x) {
+            return [&](int r) {
+                const int32_t token = divide(r, p.group);
+                return (uint32_t)token * (uint32_t)x.token_stride +
+                       (uint32_t)(r - token * group) * (uint32_t)x.head_stride;
+            };
+        };
+        sq.places(place(p.q), p.dk);
+        sg.places(place(p.d_o), p.dv);
+    }
     auto fetch = [&](int32_t r0) {
         auto row_of = [&](const T *base, const sbc_heads &x, int r) -> const T * {
             if (r0 + r >= rows) return nullptr;
             const int32_t token = divide(r0 + r, p.group);
             return base + token * x.token_stride + (r0 + r - token * group) * x.head_stride;
         };
-        sq.load([&](int r) { return row_of(qbase, p.q, r); }, qbase, p.dk);
-        sg.load([&](int r) { return row_of(gbase, p.d_o, r); }, gbase, p.dv);
+        if (kWhole && p.even_rows && r0 + RB <= rows) {
+            const int32_t token = divide(r0, p.group);
+            sq.load_all(qbase + token * p.q.token_stride);
+            sg.load_all(gbase + token * p.d_o.token_stride);
+        } else {
+            sq.load([&](int r) { return row_of(qbase, p.q, r); }, qbase, p.dk);
+            sg.load([&](int r) { return row_of(gbase, p.d_o, r); }, gbase, p.dv);
+        }
         if (threadIdx.x < RB) {
             const int32_t r = r0 + threadIdx.x;
             // (no weight for rows that do not exist or have no keys)
@@ -248,24 +261,19 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dkv_
         }
         __syncthreads();
         if (r0 + step < rows) fetch(r0 + step);
-        if (wave_key >= s.lk) continue;
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
-            // (limits do not fall along the rows; those past the last have none)
+            // (limits do not fall along the rows that there are; the others' sums are infinite)
             const int32_t first = __builtin_amdgcn_readfirstlane(limits[32 * u]);
-            const int32_t last_row = r0 + 32 * u + 31 < rows ? 31 : rows - 1 - r0 - 32 * u;
-            if (last_row < 0) break;
-            if (__builtin_amdgcn_readfirstlane(limits[32 * u + last_row]) <= wave_key) continue;
             floatx16 w[2];
             clear(w);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                bf16x8 f[NP], h[NP];
-                frag_row32<D, NP>(qt, kPlane, u, k, at, f);
-                frag_row32<D, NP>(gt, kPlane, u, k, at, h);
-                mma32<NP, NP>(f, kf[k], w[0]);
-                mma32<NP, NP>(h, vf[k], w[1]);
-            }
+            row_products<T, D, 2>(
+                [&](int k, int j, bf16x8(&f)[NP]) {
+                    frag_row32<D, NP>(j ? gt : qt, kPlane, u, k, at, f);
+                },
+                [&](int k, int j) -> const bf16x8(&)[NP] { return j ? vf[k] : kf[k]; }, w);
+            ColumnProducts<T, D, 32> grads, queries;
+            grads.read(gt, kPlane, 32 * u, at);
             const bool masked = first < wave_key + 32;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -284,24 +292,9 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dkv_
                     w[1][4 * j + i] = ok ? d : 0.f;
                 }
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 e[NP], ds[NP];
-                frag_regs<T>(w[0], h, e);
-                frag_regs<T>(w[1], h, ds);
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    bf16x8 f[NP];
-                    frag_col32<D, NP>(gt, kPlane, 2 * u + h, t, at, f);
-                    mma32<NP, NP>(f, e, dv[t]);
-                }
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    bf16x8 f[NP];
-                    frag_col32<D, NP>(qt, kPlane, 2 * u + h, t, at, f);
-                    mma32<NP, NP>(f, ds, dk[t]);
-                }
-            }
+            grads.add(reinterpret_cast<const floatx16(&)[1]>(w[0]), gt, kPlane, 32 * u, at, dv);
+            queries.read(qt, kPlane, 32 * u, at);
+            queries.add(reinterpret_cast<const floatx16(&)[1]>(w[1]), qt, kPlane, 32 * u, at, dk);
         }
     }
     if (!there) return;

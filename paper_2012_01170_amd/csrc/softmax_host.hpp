@@ -42,10 +42,14 @@ inline int64_t softmax_places(const sbc_softmax_attention *a, int32_t rows) {
     return (int64_t)a->n * (a->heads / a->kv_heads) / rows + a->n_batch;
 }
 
-// Whole 16-byte pieces of rows
-inline bool softmax_whole(const sbc_softmax_attention *a) {
+// Whole 16-byte pieces of rows, at 32-bit offsets within a tile
+inline bool softmax_whole(const sbc_softmax_attention *a,
+                          std::initializer_list<const sbc_heads *> arrays) {
     const int v = a->dtype == SBC_F32 ? 4 : 8;
-    return a->dk % v == 0 && a->dv % v == 0;
+    if (a->dk % v || a->dv % v) return false;
+    for (const sbc_heads *x : arrays)
+        if (x->token_stride >= 1 << 22) return false;
+    return true;
 }
 
 // The kernels' arguments that every call has

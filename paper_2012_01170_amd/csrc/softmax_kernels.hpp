@@ -12,6 +12,11 @@ constexpr int kSoftmaxThreads = 256;
 // would fill more than the 64 KB that let two workgroups share a CU's LDS.
 template <typename T, int D> constexpr int kTileKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
 
+// 32s of keys that a wave takes at once, as its registers allow
+template <typename T, int D> constexpr int kTogether = sizeof(T) == 2 && D <= 64 ? 2 : 1;
+// Waves a SIMD: wide float32 heads fill its registers alone
+template <typename T, int D> constexpr int kTileWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
+
 constexpr int kTileRows = 128;  // of softmax_tile_kernel: 32 a wave
 constexpr int kFewRows = 32;    // of softmax_rows_kernel
 
@@ -25,10 +30,11 @@ __device__ __forceinline__ int32_t part_keys(int32_t lk, int32_t parts) {
 // A workgroup has 128 rows, 32 a wave, and goes through the keys that they see in tiles,
 // which its waves share in LDS; the next tile is on its way into registers meanwhile.
 template <typename T, int D, bool kWhole, bool kPaged>
-__global__ __launch_bounds__(kSoftmaxThreads, 2) void softmax_tile_kernel(SoftmaxArgs p) {
-    constexpr int NP = kParts<T>, KB = kTileKeys<T, D>, kSub = KB / 32, kPlane = KB * D;
+__global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_tile_kernel(SoftmaxArgs p) {
+    constexpr int NP = kParts<T>, KB = kTileKeys<T, D>, kPlane = KB * D;
+    constexpr int kSub = KB < 32 * kTogether<T, D> ? 1 : kTogether<T, D>;
     __shared__ __attribute__((aligned(16))) bf16_t kt[NP * kPlane], vt[NP * kPlane];
-    __shared__ int32_t bad[2];
+    __shared__ int32_t first_bad[D];  // (TileLoad::put_bad_apart)
     const int32_t head_k = blockIdx.x % p.kv_heads;
     // (from the back: a causal sequence's last tiles are its longest)
     const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads;
@@ -54,8 +60,6 @@ __global__ __launch_bounds__(kSoftmaxThreads, 2) void softmax_tile_kernel(Softma
     const int32_t least = __builtin_amdgcn_readfirstlane(limit_of(r0));
     const int32_t most = __builtin_amdgcn_readfirstlane(limit_of(r0 + kTileRows - 1));
     const int32_t wave_least = __builtin_amdgcn_readfirstlane(limit_of(wave_row));
-    const int32_t wave_most =
-        wave_row < rows ? __builtin_amdgcn_readfirstlane(limit_of(wave_row + 31)) : 0;
 
     bf16x8 q[D / 16][NP];
     {
@@ -72,74 +76,75 @@ __global__ __launch_bounds__(kSoftmaxThreads, 2) void softmax_tile_kernel(Softma
         vbase = static_cast<const T *>(p.v.data) + s.k0 * p.v.token_stride + head_k * p.v.head_stride;
     }
     TileLoad<T, D, KB, kSoftmaxThreads, kWhole> sk, sv;
-    KeyPlaces places, next_places;
+    KeyPlaces next_places;
     auto fetch = [&](int32_t k0) {
         if constexpr (kPaged) {
             sk.load([&](int r) { return next_places.row<T>(p.pages.k, head_k, r); }, kbase, p.dk);
             sv.load([&](int r) { return next_places.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
         } else {
+            if (kWhole && k0 + KB <= s.lk) {
+                sk.load_all(kbase + k0 * p.k.token_stride);
+                sv.load_all(vbase + k0 * p.v.token_stride);
+                return;
+            }
             sk.load([&](int r) { return k0 + r < s.lk ? kbase + (k0 + r) * p.k.token_stride : nullptr; },
                     kbase, p.dk);
             sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
                     vbase, p.dv);
         }
     };
+    if (kWhole && !kPaged) {
+        sk.places(p.k.token_stride, p.dk);
+        sv.places(p.v.token_stride, p.dv);
+    }
     const LaneAt32<D> at;
     RowSums<D> sums;
-    if (threadIdx.x < 2) bad[threadIdx.x] = 0;
-    int turn = 0;
+    if (threadIdx.x < D) first_bad[threadIdx.x] = INT32_MAX;
+    __syncthreads();
     constexpr uint64_t kAll = KB == 64 ? ~0ull : 0xFFFFFFFFull;
     if (most > 0) {
         if constexpr (kPaged) next_places.template find<KB>(p, s, 0, s.lk);
         fetch(0);
     }
-    for (int32_t k0 = 0; k0 < most; k0 += KB, turn ^= 1) {
+    for (int32_t k0 = 0; k0 < most; k0 += KB) {
         __syncthreads();  // the last tile has been read
         sk.settle();
         sv.settle();
+        if (k0 + KB > least) sv.put_bad_apart(k0, first_bad);
         sk.store(kt);
         sv.store(vt);
-        if (k0 + KB > least && sv.not_finite()) bad[turn] = 1;
-        if (threadIdx.x == 0) bad[turn ^ 1] = 0;
-        if constexpr (kPaged) places = next_places;
+        const uint64_t known = kPaged ? next_places.there : kAll;
         __syncthreads();
         if (k0 + KB < most) {
             if constexpr (kPaged) next_places.template find<KB>(p, s, k0 + KB, s.lk);
             fetch(k0 + KB);
         }
-        if (k0 >= wave_most) continue;
-        floatx16 x[kSub];
-        clear(x);
+        // (tiles that hold nothing for this wave, behind the diagonal, are gone through as well: with a
+        // branch around them the sums were copied from registers to registers in every tile)
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k)
+        for (int u0 = 0; u0 < KB / 32; u0 += kSub) {
+            floatx16 x[kSub];
+            clear(x);
+            row_products<T, D, kSub>(
+                [&](int k, int j, bf16x8(&f)[NP]) { frag_row32<D, NP>(kt, kPlane, u0 + j, k, at, f); },
+                [&](int k, int j) -> const bf16x8(&)[NP] { return q[k]; }, x);
+            ColumnProducts<T, D, 32 * kSub> values;
+            values.read(vt, kPlane, 32 * u0, at);
+            if (k0 + 32 * (u0 + kSub) > wave_least || known != kAll) {
 #pragma unroll
-            for (int u = 0; u < kSub; ++u) {
-                bf16x8 f[NP];
-                frag_row32<D, NP>(kt, kPlane, u, k, at, f);
-                mma32<NP, NP>(f, q[k], x[u]);
-            }
-        const uint64_t known = kPaged ? places.there : kAll;
-        if (k0 + KB > wave_least || known != kAll) {
-            uint32_t seen[kSub];
+                for (int u = 0; u < kSub; ++u) {
+                    const uint32_t seen = seen_bits(known, u0 + u, limit - k0);
 #pragma unroll
-            for (int u = 0; u < kSub; ++u) {
-                seen[u] = seen_bits(known, u, limit - k0);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    x[u][r] = seen[u] >> (8 * (r / 4) + r % 4) & 1u ? x[u][r] : -INFINITY;
+                    for (int r = 0; r < 16; ++r)
+                        x[u][r] = seen >> (8 * (r / 4) + r % 4) & 1u ? x[u][r] : -INFINITY;
+                }
             }
             softmax_weights<D, kSub>(x, p.scale2, sums);
-            if (bad[turn])
-                add_values_singly<T, D, kSub>(x, seen, vt, sums);
-            else
-                add_values<T, D, kSub>(x, vt, at, sums);
-        } else {
-            softmax_weights<D, kSub>(x, p.scale2, sums);
-            add_values<T, D, kSub>(x, vt, at, sums);
+            values.add(x, vt, kPlane, 32 * u0, at, sums.o);
         }
     }
     if (!there) return;
-    const float l = sums.l + other_half(sums.l);
+    const float l = halves_sum(sums.l);
     const int64_t place = s.q0 + token;
     if (p.lse && lane < 32)
         p.lse[place * p.heads + head] = l == 0.f ? -INFINITY : (sums.m + log2f(l)) * kLn2;
@@ -151,7 +156,11 @@ __global__ __launch_bounds__(kSoftmaxThreads, 2) void softmax_tile_kernel(Softma
         for (int j = 0; j < 4; ++j) {
             float y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = l == 0.f ? 0.f : sums.o[t][4 * j + i] * part;
+            for (int i = 0; i < 4; ++i) {
+                const int c = 32 * t + 8 * j + 4 * (lane >> 5) + i;
+                y[i] = l == 0.f ? 0.f : sums.o[t][4 * j + i] * part;
+                if (first_bad[c] < limit) y[i] = NAN;
+            }
             put4<T, kWhole>(out, 32 * t + 8 * j + 4 * (lane >> 5), p.dv, y);
         }
 }
@@ -168,6 +177,7 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     constexpr int kTiles = 4 * NP * kPlane;
     __shared__ __attribute__((aligned(16))) bf16_t lds[kTiles > kJoin ? kTiles : kJoin];
     __shared__ float wave_m[4][32], wave_l[4][32];
+    __shared__ int32_t first_bad[D];
     const int32_t head_k = blockIdx.x % p.kv_heads;
     const int32_t part = blockIdx.x / p.kv_heads % p.parts;
     const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads / p.parts;
@@ -212,7 +222,7 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     }
     u32x4v kraw[D / 16][8 / kVec<T>];
     TileLoad<T, D, 32, 64, kWhole> sv;
-    KeyPlaces places, next_places;
+    KeyPlaces next_places;
     auto fetch = [&](int32_t k0) {
         if constexpr (kPaged) {
             const T *at = next_places.row<T>(p.pages.k, head_k, lane & 31);
@@ -229,6 +239,8 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     const LaneAt32<D> at;
     RowSums<D> sums;
     bf16_t *const vt = lds + wave * NP * kPlane;
+    if (threadIdx.x < D) first_bad[threadIdx.x] = INT32_MAX;
+    __syncthreads();
     int32_t k0 = first + 32 * wave;
     if (k0 < end) {
         if constexpr (kPaged) next_places.template find<32>(p, s, k0, s.lk);
@@ -240,9 +252,9 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) raw_parts<T>(kraw[k], kf[k]);
         sv.settle();
+        if (k0 + 32 > least) sv.put_bad_apart(k0, first_bad);
         sv.store(vt);
-        const bool bad = k0 + 32 > least && __any(sv.not_finite());
-        if constexpr (kPaged) places = next_places;
+        const uint64_t known = kPaged ? next_places.there : 0xFFFFFFFFull;
         if (k0 + 128 < end) {
             if constexpr (kPaged) next_places.template find<32>(p, s, k0 + 128, s.lk);
             fetch(k0 + 128);
@@ -251,23 +263,21 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
         clear(w);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) mma32<NP, NP>(kf[k], q[k], w[0]);
-        const uint64_t known = kPaged ? places.there : 0xFFFFFFFFull;
         const int32_t visible = limit < end ? limit : end;
-        const uint32_t seen[1] = {seen_bits(known, 0, visible - k0)};
+        const uint32_t seen = seen_bits(known, 0, visible - k0);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-            w[0][r] = seen[0] >> (8 * (r / 4) + r % 4) & 1u ? w[0][r] : -INFINITY;
+            w[0][r] = seen >> (8 * (r / 4) + r % 4) & 1u ? w[0][r] : -INFINITY;
         softmax_weights<D, 1>(w, p.scale2, sums);
         // (the wave's own LDS, which it reads in the order of its writes)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (bad)
-            add_values_singly<T, D, 1>(w, seen, vt, sums);
-        else
-            add_values<T, D, 1>(w, vt, at, sums);
+        ColumnProducts<T, D, 32> values;
+        values.read(vt, kPlane, 0, at);
+        values.add(w, vt, kPlane, 0, at, sums.o);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     // joined: the waves' sums as weights of the largest maximum
-    const float l = sums.l + other_half(sums.l);
+    const float l = halves_sum(sums.l);
     if (lane < 32) {
         wave_m[wave][lane] = sums.m;
         wave_l[wave][lane] = l;
@@ -293,6 +303,7 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     for (int i = 0; i < 4; ++i)
         total += wave_l[i][jr] * weight(wave_m[i][jr], out_top);
     const float inverse = 1.f / total;
+    const int32_t out_limit = limit_of(out_row);
     const int64_t flat = place * p.heads + out_head;
     if (out_row < rows && jc == 0) {
         const float lse2 = total == 0.f ? -INFINITY : out_top + log2f(total);
@@ -320,7 +331,10 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
             for (int i = 0; i < 4; ++i) y[i] += z[i];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * inverse;
+        for (int i = 0; i < 4; ++i) {
+            y[i] = total == 0.f ? 0.f : y[i] * inverse;
+            if (first_bad[32 * t + jc + i] < out_limit) y[i] = NAN;
+        }
         if (out_row < rows) {
             if (p.parts > 1)
                 put4<float, false>(p.part_o + ((int64_t)part * p.n * p.heads + flat) * p.dv, 32 * t + jc,

@@ -19,7 +19,7 @@ sbc_status softmax_forward(SoftmaxArgs p, const sbc_softmax_attention *a, const 
         p.part_lse = c.take<float>((size_t)plan.parts * a->n * a->heads);
     }
     const dim3 grid((unsigned)plan.blocks), block(kSoftmaxThreads);
-    const bool whole = softmax_whole(a);
+    const bool whole = softmax_whole(a, {&p.k, &p.v});
     trace_before("softmax_fwd", stream);
     softmax_dispatch(a->dk > a->dv ? a->dk : a->dv, [&](auto d) {
         constexpr int D = decltype(d)::value;
