@@ -151,17 +151,32 @@ template <int N> __device__ __forceinline__ void clear(floatx16 (&x)[N]) {
         for (int r = 0; r < 16; ++r) x[i][r] = 0.f;
 }
 
-// A lane's places in a tile of D columns (tile_at) for 32 x 32 products
+// A tile of D columns in LDS, row after row, one plane a part, the 16-byte pieces of a row
+// permuted by its number so that lanes which LDS serves in one cycle do not meet in one of its 64
+// banks (256 bytes): of reads of 16 bytes, 16 rows of different residues by 16; of the transposing
+// reads, 4 rows x 64 bytes, which have to fall into different quarters of the banks.  (Permuted
+// by the row's number itself, the transposing reads of neighbouring rows met: 43 % of LDS' cycles.)
+template <int D> struct TileAt {
+    static constexpr int kMask = D % 128 == 0 ? 15 : D % 64 == 0 ? 7 : 3;
+    __device__ __forceinline__ static int at(int row, int col) {
+        const int by = (row >> 2 & 3) | (kMask == 15 ? (row & 3) << 2 : kMask == 7 ? (row & 2) << 1 : 0);
+        return row * D + (((col >> 3) ^ by) << 3) + (col & 7);
+    }
+};
+// A lane's places in such a tile for 32 x 32 products
 template <int D> struct LaneAt32 {
-    static constexpr int kMask = ((D / 8) & -(D / 8)) - 1;  // (tile_at)
-    int row0, col0, col8;
+    static constexpr int kMask = TileAt<D>::kMask;
+    int row0, col0;
     __device__ __forceinline__ LaneAt32() {
         const int lane = threadIdx.x & 63, quarter = lane >> 4, i = lane & 15;
         const int r = 4 * (quarter >> 1) + (i >> 2), c = 16 * (quarter & 1) + 4 * (i & 3);
-        row0 = in_loop(tile_at<D>(lane & 31, 8 * (lane >> 5)));
-        col0 = in_loop(tile_at<D>(r, c));
-        col8 = in_loop(tile_at<D>(r + 8, c));
+        row0 = in_loop(TileAt<D>::at(lane & 31, 8 * (lane >> 5)));
+        col0 = in_loop(TileAt<D>::at(r, c));
     }
+    // The same, of which the compiler knows nothing: the places further along the rows are then
+    // made where they are used, not kept in some 20 registers across the loop.
+    __device__ __forceinline__ LaneAt32(const LaneAt32 &x)
+        : row0(in_loop(x.row0)), col0(in_loop(x.col0)) {}
     __device__ __forceinline__ static int along(int at, int pieces) {
         return (at ^ ((pieces & kMask) << 3)) + ((pieces & ~kMask) << 3);
     }
@@ -184,11 +199,13 @@ __device__ __forceinline__ void frag_col32(const bf16_t *tile, int plane, int s,
     typedef __attribute__((address_space(3))) s4 *lds_s4;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        bf16_t *base = const_cast<bf16_t *>(tile) + (i * plane + 16 * s * D);
-        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s4)(base + LaneAt32<D>::along(at.col0, 4 * t)));
-        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s4)(base + LaneAt32<D>::along(at.col8, 4 * t)));
+        bf16_t *base = const_cast<bf16_t *>(tile) + (i * plane + 16 * s * D) +
+                       LaneAt32<D>::along(at.col0, 4 * t);
+        // (8 rows on: the pieces' permutation differs in its second bit)
+        bf16_t *up = const_cast<bf16_t *>(tile) + (i * plane + (16 * s + 8) * D) +
+                     LaneAt32<D>::along(at.col0 ^ 16, 4 * t);
+        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)base);
+        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)up);
         out[i] = __builtin_bit_cast(bf16x8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     }
 }
@@ -365,7 +382,7 @@ template <typename T, int D, int kRows, int kThreads, bool kWhole> struct TileLo
         constexpr int kPlane = kRows * D;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const int at = tile_at<D>(row_of(s), col_of(s));
+            const int at = TileAt<D>::at(row_of(s), col_of(s));
             if constexpr (sizeof(T) == 2) {
                 *reinterpret_cast<u32x4v *>(tile + at) = raw[s];
             } else {
@@ -479,9 +496,9 @@ __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x
 // x[j] += the rows that read(k, j) gives of step k times operand j, kJobs products side by side.
 // The rows of kAhead steps are on their way from LDS while a step's products run: read where
 // they are used, a wave waited out LDS' latency every two products.
-template <typename T, int D, int kJobs, typename Read, typename Operand>
+template <typename T, int D, int kJobs, int kAhead, typename Read, typename Operand>
 __device__ __forceinline__ void row_products(Read read, Operand operand, floatx16 (&x)[kJobs]) {
-    constexpr int NP = kParts<T>, kSteps = D / 16, kAhead = NP == 1 && kJobs == 1 ? 4 : 2;
+    constexpr int NP = kParts<T>, kSteps = D / 16;
     bf16x8 f[kAhead][kJobs][NP];
 #pragma unroll
     for (int k = 0; k < kAhead && k < kSteps; ++k)
@@ -502,14 +519,15 @@ __device__ __forceinline__ void row_products(Read read, Operand operand, floatx1
 
 // acc[t] += columns 32 t .. + 31 of the tile, transposed, times weights by rows: k-step h takes
 // rows 16 h .. + 15.  First read(), which may lie well before, then add().
-template <typename T, int D, int kRows> struct ColumnProducts {
+// kBuffers: steps that are in registers at once, 2 or 1.
+template <typename T, int D, int kRows, int kBuffers = 2> struct ColumnProducts {
     static constexpr int NP = kParts<T>, kSteps = kRows / 16;
-    bf16x8 f[2][D / 32][NP];
+    bf16x8 f[kBuffers][D / 32][NP];
     // step h of the rows that begin `first` (a multiple of 32) into a tile
     __device__ __forceinline__ void fetch(const bf16_t *tile, int plane, int first,
                                           const LaneAt32<D> &at, int h) {
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) frag_col32<D, NP>(tile, plane, first / 16 + h, t, at, f[h % 2][t]);
+        for (int t = 0; t < D / 32; ++t) frag_col32<D, NP>(tile, plane, first / 16 + h, t, at, f[h % kBuffers][t]);
     }
     __device__ __forceinline__ void read(const bf16_t *tile, int plane, int first,
                                          const LaneAt32<D> &at) {
@@ -522,13 +540,14 @@ template <typename T, int D, int kRows> struct ColumnProducts {
 #pragma clang fp contract(off)
 #pragma unroll
         for (int h = 0; h < kSteps; ++h) {
-            if (h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
+            if (kBuffers == 2 && h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
             bf16x8 w[NP];
             frag_regs<T>(x[h / 2], h % 2, w);
             keep_order();
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) mma32<NP, NP>(f[h % 2][t], w, acc[t]);
+            for (int t = 0; t < D / 32; ++t) mma32<NP, NP>(f[h % kBuffers][t], w, acc[t]);
             keep_order();
+            if (kBuffers == 1 && h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
         }
     }
 };

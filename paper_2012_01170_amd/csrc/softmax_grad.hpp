@@ -16,13 +16,15 @@ constexpr int kGradThreads = 256;
 template <typename T, int D> constexpr int kGradKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
 // Waves a SIMD: the rows' operands and sums of wide heads in float32 fill its registers alone
 template <typename T, int D> constexpr int kGradWaves = sizeof(T) == 4 && D > 32 ? 1 : 2;
-template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) * D > 128 ? 1 : 2;
+template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) == 4 && D > 32 ? 1 : 2;
 
 template <typename T, int D, bool kWhole>
 __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_kernel(SoftmaxArgs p) {
 #pragma clang fp contract(off)
     constexpr int NP = kParts<T>, KB = kGradKeys<T, D>, kSub = KB / 32, kPlane = KB * D;
-    __shared__ __attribute__((aligned(16))) bf16_t kt[NP * kPlane], vt[NP * kPlane];
+    // (one array, so that both tiles are at constant distances from a lane's places)
+    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * kPlane];
+    bf16_t *const kt = lds, *const vt = lds + NP * kPlane;
     const int32_t head_k = blockIdx.x % p.kv_heads;
     const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads;
     const int32_t group = p.group.d;
@@ -100,7 +102,7 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
         sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
                 vbase, p.dv);
     };
-    const LaneAt32<D> at;
+    const LaneAt32<D> places;
     floatx16 acc[D / 32];
     clear(acc);
     if (most > 0) fetch(0);
@@ -114,9 +116,10 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
         if (k0 + KB < most) fetch(k0 + KB);
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
+            const LaneAt32<D> at(places);
             floatx16 w[2];  // scores, and dO v
             clear(w);
-            row_products<T, D, 2>(
+            row_products<T, D, 2, 2>(
                 [&](int k, int j, bf16x8(&f)[NP]) {
                     frag_row32<D, NP>(j ? vt : kt, kPlane, u, k, at, f);
                 },
@@ -150,25 +153,36 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
 // dk and dv: a workgroup has 128 keys of one key head, 32 a wave, and goes through the
 // rows that see them, every p.parts-th tile of rows from the part's own on (p.parts > 1:
 // sums to part_dk and part_dv, which softmax_dkv_join_kernel adds).
-constexpr int kGradCols = 128;
-template <typename T, int D> constexpr int kGradRows = sizeof(T) == 4 && D > 64 ? 32 : 64;
+// Threads of a workgroup, 32 keys a wave: 
+template <typename T, int D> constexpr int kKeyGradThreads = sizeof(T) == 2 && D > 96 ? 512 : 256;
+// Of the workgroup's keys and values, how many are kept in LDS rather than in registers
+#ifndef KK
+#define KK 2
+#endif
+template <typename T, int D> constexpr int kKeptKeys = sizeof(T) == 2 && D > 96 ? KK : 0;
+template <typename T, int D> constexpr int kGradCols = kKeyGradThreads<T, D> / 2;
+template <typename T, int D> constexpr int kGradRows = D > 96 || (sizeof(T) == 4 && D > 64) ? 32 : 64;
 
 template <typename T, int D, bool kWhole>
-__global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
+__global__ __launch_bounds__((kKeyGradThreads<T, D>), (kKeyGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
 #pragma clang fp contract(off)
     constexpr int NP = kParts<T>, RB = kGradRows<T, D>, kSub = RB / 32, kPlane = RB * D;
-    __shared__ __attribute__((aligned(16))) bf16_t qt[NP * kPlane], gt[NP * kPlane];
+    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * kPlane];
+    bf16_t *const qt = lds, *const gt = lds + NP * kPlane;
+    constexpr int kKept = kKeptKeys<T, D> * kGradCols<T, D> * D;
+    __shared__ __attribute__((aligned(16))) bf16_t kept[kKept > 0 ? kKept : 1];
     __shared__ __attribute__((aligned(16))) float lses[RB], deltas[RB];
     __shared__ __attribute__((aligned(16))) int32_t limits[RB];
     const int32_t head_k = blockIdx.x % p.kv_heads;
     const int32_t part = blockIdx.x / p.kv_heads % p.parts;
     const int32_t x = blockIdx.x / p.kv_heads / p.parts;
     const int32_t group = p.group.d;
-    auto begin = [&](int32_t b) { return k_split(p, b) / kGradCols + b; };
+    constexpr int kThreads = kKeyGradThreads<T, D>, kCols = kGradCols<T, D>;
+    auto begin = [&](int32_t b) { return k_split(p, b) / kCols + b; };
     const int32_t b = sequence_of(p.n_batch, x, begin);
     if (b < 0) return;
     const Sequence s = sequence_at<false>(p, b);
-    const int32_t c0 = (x - begin(b)) * kGradCols;
+    const int32_t c0 = (x - begin(b)) * kCols;
     if (c0 >= s.lk) return;
     const int wave = wave_of_block(), lane = threadIdx.x & 63;
     const int32_t wave_key = c0 + 32 * wave, key = wave_key + (lane & 31);
@@ -184,6 +198,16 @@ __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_d
                                       head_k * p.v.head_stride,
                                   there, p.dv, vf);
     }
+    const LaneAt32<D> places;
+    if constexpr (kKept > 0) {  // (each wave reads its own only)
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            *reinterpret_cast<bf16x8 *>(kept + 32 * wave * D + LaneAt32<D>::along(places.row0, 2 * k)) = kf[k][0];
+            if (kKeptKeys<T, D> > 1)
+                *reinterpret_cast<bf16x8 *>(kept + (kCols + 32 * wave) * D +
+                                            LaneAt32<D>::along(places.row0, 2 * k)) = vf[k][0];
+        }
+    }
     // the rows: from the first token that sees key c0 on
     const int32_t rows = s.lq * group;
     int32_t t0 = p.causal ? c0 - (s.lk - s.lq) : 0;
@@ -195,7 +219,7 @@ __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_d
                            (int64_t)head_k * group * p.q.head_stride;
     const T *const gbase = static_cast<const T *>(p.d_o.data) + s.q0 * p.d_o.token_stride +
                            (int64_t)head_k * group * p.d_o.head_stride;
-    TileLoad<T, D, RB, kGradThreads, kWhole> sq, sg;
+    TileLoad<T, D, RB, kThreads, kWhole> sq, sg;
     float next_lse = 0.f, next_delta = 0.f;
     int32_t next_limit = 0;
     if (kWhole && p.even_rows) {
@@ -241,7 +265,6 @@ __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_d
             }
         }
     };
-    const LaneAt32<D> at;
     const int half = lane >> 5;
     floatx16 dk[D / 32], dv[D / 32];
     clear(dk);
@@ -263,16 +286,35 @@ __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_d
         if (r0 + step < rows) fetch(r0 + step);
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
+            const LaneAt32<D> at(places);
             // (limits do not fall along the rows that there are; the others' sums are infinite)
             const int32_t first = __builtin_amdgcn_readfirstlane(limits[32 * u]);
             floatx16 w[2];
             clear(w);
-            row_products<T, D, 2>(
-                [&](int k, int j, bf16x8(&f)[NP]) {
-                    frag_row32<D, NP>(j ? gt : qt, kPlane, u, k, at, f);
-                },
-                [&](int k, int j) -> const bf16x8(&)[NP] { return j ? vf[k] : kf[k]; }, w);
-            ColumnProducts<T, D, 32> grads, queries;
+            if constexpr (kKept > 0) {
+                const bf16_t *const own = kept + 32 * wave * D;
+                bf16x8 f[4][1];
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    frag_row32<D, 1>(qt, kPlane, u, k, at, reinterpret_cast<bf16x8(&)[1]>(f[0]));
+                    frag_row32<D, 1>(own, 0, 0, k, at, reinterpret_cast<bf16x8(&)[1]>(f[1]));
+                    frag_row32<D, 1>(gt, kPlane, u, k, at, reinterpret_cast<bf16x8(&)[1]>(f[2]));
+                    if (kKeptKeys<T, D> > 1)
+                        frag_row32<D, 1>(own + kCols * D, 0, 0, k, at, reinterpret_cast<bf16x8(&)[1]>(f[3]));
+                    mma32<1, 1>(f[0], f[1], w[0]);
+                    if (kKeptKeys<T, D> > 1)
+                        mma32<1, 1>(f[2], f[3], w[1]);
+                    else
+                        mma32<1, 1>(f[2], reinterpret_cast<const bf16x8(&)[1]>(vf[k][0]), w[1]);
+                }
+            } else {
+                row_products<T, D, 2, 2>(
+                    [&](int k, int j, bf16x8(&f)[NP]) {
+                        frag_row32<D, NP>(j ? gt : qt, kPlane, u, k, at, f);
+                    },
+                    [&](int k, int j) -> const bf16x8(&)[NP] { return j ? vf[k] : kf[k]; }, w);
+            }
+            ColumnProducts<T, D, 32, (NP == 1 && D > 96 ? 1 : 2)> grads, queries;
             grads.read(gt, kPlane, 32 * u, at);
             const bool masked = first < wave_key + 32;
 #pragma unroll

@@ -72,8 +72,8 @@ inline SoftmaxArgs softmax_args(const sbc_softmax_attention *a) {
     return p;
 }
 
-// The forward pass takes few rows (32 to a workgroup, keys in parts) where many, 128 to a
-// workgroup, would leave CUs without work or most of their rows empty.
+// The forward pass takes rows 128 to a workgroup, or few rows 32 to one.  Either has the keys
+// in parts where there are not workgroups enough for every CU.
 struct SoftmaxPlan {
     bool few;
     int32_t parts;
@@ -81,19 +81,25 @@ struct SoftmaxPlan {
 };
 // most_keys: of one sequence
 inline SoftmaxPlan softmax_plan(const sbc_softmax_attention *a, int64_t most_keys) {
-    SoftmaxPlan s{false, 1, softmax_places(a, 128) * a->kv_heads};
     const int64_t rows = (int64_t)a->n * (a->heads / a->kv_heads);
     const int cus = device_cus();
-    s.few = rows <= (int64_t)64 * a->n_batch || s.blocks < cus / 2;
-    if (!s.few) return s;
-    const int64_t tiles = softmax_places(a, 32) * a->kv_heads;
-    int64_t parts = ((int64_t)8 * cus + tiles - 1) / tiles;
-    const int64_t most = (most_keys + 127) / 128;  // a round of keys for each
-    if (parts > most) parts = most;
-    if (parts > 64) parts = 64;
-    if (parts < 1) parts = 1;
-    s.parts = (int32_t)parts;
-    s.blocks = tiles * parts;
+    auto plan = [&](bool few, int64_t blocks_a_cu, int64_t least_keys) {
+        const int64_t tiles = softmax_places(a, few ? 32 : 128) * a->kv_heads;
+        int64_t parts = tiles > 0 ? blocks_a_cu * cus / tiles : 1;
+        const int64_t most = (most_keys + least_keys - 1) / least_keys;
+        if (parts > most) parts = most;
+        if (parts > 64) parts = 64;
+        if (parts < 1) parts = 1;
+        return SoftmaxPlan{few, (int32_t)parts, tiles * parts};
+    };
+    const SoftmaxPlan many = plan(false, 3, 256);
+    SoftmaxPlan s = many;
+    if (rows <= (int64_t)64 * a->n_batch || many.blocks < cus) s = plan(true, 8, 256);
+    // (a workgroup of the join for each row)
+    if (s.parts > 1 && (int64_t)a->n * a->heads >= (int64_t)1 << 24) {
+        s.blocks /= s.parts;
+        s.parts = 1;
+    }
     return s;
 }
 inline size_t softmax_workspace(const sbc_softmax_attention *a, const SoftmaxPlan &s) {

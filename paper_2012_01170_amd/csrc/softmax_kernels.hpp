@@ -20,8 +20,8 @@ template <typename T, int D> constexpr int kTileWaves = sizeof(T) == 4 && D > 64
 constexpr int kTileRows = 128;  // of softmax_tile_kernel: 32 a wave
 constexpr int kFewRows = 32;    // of softmax_rows_kernel
 
-// A sequence's keys in p.parts parts for softmax_rows_kernel: as even ones as multiples of 128
-// keys (a round of a workgroup's four waves) allow
+// A sequence's keys in p.parts parts: as even ones as multiples of 128 keys (a round of the
+// four waves of softmax_rows_kernel) allow
 __device__ __forceinline__ int32_t part_keys(int32_t lk, int32_t parts) {
     return (int32_t)(((int64_t)lk + parts - 1) / parts + 127) / 128 * 128;
 }
@@ -36,8 +36,9 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     __shared__ __attribute__((aligned(16))) bf16_t kt[NP * kPlane], vt[NP * kPlane];
     __shared__ int32_t first_bad[D];  // (TileLoad::put_bad_apart)
     const int32_t head_k = blockIdx.x % p.kv_heads;
+    const int32_t part = blockIdx.x / p.kv_heads % p.parts;
     // (from the back: a causal sequence's last tiles are its longest)
-    const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads;
+    const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads / p.parts;
     const int32_t group = p.group.d;
     auto begin = [&](int32_t b) {
         return (int32_t)((int64_t)q_split(p, b) * group / kTileRows) + b;
@@ -59,6 +60,11 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     };
     const int32_t least = __builtin_amdgcn_readfirstlane(limit_of(r0));
     const int32_t most = __builtin_amdgcn_readfirstlane(limit_of(r0 + kTileRows - 1));
+    // the part's keys
+    const int32_t size = p.parts > 1 ? part_keys(s.lk, p.parts) : s.lk;
+    const int32_t first = part * size;
+    const int32_t end = p.parts > 1 && most > first + size ? first + size : most;
+    if (part > 0 && first >= most) return;  // (softmax_join_kernel knows)
     const int32_t wave_least = __builtin_amdgcn_readfirstlane(limit_of(wave_row));
 
     bf16x8 q[D / 16][NP];
@@ -102,11 +108,11 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     if (threadIdx.x < D) first_bad[threadIdx.x] = INT32_MAX;
     __syncthreads();
     constexpr uint64_t kAll = KB == 64 ? ~0ull : 0xFFFFFFFFull;
-    if (most > 0) {
-        if constexpr (kPaged) next_places.template find<KB>(p, s, 0, s.lk);
-        fetch(0);
+    if (first < end) {
+        if constexpr (kPaged) next_places.template find<KB>(p, s, first, s.lk);
+        fetch(first);
     }
-    for (int32_t k0 = 0; k0 < most; k0 += KB) {
+    for (int32_t k0 = first; k0 < end; k0 += KB) {
         __syncthreads();  // the last tile has been read
         sk.settle();
         sv.settle();
@@ -115,7 +121,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
         sv.store(vt);
         const uint64_t known = kPaged ? next_places.there : kAll;
         __syncthreads();
-        if (k0 + KB < most) {
+        if (k0 + KB < end) {
             if constexpr (kPaged) next_places.template find<KB>(p, s, k0 + KB, s.lk);
             fetch(k0 + KB);
         }
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
         for (int u0 = 0; u0 < KB / 32; u0 += kSub) {
             floatx16 x[kSub];
             clear(x);
-            row_products<T, D, kSub>(
+            row_products<T, D, kSub, (NP == 1 && kSub == 1 ? 4 : 2)>(
                 [&](int k, int j, bf16x8(&f)[NP]) { frag_row32<D, NP>(kt, kPlane, u0 + j, k, at, f); },
                 [&](int k, int j) -> const bf16x8(&)[NP] { return q[k]; }, x);
             ColumnProducts<T, D, 32 * kSub> values;
@@ -145,23 +151,33 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     }
     if (!there) return;
     const float l = halves_sum(sums.l);
-    const int64_t place = s.q0 + token;
-    if (p.lse && lane < 32)
-        p.lse[place * p.heads + head] = l == 0.f ? -INFINITY : (sums.m + log2f(l)) * kLn2;
-    T *out = static_cast<T *>(p.o.data) + place * p.o.token_stride + (int64_t)head * p.o.head_stride;
-    const float part = 1.f / l;
+    const int64_t place = s.q0 + token, flat = place * p.heads + head;
+    const int64_t in_part = (int64_t)part * p.n * p.heads + flat;
+    if (lane < 32) {
+        const float lse2 = l == 0.f ? -INFINITY : sums.m + log2f(l);
+        if (p.parts > 1)
+            p.part_lse[in_part] = lse2;
+        else if (p.lse)
+            p.lse[flat] = lse2 * kLn2;
+    }
+    const float scale = 1.f / l;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float y[4];
+            const int c = 32 * t + 8 * j + 4 * (lane >> 5);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int c = 32 * t + 8 * j + 4 * (lane >> 5) + i;
-                y[i] = l == 0.f ? 0.f : sums.o[t][4 * j + i] * part;
-                if (first_bad[c] < limit) y[i] = NAN;
+                y[i] = l == 0.f ? 0.f : sums.o[t][4 * j + i] * scale;
+                if (first_bad[c + i] < limit) y[i] = NAN;
             }
-            put4<T, kWhole>(out, 32 * t + 8 * j + 4 * (lane >> 5), p.dv, y);
+            if (p.parts > 1)
+                put4<float, kWhole>(p.part_o + in_part * p.dv, c, p.dv, y);
+            else
+                put4<T, kWhole>(static_cast<T *>(p.o.data) + place * p.o.token_stride +
+                                    (int64_t)head * p.o.head_stride,
+                                c, p.dv, y);
         }
 }
 
@@ -337,7 +353,7 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
         }
         if (out_row < rows) {
             if (p.parts > 1)
-                put4<float, false>(p.part_o + ((int64_t)part * p.n * p.heads + flat) * p.dv, 32 * t + jc,
+                put4<float, kWhole>(p.part_o + ((int64_t)part * p.n * p.heads + flat) * p.dv, 32 * t + jc,
                                    p.dv, y);
             else
                 put4<T, kWhole>(static_cast<T *>(p.o.data) + place * p.o.token_stride +
@@ -347,38 +363,50 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     }
 }
 
-// The parts' sums joined, a wave a token and head: each part's own softmax weighs by its sum.
-// Only parts that begin before the row's limit have been written.
+// The parts' sums joined, a workgroup a token and head, every fourth part a wave's: each
+// part's own softmax weighs by its sum.  Only parts that begin before the row's limit have been
+// written.  (A wave alone, its 64 parts behind each other, took 15 us where they are 7's work.)
 template <typename T, bool kPaged>
 __global__ __launch_bounds__(256) void softmax_join_kernel(SoftmaxArgs p) {
-    const int64_t flat = (int64_t)blockIdx.x * 4 + wave_of_block();
-    if (flat >= (int64_t)p.n * p.heads) return;
+    __shared__ float sums[4][128];
+    const int64_t flat = blockIdx.x;
     const int32_t token = (int32_t)(flat / p.heads), head = (int32_t)(flat - (int64_t)token * p.heads);
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = wave_of_block();
+    const int64_t stride = (int64_t)p.n * p.heads;
+    const float found = lane < p.parts ? p.part_lse[lane * stride + flat] : 0.f;  // (parts <= 64)
     const int32_t b = sequence_of(p.n_batch, token, [&](int32_t i) { return q_split(p, i); });
     if (b < 0) return;
     const Sequence s = sequence_at<kPaged>(p, b);
     if (token - s.q0 >= s.lq) return;  // behind the last sequence
     const int32_t limit = s.limit(token - s.q0, p.causal), size = part_keys(s.lk, p.parts);
-    const int64_t stride = (int64_t)p.n * p.heads;
-    const bool there = lane < p.parts && (int64_t)lane * size < limit;  // (parts <= 64)
-    const float lse2 = there ? p.part_lse[lane * stride + flat] : -INFINITY;
+    const float lse2 = lane < p.parts && (int64_t)lane * size < limit ? found : -INFINITY;
     float top = lse2;
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
     const float w = lse2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lse2 - top);
     const float total = group_sum<64>(w);
     const int32_t parts = size > 0 ? (limit + size - 1) / size : 0;
-    T *out = static_cast<T *>(p.o.data) + token * p.o.token_stride + (int64_t)head * p.o.head_stride;
-    for (int c0 = 0; c0 < p.dv; c0 += 64) {
-        const int c = c0 + lane < p.dv ? c0 + lane : p.dv - 1;
-        float y = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < parts; ++i)
-            y = fmaf(__shfl(w, i), p.part_o[(i * stride + flat) * p.dv + c], y);
-        if (c0 + lane < p.dv) out[c] = from_f32<T>(total == 0.f ? 0.f : y / total);
+    float y[2] = {0.f, 0.f};
+    const int c = 2 * lane;
+#pragma unroll 8
+    for (int i = wave; i < parts; i += 4) {
+        const float u = __shfl(w, i);
+        float z[2];
+        load_f32<2>(p.part_o + (i * stride + flat) * p.dv + c, p.dv - c, z);
+        y[0] = fmaf(u, z[0], y[0]);
+        y[1] = fmaf(u, z[1], y[1]);
     }
-    if (p.lse && lane == 0) p.lse[flat] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+    sums[wave][c] = y[0];
+    sums[wave][c + 1] = y[1];
+    __syncthreads();
+    if ((int)threadIdx.x < p.dv) {
+        const int i = threadIdx.x;
+        const float sum = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+        static_cast<T *>(p.o.data)[token * p.o.token_stride + (int64_t)head * p.o.head_stride + i] =
+            from_f32<T>(total == 0.f ? 0.f : sum / total);
+    }
+    if (p.lse && threadIdx.x == 0)
+        p.lse[flat] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
 }  // namespace sbc

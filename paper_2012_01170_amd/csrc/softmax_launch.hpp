@@ -37,9 +37,8 @@ sbc_status softmax_forward(SoftmaxArgs p, const sbc_softmax_attention *a, const 
     if (plan.parts > 1) {
         trace_before("softmax_join", stream);
         const int64_t rows = (int64_t)a->n * a->heads;
-        if (rows >= (int64_t)1 << 26) return fail(SBC_ERR_UNSUPPORTED, "n * heads in parts must be below 2^26");
-        hipLaunchKernelGGL((softmax_join_kernel<T, kPaged>), dim3((unsigned)((rows + 3) / 4)),
-                           dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((softmax_join_kernel<T, kPaged>), dim3((unsigned)rows), dim3(256), 0, stream,
+                           p);
         SBC_LAUNCH_CHECK();
         trace_after("softmax_join", stream);
     }
