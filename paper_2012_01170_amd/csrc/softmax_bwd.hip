@@ -6,12 +6,8 @@ namespace sbc {
 namespace {
 
 // Parts of the rows for dk and dv: as many as give every CU two workgroups
-int32_t grad_cols(const sbc_softmax_attention *a) {
-    const int32_t d = a->dk > a->dv ? a->dk : a->dv;
-    return a->dtype == SBC_F32 ? kGradCols<float, 128> : d > 96 ? kGradCols<bf16_t, 128> : kGradCols<bf16_t, 64>;
-}
 int32_t grad_parts(const sbc_softmax_attention *a) {
-    const int64_t tiles = ((int64_t)a->m / grad_cols(a) + a->n_batch) * a->kv_heads;
+    const int64_t tiles = ((int64_t)a->m / kGradCols + a->n_batch) * a->kv_heads;
     const int64_t rows = (int64_t)a->n * (a->heads / a->kv_heads) / (a->n_batch > 0 ? a->n_batch : 1);
     int64_t parts = ((int64_t)3 * device_cus() + tiles - 1) / (tiles > 0 ? tiles : 1);
     if (parts > rows / 128) parts = rows / 128;
@@ -32,10 +28,10 @@ void carve(const sbc_softmax_attention *a, void *workspace, SoftmaxArgs *p, size
 template <typename T, bool kWhole>
 sbc_status backward(SoftmaxArgs p, const sbc_softmax_attention *a, hipStream_t stream) {
     const int64_t dq_blocks = softmax_places(a, 128) * a->kv_heads;
-    const int64_t cols = (int64_t)a->m / grad_cols(a) + a->n_batch;
+    const int64_t cols = (int64_t)a->m / kGradCols + a->n_batch;
     const int64_t dkv_blocks = cols * a->kv_heads * p.parts;
     const int64_t join = ((int64_t)a->m * a->kv_heads * ((a->dk > a->dv ? a->dk : a->dv) + 3) / 4 + 255) / 256 + 1;
-    if (dq_blocks >= (int64_t)1 << 24 || dkv_blocks >= (int64_t)1 << 24 ||
+    if (dq_blocks >= (int64_t)1 << 24 || dkv_blocks >= (int64_t)1 << 23 ||
         (p.parts > 1 && join >= (int64_t)1 << 24))
         return fail(SBC_ERR_UNSUPPORTED, "more than 2^24 workgroups needed");
     softmax_dispatch(a->dk > a->dv ? a->dk : a->dv, [&](auto d) {
@@ -56,8 +52,9 @@ sbc_status backward(SoftmaxArgs p, const sbc_softmax_attention *a, hipStream_t s
                 if (x->token_stride >= 1 << 22 || x->head_stride > ((int64_t)1 << 28) / group)
                     p.even_rows = 0;
             trace_before("softmax_dkv", stream);
-            hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole>), dim3((unsigned)dkv_blocks),
-                               dim3(kKeyGradThreads<T, D>), 0, stream, p);
+            hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole>),
+                               dim3((unsigned)(dkv_blocks * (kGradsApart<T, D> ? 2 : 1))),
+                               dim3(kGradThreads), 0, stream, p);
             trace_after("softmax_dkv", stream);
         }
     });

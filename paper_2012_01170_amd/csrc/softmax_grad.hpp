@@ -15,8 +15,8 @@ constexpr int kGradThreads = 256;
 // dq: a workgroup has 128 rows, 32 a wave, as softmax_tile_kernel.
 template <typename T, int D> constexpr int kGradKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
 // Waves a SIMD: the rows' operands and sums of wide heads in float32 fill its registers alone
-template <typename T, int D> constexpr int kGradWaves = sizeof(T) == 4 && D > 32 ? 1 : 2;
-template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) == 4 && D > 32 ? 1 : 2;
+template <typename T, int D> constexpr int kGradWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
+template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
 
 template <typename T, int D, bool kWhole>
 __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_kernel(SoftmaxArgs p) {
@@ -153,36 +153,41 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
 // dk and dv: a workgroup has 128 keys of one key head, 32 a wave, and goes through the
 // rows that see them, every p.parts-th tile of rows from the part's own on (p.parts > 1:
 // sums to part_dk and part_dv, which softmax_dkv_join_kernel adds).
-// Threads of a workgroup, 32 keys a wave: 
-template <typename T, int D> constexpr int kKeyGradThreads = sizeof(T) == 2 && D > 96 ? 512 : 256;
-// Of the workgroup's keys and values, how many are kept in LDS rather than in registers
-#ifndef KK
-#define KK 2
-#endif
-template <typename T, int D> constexpr int kKeptKeys = sizeof(T) == 2 && D > 96 ? KK : 0;
-template <typename T, int D> constexpr int kGradCols = kKeyGradThreads<T, D> / 2;
-template <typename T, int D> constexpr int kGradRows = D > 96 || (sizeof(T) == 4 && D > 64) ? 32 : 64;
+//
+// Where both sums and operands fit into half of a SIMD's registers, a workgroup makes both
+// (kDk | kDv); else one half of the workgroups makes dk and the other dv, scores twice: a wave alone on
+// its SIMD, without another's products to fill its waits, took longer (16384 tokens, 2 key heads
+// of 128 bf16 channels: 1760 us against GRADSPLIT).
+constexpr int kGradCols = 128;
+constexpr int kDk = 1, kDv = 2;
+template <typename T, int D> constexpr int kGradRows = D > 64 || (sizeof(T) == 4 && D > 32) ? (D == 96 ? 64 : 32) : 64;
+template <typename T, int D> constexpr bool kGradsApart = sizeof(T) * D > 128;
 
-template <typename T, int D, bool kWhole>
-__global__ __launch_bounds__((kKeyGradThreads<T, D>), (kKeyGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
+template <typename T, int D> struct KeyGradShared {
+    static constexpr int NP = kParts<T>, RB = kGradRows<T, D>;
+    alignas(16) bf16_t tiles[2 * NP * RB * D];
+    alignas(16) float lses[RB], deltas[RB];
+    alignas(16) int32_t limits[RB];
+};
+
+template <typename T, int D, bool kWhole, int kGrads>
+__device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
+                                          KeyGradShared<T, D> &lds) {
 #pragma clang fp contract(off)
     constexpr int NP = kParts<T>, RB = kGradRows<T, D>, kSub = RB / 32, kPlane = RB * D;
-    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * kPlane];
-    bf16_t *const qt = lds, *const gt = lds + NP * kPlane;
-    constexpr int kKept = kKeptKeys<T, D> * kGradCols<T, D> * D;
-    __shared__ __attribute__((aligned(16))) bf16_t kept[kKept > 0 ? kKept : 1];
-    __shared__ __attribute__((aligned(16))) float lses[RB], deltas[RB];
-    __shared__ __attribute__((aligned(16))) int32_t limits[RB];
-    const int32_t head_k = blockIdx.x % p.kv_heads;
-    const int32_t part = blockIdx.x / p.kv_heads % p.parts;
-    const int32_t x = blockIdx.x / p.kv_heads / p.parts;
+    constexpr bool kDoK = kGrads & kDk, kDoV = kGrads & kDv;
+    bf16_t *const qt = lds.tiles, *const gt = lds.tiles + NP * kPlane;
+    float *const lses = lds.lses, *const deltas = lds.deltas;
+    int32_t *const limits = lds.limits;
+    const int32_t head_k = block % p.kv_heads;
+    const int32_t part = block / p.kv_heads % p.parts;
+    const int32_t x = block / p.kv_heads / p.parts;
     const int32_t group = p.group.d;
-    constexpr int kThreads = kKeyGradThreads<T, D>, kCols = kGradCols<T, D>;
-    auto begin = [&](int32_t b) { return k_split(p, b) / kCols + b; };
+    auto begin = [&](int32_t b) { return k_split(p, b) / kGradCols + b; };
     const int32_t b = sequence_of(p.n_batch, x, begin);
     if (b < 0) return;
     const Sequence s = sequence_at<false>(p, b);
-    const int32_t c0 = (x - begin(b)) * kCols;
+    const int32_t c0 = (x - begin(b)) * kGradCols;
     if (c0 >= s.lk) return;
     const int wave = wave_of_block(), lane = threadIdx.x & 63;
     const int32_t wave_key = c0 + 32 * wave, key = wave_key + (lane & 31);
@@ -194,19 +199,10 @@ __global__ __launch_bounds__((kKeyGradThreads<T, D>), (kKeyGradWaves<T, D>)) voi
         row_operand<T, D, kWhole>(static_cast<const T *>(p.k.data) + at * p.k.token_stride +
                                       head_k * p.k.head_stride,
                                   there, p.dk, kf);
-        row_operand<T, D, kWhole>(static_cast<const T *>(p.v.data) + at * p.v.token_stride +
-                                      head_k * p.v.head_stride,
-                                  there, p.dv, vf);
-    }
-    const LaneAt32<D> places;
-    if constexpr (kKept > 0) {  // (each wave reads its own only)
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            *reinterpret_cast<bf16x8 *>(kept + 32 * wave * D + LaneAt32<D>::along(places.row0, 2 * k)) = kf[k][0];
-            if (kKeptKeys<T, D> > 1)
-                *reinterpret_cast<bf16x8 *>(kept + (kCols + 32 * wave) * D +
-                                            LaneAt32<D>::along(places.row0, 2 * k)) = vf[k][0];
-        }
+        if constexpr (kDoK)
+            row_operand<T, D, kWhole>(static_cast<const T *>(p.v.data) + at * p.v.token_stride +
+                                          head_k * p.v.head_stride,
+                                      there, p.dv, vf);
     }
     // the rows: from the first token that sees key c0 on
     const int32_t rows = s.lq * group;
@@ -219,7 +215,7 @@ __global__ __launch_bounds__((kKeyGradThreads<T, D>), (kKeyGradWaves<T, D>)) voi
                            (int64_t)head_k * group * p.q.head_stride;
     const T *const gbase = static_cast<const T *>(p.d_o.data) + s.q0 * p.d_o.token_stride +
                            (int64_t)head_k * group * p.d_o.head_stride;
-    TileLoad<T, D, RB, kThreads, kWhole> sq, sg;
+    TileLoad<T, D, RB, kGradThreads, kWhole> sq, sg;
     float next_lse = 0.f, next_delta = 0.f;
     int32_t next_limit = 0;
     if (kWhole && p.even_rows) {
@@ -265,6 +261,7 @@ __global__ __launch_bounds__((kKeyGradThreads<T, D>), (kKeyGradWaves<T, D>)) voi
             }
         }
     };
+    const LaneAt32<D> places;
     const int half = lane >> 5;
     floatx16 dk[D / 32], dv[D / 32];
     clear(dk);
@@ -289,82 +286,84 @@ __global__ __launch_bounds__((kKeyGradThreads<T, D>), (kKeyGradWaves<T, D>)) voi
             const LaneAt32<D> at(places);
             // (limits do not fall along the rows that there are; the others' sums are infinite)
             const int32_t first = __builtin_amdgcn_readfirstlane(limits[32 * u]);
-            floatx16 w[2];
+            floatx16 w[kDoK ? 2 : 1];  // scores, and dO v
             clear(w);
-            if constexpr (kKept > 0) {
-                const bf16_t *const own = kept + 32 * wave * D;
-                bf16x8 f[4][1];
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    frag_row32<D, 1>(qt, kPlane, u, k, at, reinterpret_cast<bf16x8(&)[1]>(f[0]));
-                    frag_row32<D, 1>(own, 0, 0, k, at, reinterpret_cast<bf16x8(&)[1]>(f[1]));
-                    frag_row32<D, 1>(gt, kPlane, u, k, at, reinterpret_cast<bf16x8(&)[1]>(f[2]));
-                    if (kKeptKeys<T, D> > 1)
-                        frag_row32<D, 1>(own + kCols * D, 0, 0, k, at, reinterpret_cast<bf16x8(&)[1]>(f[3]));
-                    mma32<1, 1>(f[0], f[1], w[0]);
-                    if (kKeptKeys<T, D> > 1)
-                        mma32<1, 1>(f[2], f[3], w[1]);
-                    else
-                        mma32<1, 1>(f[2], reinterpret_cast<const bf16x8(&)[1]>(vf[k][0]), w[1]);
-                }
-            } else {
-                row_products<T, D, 2, 2>(
-                    [&](int k, int j, bf16x8(&f)[NP]) {
-                        frag_row32<D, NP>(j ? gt : qt, kPlane, u, k, at, f);
-                    },
-                    [&](int k, int j) -> const bf16x8(&)[NP] { return j ? vf[k] : kf[k]; }, w);
-            }
-            ColumnProducts<T, D, 32, (NP == 1 && D > 96 ? 1 : 2)> grads, queries;
-            grads.read(gt, kPlane, 32 * u, at);
+            row_products<T, D, (kDoK ? 2 : 1), (NP == 1 && !kDoK ? 4 : 2)>(
+                [&](int k, int j, bf16x8(&f)[NP]) {
+                    frag_row32<D, NP>(j ? gt : qt, kPlane, u, k, at, f);
+                },
+                [&](int k, int j) -> const bf16x8(&)[NP] { return j ? vf[k] : kf[k]; }, w);
+            ColumnProducts<T, D, 32, (NP == 3 ? 1 : 2)> grads, queries;
+            if constexpr (kDoV) grads.read(gt, kPlane, 32 * u, at);
+            else queries.read(qt, kPlane, 32 * u, at);
             const bool masked = first < wave_key + 32;
+            floatx16 e[1], ds[1];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int r = 32 * u + 8 * j + 4 * half;
                 const floatx4 lse4 = *reinterpret_cast<const floatx4 *>(lses + r);
-                const floatx4 delta4 = *reinterpret_cast<const floatx4 *>(deltas + r);
-                typedef int32_t i4 __attribute__((ext_vector_type(4)));
-                i4 limit4{0, 0, 0, 0};
-                if (masked) limit4 = *reinterpret_cast<const i4 *>(limits + r);
+                floatx4 delta4{0.f, 0.f, 0.f, 0.f};
+                if (kDoK) delta4 = *reinterpret_cast<const floatx4 *>(deltas + r);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(w[0][4 * j + i], p.scale2, -lse4[i]));
-                    const float d = e * (w[1][4 * j + i] - delta4[i]);
-                    const bool ok = !masked || key < limit4[i];
-                    w[0][4 * j + i] = ok ? e : 0.f;
-                    w[1][4 * j + i] = ok ? d : 0.f;
+                    e[0][4 * j + i] = __builtin_amdgcn_exp2f(fmaf(w[0][4 * j + i], p.scale2, -lse4[i]));
+                    if constexpr (kDoK) ds[0][4 * j + i] = e[0][4 * j + i] * (w[1][4 * j + i] - delta4[i]);
                 }
             }
-            grads.add(reinterpret_cast<const floatx16(&)[1]>(w[0]), gt, kPlane, 32 * u, at, dv);
-            queries.read(qt, kPlane, 32 * u, at);
-            queries.add(reinterpret_cast<const floatx16(&)[1]>(w[1]), qt, kPlane, 32 * u, at, dk);
+            if (masked) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool ok = key < limits[32 * u + 8 * j + 4 * half + i];
+                        if constexpr (kDoV) e[0][4 * j + i] = ok ? e[0][4 * j + i] : 0.f;
+                        if constexpr (kDoK) ds[0][4 * j + i] = ok ? ds[0][4 * j + i] : 0.f;
+                    }
+            }
+            if constexpr (kDoV) grads.add(e, gt, kPlane, 32 * u, at, dv);
+            if constexpr (kDoK) {
+                if constexpr (kDoV) queries.read(qt, kPlane, 32 * u, at);
+                queries.add(ds, qt, kPlane, 32 * u, at, dk);
+            }
         }
     }
     if (!there) return;
     const int64_t place = s.k0 + key;
     const int64_t flat = ((int64_t)part * p.m + place) * p.kv_heads + head_k;
+    auto put = [&](const floatx16(&acc)[D / 32], float scale, float *parts, const sbc_heads &out,
+                   int32_t d) {
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+        for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = 32 * t + 8 * j + 4 * half;
-            float y[4], z[4];
+            for (int j = 0; j < 4; ++j) {
+                const int c = 32 * t + 8 * j + 4 * half;
+                float y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                y[i] = dk[t][4 * j + i] * p.scale;
-                z[i] = dv[t][4 * j + i];
+                for (int i = 0; i < 4; ++i) y[i] = acc[t][4 * j + i] * scale;
+                if (p.parts > 1)
+                    put4<float, kWhole>(parts + flat * d, c, d, y);
+                else
+                    put4<T, kWhole>(static_cast<T *>(out.data) + place * out.token_stride +
+                                        head_k * out.head_stride,
+                                    c, d, y);
             }
-            if (p.parts > 1) {
-                put4<float, false>(p.part_dk + flat * p.dk, c, p.dk, y);
-                put4<float, false>(p.part_dv + flat * p.dv, c, p.dv, z);
-            } else {
-                put4<T, kWhole>(static_cast<T *>(p.dk_out.data) + place * p.dk_out.token_stride +
-                                    head_k * p.dk_out.head_stride,
-                                c, p.dk, y);
-                put4<T, kWhole>(static_cast<T *>(p.dv_out.data) + place * p.dv_out.token_stride +
-                                    head_k * p.dv_out.head_stride,
-                                c, p.dv, z);
-            }
-        }
+    };
+    if constexpr (kDoK) put(dk, p.scale, p.part_dk, p.dk_out, p.dk);
+    if constexpr (kDoV) put(dv, 1.f, p.part_dv, p.dv_out, p.dv);
+}
+
+template <typename T, int D, bool kWhole>
+__global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
+    __shared__ KeyGradShared<T, D> lds;
+    if constexpr (kGradsApart<T, D>) {
+        const int32_t half = gridDim.x / 2;  // (dk first: it takes longer)
+        if ((int32_t)blockIdx.x < half)
+            key_grads<T, D, kWhole, kDk>(p, blockIdx.x, lds);
+        else
+            key_grads<T, D, kWhole, kDv>(p, blockIdx.x - half, lds);
+    } else {
+        key_grads<T, D, kWhole, kDk | kDv>(p, blockIdx.x, lds);
+    }
 }
 
 // The parts' sums of dk (blockIdx.y 0) and dv (1), in the parts' order; keys that lie in no
