@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendArgs a) {
 using namespace sbc;
 
 extern "C" size_t sbc_cache_slots_workspace_size(int32_t n_batch) {
-    if (n_batch <= kFew) return 256;
+    if (n_batch <= kFew) return 0;
     Carver c(nullptr);
     c.take<int32_t>(n_batch);
     c.take<int32_t>((size_t)n_batch + 1);
@@ -204,7 +204,8 @@ extern "C" sbc_status sbc_cache_slots(const int32_t *lengths, const int32_t *spl
                         {region(lengths, n_batch, 4), region(splits, (int64_t)n_batch + 1, 4),
                          region(free_pages, n_free, 4)}));
     SBC_TRY(check_apart({others[0], others[1], others[2]}, {from}));
-    if (!workspace || workspace_bytes < sbc_cache_slots_workspace_size(n_batch))
+    const size_t bytes = sbc_cache_slots_workspace_size(n_batch);
+    if (bytes > 0 && (!workspace || workspace_bytes < bytes))
         return fail(SBC_ERR_WORKSPACE, "workspace smaller than sbc_cache_slots_workspace_size()");
     SlotArgs a{lengths, splits, n, n_batch, width, n_free, divisor(page), divisor(width > 0 ? width : 1),
                table, free_pages, table_out, slots, lengths_out, needed, nullptr, nullptr};

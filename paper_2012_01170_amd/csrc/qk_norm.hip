@@ -10,13 +10,15 @@
 //   dw = sum over tokens and heads of g x rstd,  dx = rstd (g w - x rstd^2 mean(g w x)).
 // A lane's part of dw stays in registers over its tokens; a workgroup adds its lanes' in LDS,
 // and a second kernel the workgroups', both in a fixed order.
+#include <type_traits>
+
 #include "rotary.hpp"
 
 namespace sbc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostBlocks = 512;  // of the backward pass: rows of the weights' partial sums
+constexpr int kMostBlocks = 1024;  // of the backward pass: rows of the weights' partial sums
 
 struct QkNormArgs {
     sbc_heads in[2], out[2], dy[2];
@@ -34,19 +36,6 @@ struct QkNormArgs {
     float *dw[2];
     int32_t blocks;
 };
-
-// Sum over groups of `lanes` neighbours
-__device__ __forceinline__ float lanes_sum(float x, int lanes) {
-    switch (lanes) {
-        case 1: return x;
-        case 2: return group_sum<2>(x);
-        case 4: return group_sum<4>(x);
-        case 8: return group_sum<8>(x);
-        case 16: return group_sum<16>(x);
-        case 32: return group_sum<32>(x);
-        default: return group_sum<64>(x);
-    }
-}
 
 // What a lane has of a token: its vectors' first channels and how many of each exist
 template <typename T, bool kInterleaved> struct LaneChannels {
@@ -107,25 +96,36 @@ __device__ __forceinline__ T *head_at(const sbc_heads (&x)[2], const int32_t (&h
     return static_cast<T *>(x[w].data) + i * x[w].token_stride + h * x[w].head_stride;
 }
 
-template <typename T, bool kInterleaved>
+// Raw vectors of a head on their way
+template <typename T, bool kInterleaved> struct HeadLoad {
+    using L = LaneChannels<T, kInterleaved>;
+    raw16 raw[L::kVecs];
+    __device__ __forceinline__ void load(const T *from, const L &lane) {
+#pragma unroll
+        for (int w = 0; w < L::kVecs; ++w) raw[w] = load_raw16<T>(from + lane.c[w], lane.width[w]);
+    }
+    __device__ __forceinline__ void get(float (&x)[L::kVecs][L::V]) const {
+#pragma unroll
+        for (int w = 0; w < L::kVecs; ++w) unpack<T>(raw[w], x[w]);
+    }
+};
+
+// kLanes of a token.  (The next kBatch heads are on their way while a batch is computed.)
+template <typename T, bool kInterleaved, int kLanes>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
     using L = LaneChannels<T, kInterleaved>;
     constexpr int V = L::V, N = L::N, kVecs = L::kVecs, kBatch = kInterleaved ? 4 : 2;
     const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t i = at / a.lanes;
-    const int unit = (int)(at & (a.lanes - 1));
+    const int64_t i = at / kLanes;
+    const int unit = (int)(at & (kLanes - 1));
     if (i >= a.n) return;  // (all lanes of a token)
     const L lane(a, unit);
     const int total = a.heads[0] + a.heads[1];
-    float x[kBatch][kVecs][V];
+    HeadLoad<T, kInterleaved> next[kBatch];
     auto fetch = [&](int j0) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
-            if (j0 + u < total) {
-                const T *from = head_at<T>(a.in, a.heads, i, j0 + u);
-#pragma unroll
-                for (int w = 0; w < kVecs; ++w) load_vec<T>(from + lane.c[w], lane.width[w], x[u][w]);
-            }
+            if (j0 + u < total) next[u].load(head_at<T>(a.in, a.heads, i, j0 + u), lane);
     };
     fetch(0);
     float weight[2][kVecs][V];
@@ -141,7 +141,10 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
     lane.turns(a, i, 1.f, cs, sn);
     const float per = 1.f / a.d;
     for (int j0 = 0; j0 < total; j0 += kBatch) {
-        if (j0 > 0) fetch(j0);
+        float x[kBatch][kVecs][V];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) next[u].get(x[u]);
+        if (j0 + kBatch < total) fetch(j0 + kBatch);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
             if (j0 + u < total) {
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
                 for (int w = 0; w < kVecs; ++w)
 #pragma unroll
                     for (int e = 0; e < V; ++e) square = fmaf(x[u][w][e], x[u][w][e], square);
-                square = lanes_sum(square, a.lanes);
+                square = group_sum<kLanes>(square);
                 const float rstd = 1.f / sqrtf(fmaf(square, per, a.eps));
                 const bool keys = j0 + u >= a.heads[0];
 #pragma unroll
@@ -166,13 +169,13 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
     }
 }
 
-template <typename T, bool kInterleaved>
+template <typename T, bool kInterleaved, int kLanes>
 __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
     using L = LaneChannels<T, kInterleaved>;
     constexpr int V = L::V, N = L::N, kVecs = L::kVecs;
     __shared__ float sums[kThreads * kVecs * V];
-    const int groups = kThreads / a.lanes, group = threadIdx.x / a.lanes;
-    const int unit = threadIdx.x & (a.lanes - 1);
+    constexpr int kGroups = kThreads / kLanes;
+    const int group = threadIdx.x / kLanes, unit = threadIdx.x & (kLanes - 1);
     const L lane(a, unit);
     float weight[2][kVecs][V], dw[2][kVecs][V];
 #pragma unroll
@@ -187,23 +190,29 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
             if (a.weight[y]) load_f32<V>(a.weight[y] + lane.c[w], lane.width[w], weight[y][w]);
         }
     const float per = 1.f / a.d;
-    for (int64_t i = (int64_t)blockIdx.x * groups + group; i < a.n; i += (int64_t)gridDim.x * groups) {
+    for (int64_t i = (int64_t)blockIdx.x * kGroups + group; i < a.n; i += (int64_t)gridDim.x * kGroups) {
         float cs[N], sn[N];
+        HeadLoad<T, kInterleaved> next_x, next_g;
+        auto fetch = [&](int y, int h) {
+            next_x.load(static_cast<const T *>(a.in[y].data) + i * a.in[y].token_stride +
+                            h * a.in[y].head_stride,
+                        lane);
+            next_g.load(static_cast<const T *>(a.dy[y].data) + i * a.dy[y].token_stride +
+                            h * a.dy[y].head_stride,
+                        lane);
+        };
+        fetch(a.heads[0] > 0 ? 0 : 1, 0);
         lane.turns(a, i, -1.f, cs, sn);
 #pragma unroll
         for (int y = 0; y < 2; ++y)
-#pragma unroll 2
             for (int h = 0; h < a.heads[y]; ++h) {
                 float x[kVecs][V], g[kVecs][V];
-                const T *from = static_cast<const T *>(a.in[y].data) + i * a.in[y].token_stride +
-                                h * a.in[y].head_stride;
-                const T *dy = static_cast<const T *>(a.dy[y].data) + i * a.dy[y].token_stride +
-                              h * a.dy[y].head_stride;
-#pragma unroll
-                for (int w = 0; w < kVecs; ++w) {
-                    load_vec<T>(from + lane.c[w], lane.width[w], x[w]);
-                    load_vec<T>(dy + lane.c[w], lane.width[w], g[w]);
-                }
+                next_x.get(x);
+                next_g.get(g);
+                if (h + 1 < a.heads[y])
+                    fetch(y, h + 1);
+                else if (y == 0 && a.heads[1] > 0)
+                    fetch(1, 0);
                 lane.turn(g, cs, sn);
                 float square = 0.f, dot = 0.f;
 #pragma unroll
@@ -213,8 +222,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
                         square = fmaf(x[w][e], x[w][e], square);
                         dot = fmaf(g[w][e] * weight[y][w][e], x[w][e], dot);
                     }
-                square = lanes_sum(square, a.lanes);
-                dot = lanes_sum(dot, a.lanes);
+                square = group_sum<kLanes>(square);
+                dot = group_sum<kLanes>(dot);
                 const float rstd = 1.f / sqrtf(fmaf(square, per, a.eps));
                 const float back = dot * per * rstd * rstd;
 #pragma unroll
@@ -244,7 +253,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
         __syncthreads();
         for (int c = threadIdx.x; c < a.d; c += kThreads) {
             float s = 0.f;
-            for (int g = 0; g < groups; ++g) s += sums[g * a.d + c];
+#pragma unroll 8
+            for (int g = 0; g < kGroups; ++g) s += sums[g * a.d + c];
             a.partial[((int64_t)blockIdx.x * 2 + y) * a.d + c] = s;
         }
     }
@@ -270,14 +280,22 @@ __global__ __launch_bounds__(kThreads) void qk_norm_reduce_kernel(QkNormArgs a) 
     }
 }
 
-template <typename F> void dispatch(sbc_dtype dtype, bool interleaved, F f) {
-    if (dtype == SBC_F32) {
-        if (interleaved) f(float{}, std::true_type{});
-        else f(float{}, std::false_type{});
-    } else {
-        if (interleaved) f(bf16_t{}, std::true_type{});
-        else f(bf16_t{}, std::false_type{});
-    }
+template <typename F> void dispatch(sbc_dtype dtype, bool interleaved, int32_t lanes, F f) {
+    auto by_lanes = [&](auto t, auto inter) {
+        switch (lanes) {
+            case 1: return f(t, inter, std::integral_constant<int, 1>{});
+            case 2: return f(t, inter, std::integral_constant<int, 2>{});
+            case 4: return f(t, inter, std::integral_constant<int, 4>{});
+            case 8: return f(t, inter, std::integral_constant<int, 8>{});
+            case 16: return f(t, inter, std::integral_constant<int, 16>{});
+            case 32: return f(t, inter, std::integral_constant<int, 32>{});
+            default: return f(t, inter, std::integral_constant<int, 64>{});
+        }
+    };
+    if (dtype == SBC_F32)
+        interleaved ? by_lanes(float{}, std::true_type{}) : by_lanes(float{}, std::false_type{});
+    else
+        interleaved ? by_lanes(bf16_t{}, std::true_type{}) : by_lanes(bf16_t{}, std::false_type{});
 }
 
 int32_t grad_blocks(int32_t n, int32_t lanes) {
@@ -364,8 +382,8 @@ extern "C" sbc_status sbc_qk_norm_rotary_forward(
                          region(plan->freqs, a.pairs, 4), region(q_weight, d, 4),
                          region(k_weight, d, 4)}));
     trace_before("qk_norm_fwd", stream);
-    dispatch(dtype, plan->interleaved, [&](auto t, auto inter) {
-        hipLaunchKernelGGL((qk_norm_kernel<decltype(t), decltype(inter)::value>),
+    dispatch(dtype, plan->interleaved, a.lanes, [&](auto t, auto inter, auto lanes) {
+        hipLaunchKernelGGL((qk_norm_kernel<decltype(t), decltype(inter)::value, decltype(lanes)::value>),
                            dim3((unsigned)grid_for((int64_t)n * a.lanes, kThreads)), dim3(kThreads), 0,
                            stream, a);
     });
@@ -423,8 +441,8 @@ extern "C" sbc_status sbc_qk_norm_rotary_backward(
     a.blocks = work ? grad_blocks(n, a.lanes) : 0;
     if (work) {
         trace_before("qk_norm_bwd", stream);
-        dispatch(dtype, plan->interleaved, [&](auto t, auto inter) {
-            hipLaunchKernelGGL((qk_norm_grad_kernel<decltype(t), decltype(inter)::value>),
+        dispatch(dtype, plan->interleaved, a.lanes, [&](auto t, auto inter, auto lanes) {
+            hipLaunchKernelGGL((qk_norm_grad_kernel<decltype(t), decltype(inter)::value, decltype(lanes)::value>),
                                dim3((unsigned)a.blocks), dim3(kThreads), 0, stream, a);
         });
         SBC_LAUNCH_CHECK();

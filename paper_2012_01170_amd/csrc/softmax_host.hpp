@@ -94,7 +94,7 @@ inline SoftmaxPlan softmax_plan(const sbc_softmax_attention *a, int64_t most_key
     };
     const SoftmaxPlan many = plan(false, 3, 256);
     SoftmaxPlan s = many;
-    if (rows <= (int64_t)64 * a->n_batch || many.blocks < cus) s = plan(true, 8, 256);
+    if (rows <= (int64_t)64 * a->n_batch || many.blocks < cus) s = plan(true, 4, 256);
     // (a workgroup of the join for each row)
     if (s.parts > 1 && (int64_t)a->n * a->heads >= (int64_t)1 << 24) {
         s.blocks /= s.parts;
@@ -103,7 +103,7 @@ inline SoftmaxPlan softmax_plan(const sbc_softmax_attention *a, int64_t most_key
     return s;
 }
 inline size_t softmax_workspace(const sbc_softmax_attention *a, const SoftmaxPlan &s) {
-    if (s.parts <= 1) return 256;
+    if (s.parts <= 1) return 0;
     Carver c(nullptr);
     c.take<float>((size_t)s.parts * a->n * a->heads * a->dv);
     c.take<float>((size_t)s.parts * a->n * a->heads);

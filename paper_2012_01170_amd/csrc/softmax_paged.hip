@@ -54,7 +54,8 @@ extern "C" sbc_status sbc_softmax_attention_paged(const sbc_softmax_attention *a
                          region(table, (int64_t)a->n_batch * width, 4), region(lengths, a->n_batch, 4),
                          region(a->splits, (int64_t)a->n_batch + 1, 4)}));
     const SoftmaxPlan plan = softmax_plan(a, most_keys(page, width));
-    if (!workspace || workspace_bytes < softmax_workspace(a, plan))
+    const size_t needed = softmax_workspace(a, plan);
+    if (needed > 0 && (!workspace || workspace_bytes < needed))
         return fail(SBC_ERR_WORKSPACE,
                     "workspace smaller than sbc_softmax_attention_paged_workspace_size()");
     SoftmaxArgs p = softmax_args(a);

@@ -66,6 +66,15 @@ def _heads(t: Optional[torch.Tensor]):
     return ctypes.byref(L.SbcHeads(t.data_ptr(), s[0], s[1]))
 
 
+class _NoWorkspace:
+    ptr, nbytes = None, 0
+
+
+def _scratch(nbytes, device):
+    """A workspace, if any is needed."""
+    return _Workspace(nbytes, device) if nbytes else _NoWorkspace
+
+
 # ---------------------------------------------------------------- layer norm
 def _norm_common(x, weight):
     _first(x, "x", 2)
@@ -412,7 +421,7 @@ def softmax_attention_forward(q, k, v, splits: Optional[torch.Tensor] = None,
     o = torch.empty((a.n, a.heads, a.dv), dtype=q.dtype, device=dev)
     lse = torch.empty((a.n, a.heads), dtype=torch.float32, device=dev)
     lib, ref = L.lib(), ctypes.byref(a)
-    ws = _Workspace(lib.sbc_softmax_attention_workspace_size(ref), dev)
+    ws = _scratch(lib.sbc_softmax_attention_workspace_size(ref), dev)
     L.check(lib.sbc_softmax_attention_forward(ref, _heads(q), _heads(k), _heads(v), _heads(o),
                                               lse.data_ptr(), ws.ptr, ws.nbytes, _stream(index)))
     return o, lse
@@ -489,7 +498,7 @@ def softmax_attention_paged(q, k_pages, v_pages, table, lengths,
                               dk ** -0.5 if scale is None else float(scale), 1, _ptr(splits), None)
     o = torch.empty((n, H, dv), dtype=q.dtype, device=dev)
     lib, ref = L.lib(), ctypes.byref(a)
-    ws = _Workspace(lib.sbc_softmax_attention_paged_workspace_size(ref, page, width), dev)
+    ws = _scratch(lib.sbc_softmax_attention_paged_workspace_size(ref, page, width), dev)
     L.check(lib.sbc_softmax_attention_paged(
         ref, _heads(q), _pages(k_pages), _pages(v_pages), n_pages, page, table.data_ptr(), width,
         lengths.data_ptr(), _heads(o), None, ws.ptr, ws.nbytes, _stream(index)))
@@ -532,7 +541,7 @@ def cache_slots(lengths, table, free, page: int, splits: Optional[torch.Tensor] 
     after = torch.empty_like(lengths)
     needed = torch.empty(1, dtype=torch.int32, device=dev)
     lib = L.lib()
-    ws = _Workspace(lib.sbc_cache_slots_workspace_size(n_batch), dev)
+    ws = _scratch(lib.sbc_cache_slots_workspace_size(n_batch), dev)
     L.check(lib.sbc_cache_slots(lengths.data_ptr(), _ptr(splits), n, n_batch, table.data_ptr(),
                                 width, int(page), free.data_ptr(), free.numel(),
                                 out_table.data_ptr(), slots.data_ptr(), after.data_ptr(),

@@ -145,7 +145,7 @@ def _soft_bwd(lib, at, wsb=1 << 24, **kw):
     (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(dk=129), UNSUPPORTED), (dict(dv=129), UNSUPPORTED), (dict(splits=None), INVALID),
     (dict(k_splits=None), INVALID), (dict(heads=65536), UNSUPPORTED),
-    (dict(n=1 << 30), UNSUPPORTED), (dict(m=1 << 30), UNSUPPORTED), (dict(wsb=8), WORKSPACE),
+    (dict(n=1 << 30), UNSUPPORTED), (dict(m=1 << 30), UNSUPPORTED), (dict(wsb=8, n=2, m=4000), WORKSPACE),
 ])
 def test_attention_refusals(lib, call, kw, status):
     assert call(lib, _soft_at(), **kw) == status and lib.sbc_last_error() != b""
@@ -173,13 +173,13 @@ def test_attention_workspaces(lib):
     at = _soft_at()
     for f in (lib.sbc_softmax_attention_workspace_size,
               lib.sbc_softmax_attention_backward_workspace_size):
-        assert f(None) == 0 and f(_soft(at, dk=129)) == 0 and f(_soft(at)) > 0
+        assert f(None) == 0 and f(_soft(at, dk=129)) == 0
         for n in (1, 1000, 100_000):  # no scores are kept
             size = f(_soft(at, n=n, m=n, heads=8, kv_heads=8, dk=64, dv=64))
-            assert 0 < size <= (1 << 25) + 40 * n * 8 * 128 * 4
+            assert 0 <= size <= (1 << 25) + 40 * n * 8 * 128 * 4
     f = lib.sbc_softmax_attention_paged_workspace_size
     assert f(_soft(at), 0, 4) == 0 and f(_soft(at), 16, -1) == 0
-    assert 0 < f(_soft(at, n=1, n_batch=1), 16, 0) <= f(_soft(at, n=1, n_batch=1), 16, 10_000)
+    assert 0 == f(_soft(at, n=1, n_batch=1), 16, 0) < f(_soft(at, n=1, n_batch=1), 16, 10_000)
     assert f(_soft(at, n=1, n_batch=1), 1 << 30, 1 << 30) > 0
 
 
@@ -214,7 +214,8 @@ def _cache_at(case=None):
 @pytest.mark.parametrize("kw,status", [
     (dict(n_pages=-1), INVALID), (dict(page=0), INVALID), (dict(width=-1), INVALID),
     (dict(splits=None), INVALID), (dict(n_batch=0), INVALID), (dict(scale=0.0), INVALID),
-    (dict(k_stride=(-1, 32, 16)), INVALID), (dict(dk=200), UNSUPPORTED), (dict(wsb=8), WORKSPACE),
+    (dict(k_stride=(-1, 32, 16)), INVALID), (dict(dk=200), UNSUPPORTED),
+    (dict(wsb=8, width=1000), WORKSPACE),
     (dict(n=0), 0),
 ])
 def test_paged_refusals(lib, kw, status):
@@ -245,7 +246,7 @@ def _slots(lib, case=None, n=9, n_batch=5, width=WIDTH, page=PAGE, n_free=4, wsb
 @pytest.mark.parametrize("kw,status", [
     (dict(n=-1), INVALID), (dict(n_batch=-1), INVALID), (dict(width=-1), INVALID),
     (dict(page=0), INVALID), (dict(n_free=-1), INVALID), (dict(case=("splits", None)), INVALID),
-    (dict(width=1 << 30), UNSUPPORTED), (dict(wsb=0), WORKSPACE), (dict(case=("ws", None)), WORKSPACE),
+    (dict(width=1 << 30), UNSUPPORTED), (dict(n_batch=5000, case=("ws", None)), WORKSPACE),
     (dict(n_batch=5000, wsb=256), WORKSPACE),
 ])
 def test_cache_slots_refusals(lib, kw, status):
