@@ -18,7 +18,7 @@ namespace sbc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostBlocks = 1024;  // of the backward pass: rows of the weights' partial sums
+constexpr int kMostBlocks = 768;  // of the backward pass: rows of the weights' partial sums
 
 struct QkNormArgs {
     sbc_heads in[2], out[2], dy[2];
@@ -97,21 +97,43 @@ __device__ __forceinline__ T *head_at(const sbc_heads (&x)[2], const int32_t (&h
 }
 
 // Raw vectors of a head on their way
-template <typename T, bool kInterleaved> struct HeadLoad {
+// (kEven: a lane's vectors are whole or none, and no branch lies between the loads)
+template <typename T, bool kInterleaved, bool kEven> struct HeadLoad {
     using L = LaneChannels<T, kInterleaved>;
     raw16 raw[L::kVecs];
     __device__ __forceinline__ void load(const T *from, const L &lane) {
 #pragma unroll
-        for (int w = 0; w < L::kVecs; ++w) raw[w] = load_raw16<T>(from + lane.c[w], lane.width[w]);
+        for (int w = 0; w < L::kVecs; ++w) {
+            if constexpr (kEven)
+                __builtin_memcpy(&raw[w], from + (lane.width[w] > 0 ? lane.c[w] : 0), 16);
+            else
+                raw[w] = load_raw16<T>(from + lane.c[w], lane.width[w]);
+        }
     }
-    __device__ __forceinline__ void get(float (&x)[L::kVecs][L::V]) const {
+    __device__ __forceinline__ void get(const L &lane, float (&x)[L::kVecs][L::V]) const {
 #pragma unroll
-        for (int w = 0; w < L::kVecs; ++w) unpack<T>(raw[w], x[w]);
+        for (int w = 0; w < L::kVecs; ++w) {
+            unpack<T>(raw[w], x[w]);
+            if constexpr (kEven) {
+#pragma unroll
+                for (int e = 0; e < L::V; ++e) x[w][e] = lane.width[w] > 0 ? x[w][e] : 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ static void put(T *to, const L &lane, const float (&x)[L::kVecs][L::V]) {
+#pragma unroll
+        for (int w = 0; w < L::kVecs; ++w) {
+            if constexpr (kEven) {
+                if (lane.width[w] > 0) store_vec<T>(to + lane.c[w], L::V, x[w]);
+            } else {
+                store_vec<T>(to + lane.c[w], lane.width[w], x[w]);
+            }
+        }
     }
 };
 
 // kLanes of a token.  (The next kBatch heads are on their way while a batch is computed.)
-template <typename T, bool kInterleaved, int kLanes>
+template <typename T, bool kInterleaved, bool kEven, int kLanes>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
     using L = LaneChannels<T, kInterleaved>;
     constexpr int V = L::V, N = L::N, kVecs = L::kVecs, kBatch = kInterleaved ? 4 : 2;
@@ -121,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
     if (i >= a.n) return;  // (all lanes of a token)
     const L lane(a, unit);
     const int total = a.heads[0] + a.heads[1];
-    HeadLoad<T, kInterleaved> next[kBatch];
+    HeadLoad<T, kInterleaved, kEven> next[kBatch];
     auto fetch = [&](int j0) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
@@ -143,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
     for (int j0 = 0; j0 < total; j0 += kBatch) {
         float x[kBatch][kVecs][V];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) next[u].get(x[u]);
+        for (int u = 0; u < kBatch; ++u) next[u].get(lane, x[u]);
         if (j0 + kBatch < total) fetch(j0 + kBatch);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
@@ -163,13 +185,12 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkNormArgs a) {
                         x[u][w][e] *= rstd * (keys ? weight[1][w][e] : weight[0][w][e]);
                 lane.turn(x[u], cs, sn);
                 T *to = head_at<T>(a.out, a.heads, i, j0 + u);
-#pragma unroll
-                for (int w = 0; w < kVecs; ++w) store_vec<T>(to + lane.c[w], lane.width[w], x[u][w]);
+                HeadLoad<T, kInterleaved, kEven>::put(to, lane, x[u]);
             }
     }
 }
 
-template <typename T, bool kInterleaved, int kLanes>
+template <typename T, bool kInterleaved, bool kEven, int kLanes>
 __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
     using L = LaneChannels<T, kInterleaved>;
     constexpr int V = L::V, N = L::N, kVecs = L::kVecs;
@@ -192,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
     const float per = 1.f / a.d;
     for (int64_t i = (int64_t)blockIdx.x * kGroups + group; i < a.n; i += (int64_t)gridDim.x * kGroups) {
         float cs[N], sn[N];
-        HeadLoad<T, kInterleaved> next_x, next_g;
+        HeadLoad<T, kInterleaved, kEven> next_x, next_g;
         auto fetch = [&](int y, int h) {
             next_x.load(static_cast<const T *>(a.in[y].data) + i * a.in[y].token_stride +
                             h * a.in[y].head_stride,
@@ -207,8 +228,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
         for (int y = 0; y < 2; ++y)
             for (int h = 0; h < a.heads[y]; ++h) {
                 float x[kVecs][V], g[kVecs][V];
-                next_x.get(x);
-                next_g.get(g);
+                next_x.get(lane, x);
+                next_g.get(lane, g);
                 if (h + 1 < a.heads[y])
                     fetch(y, h + 1);
                 else if (y == 0 && a.heads[1] > 0)
@@ -236,8 +257,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
                     }
                 T *to = static_cast<T *>(a.out[y].data) + i * a.out[y].token_stride +
                         h * a.out[y].head_stride;
-#pragma unroll
-                for (int w = 0; w < kVecs; ++w) store_vec<T>(to + lane.c[w], lane.width[w], x[w]);
+                HeadLoad<T, kInterleaved, kEven>::put(to, lane, x);
             }
     }
     if (!a.partial) return;
@@ -280,22 +300,28 @@ __global__ __launch_bounds__(kThreads) void qk_norm_reduce_kernel(QkNormArgs a) 
     }
 }
 
-template <typename F> void dispatch(sbc_dtype dtype, bool interleaved, int32_t lanes, F f) {
-    auto by_lanes = [&](auto t, auto inter) {
-        switch (lanes) {
-            case 1: return f(t, inter, std::integral_constant<int, 1>{});
-            case 2: return f(t, inter, std::integral_constant<int, 2>{});
-            case 4: return f(t, inter, std::integral_constant<int, 4>{});
-            case 8: return f(t, inter, std::integral_constant<int, 8>{});
-            case 16: return f(t, inter, std::integral_constant<int, 16>{});
-            case 32: return f(t, inter, std::integral_constant<int, 32>{});
-            default: return f(t, inter, std::integral_constant<int, 64>{});
-        }
+template <typename T, bool kInterleaved, typename F> void dispatch_lanes(const QkNormArgs &a, F f) {
+    using L = LaneChannels<T, kInterleaved>;
+    const bool even = a.pairs % L::N == 0 && (a.d - 2 * a.pairs) % L::V == 0;
+    auto by_even = [&](auto lanes) {
+        even ? f(T{}, std::bool_constant<kInterleaved>{}, std::true_type{}, lanes)
+             : f(T{}, std::bool_constant<kInterleaved>{}, std::false_type{}, lanes);
     };
+    switch (a.lanes) {
+        case 1: return by_even(std::integral_constant<int, 1>{});
+        case 2: return by_even(std::integral_constant<int, 2>{});
+        case 4: return by_even(std::integral_constant<int, 4>{});
+        case 8: return by_even(std::integral_constant<int, 8>{});
+        case 16: return by_even(std::integral_constant<int, 16>{});
+        case 32: return by_even(std::integral_constant<int, 32>{});
+        default: return by_even(std::integral_constant<int, 64>{});
+    }
+}
+template <typename F> void dispatch(sbc_dtype dtype, bool interleaved, const QkNormArgs &a, F f) {
     if (dtype == SBC_F32)
-        interleaved ? by_lanes(float{}, std::true_type{}) : by_lanes(float{}, std::false_type{});
+        interleaved ? dispatch_lanes<float, true>(a, f) : dispatch_lanes<float, false>(a, f);
     else
-        interleaved ? by_lanes(bf16_t{}, std::true_type{}) : by_lanes(bf16_t{}, std::false_type{});
+        interleaved ? dispatch_lanes<bf16_t, true>(a, f) : dispatch_lanes<bf16_t, false>(a, f);
 }
 
 int32_t grad_blocks(int32_t n, int32_t lanes) {
@@ -382,8 +408,9 @@ extern "C" sbc_status sbc_qk_norm_rotary_forward(
                          region(plan->freqs, a.pairs, 4), region(q_weight, d, 4),
                          region(k_weight, d, 4)}));
     trace_before("qk_norm_fwd", stream);
-    dispatch(dtype, plan->interleaved, a.lanes, [&](auto t, auto inter, auto lanes) {
-        hipLaunchKernelGGL((qk_norm_kernel<decltype(t), decltype(inter)::value, decltype(lanes)::value>),
+    dispatch(dtype, plan->interleaved, a, [&](auto t, auto inter, auto even, auto lanes) {
+        hipLaunchKernelGGL((qk_norm_kernel<decltype(t), decltype(inter)::value, decltype(even)::value,
+                            decltype(lanes)::value>),
                            dim3((unsigned)grid_for((int64_t)n * a.lanes, kThreads)), dim3(kThreads), 0,
                            stream, a);
     });
@@ -441,8 +468,9 @@ extern "C" sbc_status sbc_qk_norm_rotary_backward(
     a.blocks = work ? grad_blocks(n, a.lanes) : 0;
     if (work) {
         trace_before("qk_norm_bwd", stream);
-        dispatch(dtype, plan->interleaved, a.lanes, [&](auto t, auto inter, auto lanes) {
-            hipLaunchKernelGGL((qk_norm_grad_kernel<decltype(t), decltype(inter)::value, decltype(lanes)::value>),
+        dispatch(dtype, plan->interleaved, a, [&](auto t, auto inter, auto even, auto lanes) {
+            hipLaunchKernelGGL((qk_norm_grad_kernel<decltype(t), decltype(inter)::value, decltype(even)::value,
+                            decltype(lanes)::value>),
                                dim3((unsigned)a.blocks), dim3(kThreads), 0, stream, a);
         });
         SBC_LAUNCH_CHECK();

@@ -409,22 +409,25 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Where the keys of a tile lie: lane j looks up key first + j (j below kKeys).
+// Where the keys of a tile lie: lane j looks up key first + j (j below kKeys), with look() well
+// before settle().
 struct KeyPlaces {
     int32_t page, at;  // -1: no such key
     uint64_t there;    // a bit for each key of the tile
     template <int kKeys>
-    __device__ __forceinline__ void find(const SoftmaxArgs &p, const Sequence &s, int32_t first,
+    __device__ __forceinline__ void look(const SoftmaxArgs &p, const Sequence &s, int32_t first,
                                          int32_t end) {
-        const int32_t j = threadIdx.x & (kKeys - 1), key = first + j;
+        const int32_t key = first + (int32_t)(threadIdx.x & (kKeys - 1));
         page = -1;
         at = 0;
         if (key < end) {
             const int32_t i = divide(key, p.pages.page);
             at = key - i * (int32_t)p.pages.page.d;
             page = p.pages.table[(int64_t)s.b * p.pages.width + i];
-            if (page < 0 || page >= p.pages.n_pages) page = -1;
         }
+    }
+    template <int kKeys> __device__ __forceinline__ void settle(const SoftmaxArgs &p) {
+        if ((uint32_t)page >= (uint32_t)p.pages.n_pages) page = -1;
         there = __ballot(page >= 0);
         if constexpr (kKeys == 32) there &= 0xFFFFFFFFull;
     }

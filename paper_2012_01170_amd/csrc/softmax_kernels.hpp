@@ -81,12 +81,17 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
         kbase = static_cast<const T *>(p.k.data) + s.k0 * p.k.token_stride + head_k * p.k.head_stride;
         vbase = static_cast<const T *>(p.v.data) + s.k0 * p.v.token_stride + head_k * p.v.head_stride;
     }
+    constexpr uint64_t kAll = KB == 64 ? ~0ull : 0xFFFFFFFFull;
     TileLoad<T, D, KB, kSoftmaxThreads, kWhole> sk, sv;
-    KeyPlaces next_places;
+    KeyPlaces where;  // of the tile that is fetched next
+    uint64_t known = kAll, next_known = kAll;
     auto fetch = [&](int32_t k0) {
         if constexpr (kPaged) {
-            sk.load([&](int r) { return next_places.row<T>(p.pages.k, head_k, r); }, kbase, p.dk);
-            sv.load([&](int r) { return next_places.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
+            where.template settle<KB>(p);
+            sk.load([&](int r) { return where.row<T>(p.pages.k, head_k, r); }, kbase, p.dk);
+            sv.load([&](int r) { return where.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
+            next_known = where.there;
+            where.template look<KB>(p, s, k0 + KB, s.lk);
         } else {
             if (kWhole && k0 + KB <= s.lk) {
                 sk.load_all(kbase + k0 * p.k.token_stride);
@@ -107,9 +112,8 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     RowSums<D> sums;
     if (threadIdx.x < D) first_bad[threadIdx.x] = INT32_MAX;
     __syncthreads();
-    constexpr uint64_t kAll = KB == 64 ? ~0ull : 0xFFFFFFFFull;
     if (first < end) {
-        if constexpr (kPaged) next_places.template find<KB>(p, s, first, s.lk);
+        if constexpr (kPaged) where.template look<KB>(p, s, first, s.lk);
         fetch(first);
     }
     for (int32_t k0 = first; k0 < end; k0 += KB) {
@@ -119,12 +123,9 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
         if (k0 + KB > least) sv.put_bad_apart(k0, first_bad);
         sk.store(kt);
         sv.store(vt);
-        const uint64_t known = kPaged ? next_places.there : kAll;
+        known = next_known;
         __syncthreads();
-        if (k0 + KB < end) {
-            if constexpr (kPaged) next_places.template find<KB>(p, s, k0 + KB, s.lk);
-            fetch(k0 + KB);
-        }
+        if (k0 + KB < end) fetch(k0 + KB);
         // (tiles that hold nothing for this wave, behind the diagonal, are gone through as well: with a
         // branch around them the sums were copied from registers to registers in every tile)
 #pragma unroll
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
 // and the waves' sums are joined at the end.  Memory bounds it where a row or few meet a long cache:
 // the next 32 keys and values are always on their way.
 template <typename T, int D, bool kWhole, bool kPaged>
-__global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxArgs p) {
+__global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_rows_kernel(SoftmaxArgs p) {
     constexpr int NP = kParts<T>, kPlane = 32 * D;
     constexpr int kJoin = 4 * 32 * 36 * 2;  // (bf16 elements of [4][32][36] float32)
     constexpr int kTiles = 4 * NP * kPlane;
@@ -238,47 +239,54 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     }
     u32x4v kraw[D / 16][8 / kVec<T>];
     TileLoad<T, D, 32, 64, kWhole> sv;
-    KeyPlaces next_places;
+    KeyPlaces where;  // of the keys that are fetched next
+    uint64_t known = 0xFFFFFFFFull, next_known = known;
     auto fetch = [&](int32_t k0) {
         if constexpr (kPaged) {
-            const T *at = next_places.row<T>(p.pages.k, head_k, lane & 31);
+            where.template settle<32>(p);
+            const T *at = where.row<T>(p.pages.k, head_k, lane & 31);
             load_row<T, D, kWhole>(at ? at : kbase, at != nullptr, p.dk, kraw);
-            sv.load([&](int r) { return next_places.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
+            sv.load([&](int r) { return where.row<T>(p.pages.v, head_k, r); }, vbase, p.dv);
+            next_known = where.there;
+            where.template look<32>(p, s, k0 + 128, s.lk);
         } else {
             const int32_t key = k0 + (lane & 31);
             const bool ok = key < s.lk;
             load_row<T, D, kWhole>(kbase + (ok ? key : 0) * p.k.token_stride, ok, p.dk, kraw);
-            sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
-                    vbase, p.dv);
+            if (kWhole && k0 + 32 <= s.lk)
+                sv.load_all(vbase + k0 * p.v.token_stride);
+            else
+                sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
+                        vbase, p.dv);
         }
     };
-    const LaneAt32<D> at;
+    if (kWhole && !kPaged) sv.places(p.v.token_stride, p.dv);
+    const LaneAt32<D> lane_at;
     RowSums<D> sums;
     bf16_t *const vt = lds + wave * NP * kPlane;
     if (threadIdx.x < D) first_bad[threadIdx.x] = INT32_MAX;
     __syncthreads();
     int32_t k0 = first + 32 * wave;
     if (k0 < end) {
-        if constexpr (kPaged) next_places.template find<32>(p, s, k0, s.lk);
+        if constexpr (kPaged) where.template look<32>(p, s, k0, s.lk);
         fetch(k0);
     }
     for (; k0 < end; k0 += 128) {
-        bf16x8 kf[D / 16][NP];
+        const LaneAt32<D> at(lane_at);
+        floatx16 w[1];
+        clear(w);
         settle_row<T, D, kWhole>(true, p.dk, kraw);  // (scores of keys that are not there are hidden)
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) raw_parts<T>(kraw[k], kf[k]);
+        for (int k = 0; k < D / 16; ++k) {
+            bf16x8 f[NP];
+            raw_parts<T>(kraw[k], f);
+            mma32<NP, NP>(f, q[k], w[0]);
+        }
         sv.settle();
         if (k0 + 32 > least) sv.put_bad_apart(k0, first_bad);
         sv.store(vt);
-        const uint64_t known = kPaged ? next_places.there : 0xFFFFFFFFull;
-        if (k0 + 128 < end) {
-            if constexpr (kPaged) next_places.template find<32>(p, s, k0 + 128, s.lk);
-            fetch(k0 + 128);
-        }
-        floatx16 w[1];
-        clear(w);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) mma32<NP, NP>(kf[k], q[k], w[0]);
+        known = next_known;
+        if (k0 + 128 < end) fetch(k0 + 128);
         const int32_t visible = limit < end ? limit : end;
         const uint32_t seen = seen_bits(known, 0, visible - k0);
 #pragma unroll
@@ -363,22 +371,27 @@ __global__ __launch_bounds__(kSoftmaxThreads) void softmax_rows_kernel(SoftmaxAr
     }
 }
 
-// The parts' sums joined, a workgroup a token and head, every fourth part a wave's: each
-// part's own softmax weighs by its sum.  Only parts that begin before the row's limit have been
-// written.  (A wave alone, its 64 parts behind each other, took 15 us where they are 7's work.)
-template <typename T, bool kPaged>
+// The parts' sums joined, kAcross waves a token and head, each of them every kAcross-th part:
+// each part's own softmax weighs by its sum.  Only parts that begin before the row's limit have been
+// written.  Few parts take a wave (12984 rows of 4: 10 us, 24 with four waves each), many
+// four (8 rows of 63: 4 us, 15 with one).
+template <typename T, bool kPaged, int kAcross>
 __global__ __launch_bounds__(256) void softmax_join_kernel(SoftmaxArgs p) {
+    constexpr int kRows = 4 / kAcross;
     __shared__ float sums[4][128];
-    const int64_t flat = blockIdx.x;
-    const int32_t token = (int32_t)(flat / p.heads), head = (int32_t)(flat - (int64_t)token * p.heads);
-    const int lane = threadIdx.x & 63, wave = wave_of_block();
+    const int lane = threadIdx.x & 63, wave = wave_of_block(), across = wave % kAcross;
     const int64_t stride = (int64_t)p.n * p.heads;
-    const float found = lane < p.parts ? p.part_lse[lane * stride + flat] : 0.f;  // (parts <= 64)
+    const int64_t flat = (int64_t)blockIdx.x * kRows + wave / kAcross;
+    const bool row = flat < stride;
+    const int32_t token = row ? (int32_t)(flat / p.heads) : 0;
+    const int32_t head = row ? (int32_t)(flat - (int64_t)token * p.heads) : 0;
+    const float found = row && lane < p.parts ? p.part_lse[lane * stride + flat] : 0.f;  // (parts <= 64)
     const int32_t b = sequence_of(p.n_batch, token, [&](int32_t i) { return q_split(p, i); });
-    if (b < 0) return;
-    const Sequence s = sequence_at<kPaged>(p, b);
-    if (token - s.q0 >= s.lq) return;  // behind the last sequence
-    const int32_t limit = s.limit(token - s.q0, p.causal), size = part_keys(s.lk, p.parts);
+    Sequence s{};
+    if (b >= 0) s = sequence_at<kPaged>(p, b);
+    const bool there = row && b >= 0 && token - s.q0 < s.lq;  // (not behind the last sequence)
+    const int32_t limit = there ? s.limit(token - s.q0, p.causal) : 0;
+    const int32_t size = part_keys(s.lk, p.parts);
     const float lse2 = lane < p.parts && (int64_t)lane * size < limit ? found : -INFINITY;
     float top = lse2;
 #pragma unroll
@@ -389,24 +402,29 @@ __global__ __launch_bounds__(256) void softmax_join_kernel(SoftmaxArgs p) {
     float y[2] = {0.f, 0.f};
     const int c = 2 * lane;
 #pragma unroll 8
-    for (int i = wave; i < parts; i += 4) {
+    for (int i = across; i < parts; i += kAcross) {
         const float u = __shfl(w, i);
         float z[2];
         load_f32<2>(p.part_o + (i * stride + flat) * p.dv + c, p.dv - c, z);
         y[0] = fmaf(u, z[0], y[0]);
         y[1] = fmaf(u, z[1], y[1]);
     }
-    sums[wave][c] = y[0];
-    sums[wave][c + 1] = y[1];
-    __syncthreads();
-    if ((int)threadIdx.x < p.dv) {
-        const int i = threadIdx.x;
-        const float sum = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
-        static_cast<T *>(p.o.data)[token * p.o.token_stride + (int64_t)head * p.o.head_stride + i] =
-            from_f32<T>(total == 0.f ? 0.f : sum / total);
+    if constexpr (kAcross > 1) {
+        sums[wave][c] = y[0];
+        sums[wave][c + 1] = y[1];
+        __syncthreads();
+        if (across > 0) return;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            y[e] = (sums[wave][c + e] + sums[wave + 1][c + e]) +
+                   (sums[wave + 2][c + e] + sums[wave + 3][c + e]);
     }
-    if (p.lse && threadIdx.x == 0)
-        p.lse[flat] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+    if (!there) return;
+    T *out = static_cast<T *>(p.o.data) + token * p.o.token_stride + (int64_t)head * p.o.head_stride;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (c + e < p.dv) out[c + e] = from_f32<T>(total == 0.f ? 0.f : y[e] / total);
+    if (p.lse && lane == 0) p.lse[flat] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
 }  // namespace sbc

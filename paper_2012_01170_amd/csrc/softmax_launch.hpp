@@ -37,8 +37,12 @@ sbc_status softmax_forward(SoftmaxArgs p, const sbc_softmax_attention *a, const 
     if (plan.parts > 1) {
         trace_before("softmax_join", stream);
         const int64_t rows = (int64_t)a->n * a->heads;
-        hipLaunchKernelGGL((softmax_join_kernel<T, kPaged>), dim3((unsigned)rows), dim3(256), 0, stream,
-                           p);
+        if (plan.parts > 8)
+            hipLaunchKernelGGL((softmax_join_kernel<T, kPaged, 4>), dim3((unsigned)rows), dim3(256), 0,
+                               stream, p);
+        else
+            hipLaunchKernelGGL((softmax_join_kernel<T, kPaged, 1>), dim3((unsigned)((rows + 3) / 4)),
+                               dim3(256), 0, stream, p);
         SBC_LAUNCH_CHECK();
         trace_after("softmax_join", stream);
     }
