@@ -20,7 +20,7 @@ const char *kKernelNames =
     "decay_dot,decay_fused,decay_dw_reduce,sample_count,sample,lif_sort,lif_cells,lif_emit,stream_lists,stream_gather,stream_gemm,"
     "stream_update,norm_fwd,norm_bwd,norm_reduce,rotary,attn_state,attn_scan,attn_fwd,attn_bwd_state,"
     "attn_bwd,attn_rates,attn_step,qk_norm_fwd,qk_norm_bwd,qk_norm_reduce,softmax_fwd,softmax_join,"
-    "softmax_dq,softmax_dkv,softmax_dkv_join,cache_slots,cache_append";
+    "softmax_grads,softmax_dq,softmax_dkv,softmax_dkv_join,cache_slots,cache_append";
 }  // namespace
 
 void trace_before(const char *name, hipStream_t stream) {

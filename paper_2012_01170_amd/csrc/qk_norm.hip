@@ -260,7 +260,6 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
                 HeadLoad<T, kInterleaved, kEven>::put(to, lane, x);
             }
     }
-    if (!a.partial) return;
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
         if (!a.dw[y]) continue;
@@ -275,7 +274,10 @@ __global__ __launch_bounds__(kThreads) void qk_norm_grad_kernel(QkNormArgs a) {
             float s = 0.f;
 #pragma unroll 8
             for (int g = 0; g < kGroups; ++g) s += sums[g * a.d + c];
-            a.partial[((int64_t)blockIdx.x * 2 + y) * a.d + c] = s;
+            if (gridDim.x == 1)
+                a.dw[y][c] = s;  // (nothing to add it to)
+            else
+                a.partial[((int64_t)blockIdx.x * 2 + y) * a.d + c] = s;
         }
     }
 }
@@ -476,7 +478,7 @@ extern "C" sbc_status sbc_qk_norm_rotary_backward(
         SBC_LAUNCH_CHECK();
         trace_after("qk_norm_bwd", stream);
     }
-    if (sums) {
+    if (sums && a.blocks != 1) {
         trace_before("qk_norm_reduce", stream);
         hipLaunchKernelGGL(qk_norm_reduce_kernel, dim3((unsigned)((d + 15) / 16), 2), dim3(kThreads),
                            0, stream, a);

@@ -2,6 +2,7 @@
 #include "softmax_grad.hpp"
 #include "softmax_host.hpp"
 
+
 namespace sbc {
 namespace {
 
@@ -14,10 +15,15 @@ int32_t grad_parts(const sbc_softmax_attention *a) {
     if (parts > 16) parts = 16;
     return parts < 1 ? 1 : (int32_t)parts;
 }
+// One launch for all: while its workgroups are few
+bool grads_joint(const sbc_softmax_attention *a) {
+    const int64_t rows = softmax_places(a, 128), keys = (int64_t)a->m / kGradCols + a->n_batch;
+    return a->n > 0 && a->m > 0 && (rows + 2 * keys * grad_parts(a)) * a->kv_heads <= 2 * device_cus();
+}
 void carve(const sbc_softmax_attention *a, void *workspace, SoftmaxArgs *p, size_t *used) {
     Carver c(workspace);
     p->parts = grad_parts(a);
-    p->delta = c.take<float>((size_t)a->n * a->heads);
+    if (!grads_joint(a)) p->delta = c.take<float>((size_t)a->n * a->heads);
     if (p->parts > 1) {
         p->part_dk = c.take<float>((size_t)p->parts * a->m * a->kv_heads * a->dk);
         p->part_dv = c.take<float>((size_t)p->parts * a->m * a->kv_heads * a->dv);
@@ -36,25 +42,34 @@ sbc_status backward(SoftmaxArgs p, const sbc_softmax_attention *a, hipStream_t s
         return fail(SBC_ERR_UNSUPPORTED, "more than 2^24 workgroups needed");
     softmax_dispatch(a->dk > a->dv ? a->dk : a->dv, [&](auto d) {
         constexpr int D = decltype(d)::value;
+        constexpr int kRows = kGradRows<T, D>;
+        const int32_t group = a->heads / a->kv_heads;
+        p.even_rows = kRows % group == 0;
+        for (const sbc_heads *x : {&p.q, &p.d_o})
+            if (x->token_stride >= 1 << 22 || x->head_stride > ((int64_t)1 << 28) / group)
+                p.even_rows = 0;
+        const int32_t dkv_kinds = kGradsApart<T, D> ? 2 : 1;
+        p.slots = (int32_t)softmax_places(a, 128);  // (of rows)
+        if (grads_joint(a)) {
+            trace_before("softmax_grads", stream);
+            hipLaunchKernelGGL((softmax_grads_kernel<T, D, kWhole>),
+                               dim3((unsigned)(dq_blocks + dkv_blocks * dkv_kinds)),
+                               dim3(kGradThreads), 0, stream, p, (int32_t)dq_blocks,
+                               (int32_t)dkv_blocks);
+            trace_after("softmax_grads", stream);
+            return;
+        }
         if (a->n > 0) {
-            p.slots = (int32_t)softmax_places(a, 128);
             trace_before("softmax_dq", stream);
             hipLaunchKernelGGL((softmax_dq_kernel<T, D, kWhole>), dim3((unsigned)dq_blocks),
                                dim3(kGradThreads), 0, stream, p);
             trace_after("softmax_dq", stream);
         }
         if (a->m > 0) {
-            p.slots = (int32_t)cols;
-            constexpr int kRows = kGradRows<T, D>;
-            const int32_t group = a->heads / a->kv_heads;
-            p.even_rows = kRows % group == 0;
-            for (const sbc_heads *x : {&p.q, &p.d_o})
-                if (x->token_stride >= 1 << 22 || x->head_stride > ((int64_t)1 << 28) / group)
-                    p.even_rows = 0;
             trace_before("softmax_dkv", stream);
             hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole>),
-                               dim3((unsigned)(dkv_blocks * (kGradsApart<T, D> ? 2 : 1))),
-                               dim3(kGradThreads), 0, stream, p);
+                               dim3((unsigned)(dkv_blocks * dkv_kinds)), dim3(kGradThreads), 0,
+                               stream, p);
             trace_after("softmax_dkv", stream);
         }
     });
@@ -110,7 +125,7 @@ extern "C" sbc_status sbc_softmax_attention_backward(
     SoftmaxArgs p = softmax_args(a);
     size_t used = 0;
     carve(a, workspace, &p, &used);
-    if (!workspace || workspace_bytes < used)
+    if (used > 0 && (!workspace || workspace_bytes < used))
         return fail(SBC_ERR_WORKSPACE,
                     "workspace smaller than sbc_softmax_attention_backward_workspace_size()");
     if (n > 0) {

@@ -18,15 +18,18 @@ template <typename T, int D> constexpr int kGradKeys = sizeof(T) == 4 && D > 64 
 template <typename T, int D> constexpr int kGradWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
 template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
 
+template <typename T, int D> struct RowGradShared {
+    // (one array, so that both tiles are at constant distances from a lane's places)
+    alignas(16) bf16_t tiles[2 * kParts<T> * kGradKeys<T, D> * D];
+};
 template <typename T, int D, bool kWhole>
-__global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_kernel(SoftmaxArgs p) {
+__device__ __forceinline__ void row_grads(const SoftmaxArgs &p, int32_t block,
+                                          RowGradShared<T, D> &lds) {
 #pragma clang fp contract(off)
     constexpr int NP = kParts<T>, KB = kGradKeys<T, D>, kSub = KB / 32, kPlane = KB * D;
-    // (one array, so that both tiles are at constant distances from a lane's places)
-    __shared__ __attribute__((aligned(16))) bf16_t lds[2 * NP * kPlane];
-    bf16_t *const kt = lds, *const vt = lds + NP * kPlane;
-    const int32_t head_k = blockIdx.x % p.kv_heads;
-    const int32_t x = p.slots - 1 - blockIdx.x / p.kv_heads;
+    bf16_t *const kt = lds.tiles, *const vt = lds.tiles + NP * kPlane;
+    const int32_t head_k = block % p.kv_heads;
+    const int32_t x = p.slots - 1 - block / p.kv_heads;
     const int32_t group = p.group.d;
     auto begin = [&](int32_t b) { return (int32_t)((int64_t)q_split(p, b) * group / 128) + b; };
     const int32_t b = sequence_of(p.n_batch, x, begin);
@@ -77,7 +80,7 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
         delta = halves_sum(delta);
     }
     const int64_t flat = place * p.heads + head;
-    if (there && lane < 32) p.delta[flat] = delta;
+    if (p.delta && there && lane < 32) p.delta[flat] = delta;
     // (of a row whose scores are all -inf no key has a weight)
     float lse2 = there ? p.lse_in[flat] * kLog2E : 0.f;
     if (lse2 == -INFINITY) lse2 = INFINITY;
@@ -150,6 +153,12 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
         }
 }
 
+template <typename T, int D, bool kWhole>
+__global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_kernel(SoftmaxArgs p) {
+    __shared__ RowGradShared<T, D> lds;
+    row_grads<T, D, kWhole>(p, blockIdx.x, lds);
+}
+
 // dk and dv: a workgroup has 128 keys of one key head, 32 a wave, and goes through the
 // rows that see them, every p.parts-th tile of rows from the part's own on (p.parts > 1:
 // sums to part_dk and part_dv, which softmax_dkv_join_kernel adds).
@@ -170,7 +179,8 @@ template <typename T, int D> struct KeyGradShared {
     alignas(16) int32_t limits[RB];
 };
 
-template <typename T, int D, bool kWhole, int kGrads>
+// kOwnDelta: delta is made here from o, by 256 / RB neighbouring lanes a row
+template <typename T, int D, bool kWhole, int kGrads, bool kOwnDelta>
 __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
                                           KeyGradShared<T, D> &lds) {
 #pragma clang fp contract(off)
@@ -218,6 +228,9 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
     TileLoad<T, D, RB, kGradThreads, kWhole> sq, sg;
     float next_lse = 0.f, next_delta = 0.f;
     int32_t next_limit = 0;
+    constexpr int kAcross = kOwnDelta ? kGradThreads / RB : 1, kMine = D / kAcross;
+    const int stat_row = threadIdx.x / kAcross;
+    u32x4v next_g[kMine / kVec<T>], next_o[kMine / kVec<T>];  // (kOwnDelta)
     if (kWhole && p.even_rows) {
         auto place = [&](const sbc_heads &x) {
             return [&](int r) {
@@ -243,20 +256,34 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
             sq.load([&](int r) { return row_of(qbase, p.q, r); }, qbase, p.dk);
             sg.load([&](int r) { return row_of(gbase, p.d_o, r); }, gbase, p.dv);
         }
-        if (threadIdx.x < RB) {
-            const int32_t r = r0 + threadIdx.x;
+        if (kOwnDelta || threadIdx.x < RB) {
+            const int32_t r = r0 + stat_row;
             // (no weight for rows that do not exist or have no keys)
             next_lse = INFINITY;
             next_delta = 0.f;
             next_limit = 0;
+            const int32_t token = divide(r < rows ? r : rows - 1, p.group);
+            const int32_t head = head_k * group + (r < rows ? r - token * group : 0);
             if (r < rows) {
-                const int32_t token = divide(r, p.group);
-                const int64_t flat = (int64_t)(s.q0 + token) * p.heads + head_k * group + r - token * group;
+                const int64_t flat = (int64_t)(s.q0 + token) * p.heads + head;
                 next_limit = s.limit(token, p.causal);
                 if (next_limit > 0) {
                     next_lse = p.lse_in[flat] * kLog2E;
                     if (next_lse == -INFINITY) next_lse = INFINITY;
-                    next_delta = p.delta[flat];
+                    if constexpr (!kOwnDelta && kDoK) next_delta = p.delta[flat];
+                }
+            }
+            if constexpr (kOwnDelta && kDoK) {
+                const int c0 = threadIdx.x % kAcross * kMine;
+                auto row = [&](const sbc_heads &x) {
+                    return static_cast<const T *>(x.data) + (s.q0 + token) * x.token_stride +
+                           (int64_t)head * x.head_stride;
+                };
+                const T *g = row(p.d_o), *o = row(p.o);
+#pragma unroll
+                for (int i = 0; i < kMine / kVec<T>; ++i) {
+                    next_g[i] = load_elements<T>(g, c0 + i * kVec<T>, p.dv, next_limit > 0);
+                    next_o[i] = load_elements<T>(o, c0 + i * kVec<T>, p.dv, next_limit > 0);
                 }
             }
         }
@@ -274,10 +301,22 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
         sg.settle();
         sq.store(qt);
         sg.store(gt);
-        if (threadIdx.x < RB) {
-            lses[threadIdx.x] = next_lse;
-            deltas[threadIdx.x] = next_delta;
-            limits[threadIdx.x] = next_limit;
+        if constexpr (kOwnDelta && kDoK) {
+            next_delta = 0.f;
+#pragma unroll
+            for (int i = 0; i < kMine / kVec<T>; ++i) {
+                float a[kVec<T>], c[kVec<T>];
+                unpack<T>(__builtin_bit_cast(raw16, next_g[i]), a);
+                unpack<T>(__builtin_bit_cast(raw16, next_o[i]), c);
+#pragma unroll
+                for (int e = 0; e < kVec<T>; ++e) next_delta = fmaf(a[e], c[e], next_delta);
+            }
+            next_delta = group_sum<kAcross>(next_delta);
+        }
+        if (threadIdx.x % kAcross == 0 && (kOwnDelta || threadIdx.x < RB)) {
+            lses[stat_row] = next_lse;
+            deltas[stat_row] = next_delta;
+            limits[stat_row] = next_limit;
         }
         __syncthreads();
         if (r0 + step < rows) fetch(r0 + step);
@@ -358,12 +397,34 @@ __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_d
     if constexpr (kGradsApart<T, D>) {
         const int32_t half = gridDim.x / 2;  // (dk first: it takes longer)
         if ((int32_t)blockIdx.x < half)
-            key_grads<T, D, kWhole, kDk>(p, blockIdx.x, lds);
+            key_grads<T, D, kWhole, kDk, false>(p, blockIdx.x, lds);
         else
-            key_grads<T, D, kWhole, kDv>(p, blockIdx.x - half, lds);
+            key_grads<T, D, kWhole, kDv, false>(p, blockIdx.x - half, lds);
     } else {
-        key_grads<T, D, kWhole, kDk | kDv>(p, blockIdx.x, lds);
+        key_grads<T, D, kWhole, kDk | kDv, false>(p, blockIdx.x, lds);
     }
+}
+
+// All three in one launch, for small problems, where a launch is most of the time: dq's
+// workgroups first, each of the others making the deltas that it needs (8 tokens of 4 heads of 64
+// bf16 channels: GRADSJOINT).
+template <typename T, int D, bool kWhole>
+__global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_grads_kernel(
+    SoftmaxArgs p, int32_t dq_blocks, int32_t dkv_blocks) {
+    __shared__ union Shared {
+        RowGradShared<T, D> rows;
+        KeyGradShared<T, D> keys;
+        __device__ Shared() {}
+    } lds;
+    const int32_t block = (int32_t)blockIdx.x - dq_blocks;
+    if (block < 0)
+        row_grads<T, D, kWhole>(p, blockIdx.x, lds.rows);
+    else if constexpr (!kGradsApart<T, D>)
+        key_grads<T, D, kWhole, kDk | kDv, true>(p, block, lds.keys);
+    else if (block < dkv_blocks)
+        key_grads<T, D, kWhole, kDk, true>(p, block, lds.keys);
+    else
+        key_grads<T, D, kWhole, kDv, true>(p, block - dkv_blocks, lds.keys);
 }
 
 // The parts' sums of dk (blockIdx.y 0) and dv (1), in the parts' order; keys that lie in no

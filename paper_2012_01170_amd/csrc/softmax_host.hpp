@@ -94,7 +94,7 @@ inline SoftmaxPlan softmax_plan(const sbc_softmax_attention *a, int64_t most_key
     };
     const SoftmaxPlan many = plan(false, 3, 256);
     SoftmaxPlan s = many;
-    if (rows <= (int64_t)64 * a->n_batch || many.blocks < cus) s = plan(true, 4, 256);
+    if (rows <= (int64_t)64 * a->n_batch || many.blocks < cus) s = plan(true, 4, most_keys > 512 ? 128 : 512);
     // (a workgroup of the join for each row)
     if (s.parts > 1 && (int64_t)a->n * a->heads >= (int64_t)1 << 24) {
         s.blocks /= s.parts;

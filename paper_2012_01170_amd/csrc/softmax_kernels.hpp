@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
 // and the waves' sums are joined at the end.  Memory bounds it where a row or few meet a long cache:
 // the next 32 keys and values are always on their way.
 template <typename T, int D, bool kWhole, bool kPaged>
-__global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_rows_kernel(SoftmaxArgs p) {
+__global__ __launch_bounds__(kSoftmaxThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)) void softmax_rows_kernel(SoftmaxArgs p) {
     constexpr int NP = kParts<T>, kPlane = 32 * D;
     constexpr int kJoin = 4 * 32 * 36 * 2;  // (bf16 elements of [4][32][36] float32)
     constexpr int kTiles = 4 * NP * kPlane;

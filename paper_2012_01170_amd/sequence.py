@@ -135,6 +135,9 @@ def layer_norm_backward(dy, x, weight, mean, rstd, need_dx: bool = True,
 
 
 # ---------------------------------------------------------------- rotary positions
+_Sections = ctypes.c_int32 * L.SBC_MAX_AXES
+
+
 def _rotary_plan(q, k, positions, freqs, sections, interleaved):
     """The checked q and k, one of them, and their plan."""
     one = q if q is not None else k
@@ -142,26 +145,25 @@ def _rotary_plan(q, k, positions, freqs, sections, interleaved):
         raise ValueError("q or k is needed")
     _first(one, "q" if q is not None else "k", 3)
     index, (n, _, d) = one.get_device(), one.shape
-    for name, x in (("q", q), ("k", k)):
-        if x is not None:
-            _view(x, name, one.dtype, 3, index)
-            if x.shape[0] != n or x.shape[2] != d:
-                raise ValueError(f"{name} must be [{n}, heads, {d}], got {tuple(x.shape)}")
+    if k is not None and k is not one:
+        _view(k, "k", one.dtype, 3, index)
+        if k.shape[0] != n or k.shape[2] != d:
+            raise ValueError(f"k must be [{n}, heads, {d}], got {tuple(k.shape)}")
     sections = [int(s) for s in sections]
-    if not 1 <= len(sections) <= L.SBC_MAX_AXES:
-        raise ValueError(f"1 .. {L.SBC_MAX_AXES} sections expected, got {len(sections)}")
+    axes = len(sections)
+    if not 1 <= axes <= L.SBC_MAX_AXES:
+        raise ValueError(f"1 .. {L.SBC_MAX_AXES} sections expected, got {axes}")
     if min(sections) < 0:
         raise ValueError(f"sections must be >= 0, got {sections}")
     is_float = isinstance(positions, torch.Tensor) and positions.dtype is torch.float32
     _view(positions, "positions", torch.float32 if is_float else torch.int32, 2, index)
-    if tuple(positions.shape) != (n, len(sections)):
-        raise ValueError(f"positions must be [{n}, {len(sections)}], got {tuple(positions.shape)}")
+    if positions.shape != (n, axes):
+        raise ValueError(f"positions must be [{n}, {axes}], got {tuple(positions.shape)}")
     _dense(freqs, "freqs", torch.float32, 1, index)
-    if freqs.numel() != sum(sections):
+    if freqs.shape[0] != sum(sections):
         raise ValueError(f"freqs must be [{sum(sections)}], got {tuple(freqs.shape)}")
-    plan = L.SbcRotaryPlan(positions.data_ptr(), _row_stride(positions),
-                           int(is_float), freqs.data_ptr(), len(sections),
-                           (ctypes.c_int32 * L.SBC_MAX_AXES)(*sections), int(interleaved))
+    plan = L.SbcRotaryPlan(positions.data_ptr(), _row_stride(positions), int(is_float),
+                           freqs.data_ptr(), axes, _Sections(*sections), int(interleaved))
     return one, index, plan
 
 
@@ -366,7 +368,7 @@ def qk_norm_rotary_backward(dq, dk, q, k, q_weight, k_weight, positions, freqs,
     dw = [torch.empty(d, dtype=torch.float32, device=dev) if need_weights and x is not None
           else None for x in (q, k)]
     lib = L.lib()
-    ws = _Workspace(lib.sbc_qk_norm_rotary_workspace_size(n, d) if need_weights else 0, dev)
+    ws = _scratch(lib.sbc_qk_norm_rotary_workspace_size(n, d) if need_weights else 0, dev)
     L.check(lib.sbc_qk_norm_rotary_backward(
         ctypes.byref(plan), _heads(dq), _heads(dk), _heads(q), 0 if q is None else q.shape[1],
         _heads(k), 0 if k is None else k.shape[1], _ptr(q_weight), _ptr(k_weight),
@@ -443,7 +445,7 @@ def softmax_attention_backward(do, q, k, v, o, lse, splits: Optional[torch.Tenso
         raise ValueError(f"lse must be {shape[:2]}, got {tuple(lse.shape)}")
     dq, dk, dv = (torch.empty(x.shape, dtype=q.dtype, device=dev) for x in (q, k, v))
     lib, ref = L.lib(), ctypes.byref(a)
-    ws = _Workspace(lib.sbc_softmax_attention_backward_workspace_size(ref), dev)
+    ws = _scratch(lib.sbc_softmax_attention_backward_workspace_size(ref), dev)
     L.check(lib.sbc_softmax_attention_backward(
         ref, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), lse.data_ptr(), _heads(dq),
         _heads(dk), _heads(dv), ws.ptr, ws.nbytes, _stream(index)))
