@@ -507,6 +507,7 @@ __device__ __forceinline__ void row_products(Read read, Operand operand, floatx1
     for (int k = 0; k < kAhead && k < kSteps; ++k)
 #pragma unroll
         for (int j = 0; j < kJobs; ++j) read(k, j, f[k][j]);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
         keep_order();
@@ -518,6 +519,7 @@ __device__ __forceinline__ void row_products(Read read, Operand operand, floatx1
             for (int j = 0; j < kJobs; ++j) read(k + kAhead, j, f[k % kAhead][j]);
         }
     }
+    __builtin_amdgcn_s_setprio(0);
 }
 
 // acc[t] += columns 32 t .. + 31 of the tile, transposed, times weights by rows: k-step h takes
@@ -541,6 +543,7 @@ template <typename T, int D, int kRows, int kBuffers = 2> struct ColumnProducts 
                                         int plane, int first, const LaneAt32<D> &at,
                                         floatx16 (&acc)[D / 32]) {
 #pragma clang fp contract(off)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int h = 0; h < kSteps; ++h) {
             if (kBuffers == 2 && h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
@@ -552,6 +555,7 @@ template <typename T, int D, int kRows, int kBuffers = 2> struct ColumnProducts 
             keep_order();
             if (kBuffers == 1 && h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
         }
+        __builtin_amdgcn_s_setprio(0);
     }
 };
 
