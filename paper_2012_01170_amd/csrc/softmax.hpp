@@ -68,13 +68,20 @@ struct SoftmaxArgs {
     // gradients
     sbc_heads d_o, dq, dk_out, dv_out;
     const float *lse_in;
-    float *delta;
+    // the rows' deltas, and their sums in units of log 2 (infinite where no key has a weight), a
+    // key head's rows behind each other (packed_row)
+    float *row_delta, *row_lse;
     float *part_dk, *part_dv;
     int32_t even_rows;  // whether tiles of rows begin with a token's first head, at 32-bit offsets
 };
 
 __device__ __forceinline__ int32_t clamp_i(int32_t x, int32_t lo, int32_t hi) {
     return x < lo ? lo : x > hi ? hi : x;
+}
+// Where row `row` of key head head_k lies among the packed ones
+__device__ __forceinline__ int64_t packed_row(const SoftmaxArgs &p, int32_t head_k, int32_t q0,
+                                              int32_t row) {
+    return ((int64_t)head_k * p.n + q0) * p.group.d + row;
 }
 // (whatever the splits hold, rows are read and written inside the arrays)
 __device__ __forceinline__ int32_t q_split(const SoftmaxArgs &p, int32_t b) {
@@ -398,6 +405,54 @@ template <typename T, int D, int kRows, int kThreads, bool kWhole> struct TileLo
         }
     }
 };
+
+// kRows x D bf16 values straight to LDS, 16 bytes a lane: the pieces of a wave land behind each
+// other, so that the rows' permutation (TileAt) is in what each lane asks for.  The compiler does
+// not count these loads (it would wait for all of them before any LDS read): wait_direct() does.
+template <int D, int kRows, int kThreads> struct DirectTile {
+    static constexpr int kPerRow = D / 8, kSteps = kRows * kPerRow / kThreads;
+    static_assert(kRows * kPerRow % kThreads == 0 && D % 64 == 0, "pieces");
+    uint32_t off[kSteps];
+    // row r is at(r) elements from the base
+    template <typename F> __device__ __forceinline__ void places(F at) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int piece = s * kThreads + threadIdx.x, row = piece / kPerRow;
+            const int in_row = piece % kPerRow * 8;
+            const int col = TileAt<D>::at(row, in_row) - row * D;  // (the permutation is its own inverse)
+            off[s] = (at(row) + (uint32_t)col) * 2u;
+        }
+    }
+    // base, tile: the same in all lanes of a wave
+    __device__ __forceinline__ void load(const bf16_t *base, const bf16_t *tile) const {
+        typedef __attribute__((address_space(3))) const bf16_t *lds_p;
+        const uint32_t to = (uint32_t)(uintptr_t)(lds_p)tile;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const uint32_t m0 = __builtin_amdgcn_readfirstlane(
+                to + (uint32_t)(s * kThreads + 64 * wave_of_block()) * 16u);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :
+                         : "s"(m0), "v"(off[s]), "s"(base)
+                         : "memory");
+        }
+    }
+};
+// `count` float32 values (64 at most) behind each other to LDS
+__device__ __forceinline__ void direct_floats(const float *base, const float *to, int count) {
+    typedef __attribute__((address_space(3))) const float *lds_p;
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_p)to);
+    const int lane = threadIdx.x & 63;
+    if (lane < count)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                     :
+                     : "s"(m0), "v"((uint32_t)lane * 4u), "s"(base)
+                     : "memory");
+}
+// until at most kLeft of this wave's loads are on their way
+template <int kLeft> __device__ __forceinline__ void wait_direct() {
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLeft) : "memory");
+}
 
 // A row's two halves joined, in both
 __device__ __forceinline__ float halves_max(float x) {

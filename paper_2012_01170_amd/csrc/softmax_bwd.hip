@@ -23,7 +23,10 @@ bool grads_joint(const sbc_softmax_attention *a) {
 void carve(const sbc_softmax_attention *a, void *workspace, SoftmaxArgs *p, size_t *used) {
     Carver c(workspace);
     p->parts = grad_parts(a);
-    if (!grads_joint(a)) p->delta = c.take<float>((size_t)a->n * a->heads);
+    if (!grads_joint(a)) {
+        p->row_delta = c.take<float>((size_t)a->n * a->heads);
+        p->row_lse = c.take<float>((size_t)a->n * a->heads);
+    }
     if (p->parts > 1) {
         p->part_dk = c.take<float>((size_t)p->parts * a->m * a->kv_heads * a->dk);
         p->part_dv = c.take<float>((size_t)p->parts * a->m * a->kv_heads * a->dv);
@@ -67,9 +70,12 @@ sbc_status backward(SoftmaxArgs p, const sbc_softmax_attention *a, hipStream_t s
         }
         if (a->m > 0) {
             trace_before("softmax_dkv", stream);
-            hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole>),
-                               dim3((unsigned)(dkv_blocks * dkv_kinds)), dim3(kGradThreads), 0,
-                               stream, p);
+            const dim3 grid((unsigned)(dkv_blocks * dkv_kinds)), block(kGradThreads);
+            constexpr bool kCan = sizeof(T) == 2 && D % 64 == 0 && kWhole;
+            if (kCan && p.even_rows && a->dk == D && a->dv == D)
+                hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole, kCan>), grid, block, 0, stream, p);
+            else
+                hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole, false>), grid, block, 0, stream, p);
             trace_after("softmax_dkv", stream);
         }
     });

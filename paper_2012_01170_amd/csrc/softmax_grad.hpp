@@ -80,10 +80,13 @@ __device__ __forceinline__ void row_grads(const SoftmaxArgs &p, int32_t block,
         delta = halves_sum(delta);
     }
     const int64_t flat = place * p.heads + head;
-    if (p.delta && there && lane < 32) p.delta[flat] = delta;
     // (of a row whose scores are all -inf no key has a weight)
     float lse2 = there ? p.lse_in[flat] * kLog2E : 0.f;
     if (lse2 == -INFINITY) lse2 = INFINITY;
+    if (p.row_delta && there && lane < 32) {
+        p.row_delta[packed_row(p, head_k, s.q0, row)] = delta;
+        p.row_lse[packed_row(p, head_k, s.q0, row)] = lse2;
+    }
 
     const T *const kbase =
         static_cast<const T *>(p.k.data) + s.k0 * p.k.token_stride + head_k * p.k.head_stride;
@@ -172,23 +175,23 @@ constexpr int kDk = 1, kDv = 2;
 template <typename T, int D> constexpr int kGradRows = D > 64 || (sizeof(T) == 4 && D > 32) ? (D == 96 ? 64 : 32) : 64;
 template <typename T, int D> constexpr bool kGradsApart = sizeof(T) * D > 128;
 
-template <typename T, int D> struct KeyGradShared {
+template <typename T, int D, int kBuffers = 1> struct KeyGradShared {
     static constexpr int NP = kParts<T>, RB = kGradRows<T, D>;
-    alignas(16) bf16_t tiles[2 * NP * RB * D];
-    alignas(16) float lses[RB], deltas[RB];
-    alignas(16) int32_t limits[RB];
+    alignas(16) bf16_t tiles[kBuffers * 2 * NP * RB * D];
+    alignas(16) float lses[kBuffers * RB], deltas[kBuffers * RB];
 };
 
-// kOwnDelta: delta is made here from o, by 256 / RB neighbouring lanes a row
-template <typename T, int D, bool kWhole, int kGrads, bool kOwnDelta>
+// kOwnDelta: delta is made here from o, by 256 / RB neighbouring lanes a row.
+// kDirect: whole tiles of rows go straight to LDS, two ahead, in three buffers: registers of
+// a tile on its way reach one tile ahead only, which is less than a load takes (16384 tokens, 2
+// key heads of 128 bf16 channels: DIRECTTIME).
+template <typename T, int D, bool kWhole, int kGrads, bool kOwnDelta, bool kDirect = false>
 __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
-                                          KeyGradShared<T, D> &lds) {
+                                          KeyGradShared<T, D, (kDirect ? 3 : 1)> &lds) {
 #pragma clang fp contract(off)
     constexpr int NP = kParts<T>, RB = kGradRows<T, D>, kSub = RB / 32, kPlane = RB * D;
     constexpr bool kDoK = kGrads & kDk, kDoV = kGrads & kDv;
-    bf16_t *const qt = lds.tiles, *const gt = lds.tiles + NP * kPlane;
-    float *const lses = lds.lses, *const deltas = lds.deltas;
-    int32_t *const limits = lds.limits;
+    static_assert(!kDirect || (NP == 1 && kWhole && !kOwnDelta), "direct");
     const int32_t head_k = block % p.kv_heads;
     const int32_t part = block / p.kv_heads % p.parts;
     const int32_t x = block / p.kv_heads / p.parts;
@@ -226,8 +229,8 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
     const T *const gbase = static_cast<const T *>(p.d_o.data) + s.q0 * p.d_o.token_stride +
                            (int64_t)head_k * group * p.d_o.head_stride;
     TileLoad<T, D, RB, kGradThreads, kWhole> sq, sg;
+    DirectTile<(kDirect ? D : 64), (kDirect ? RB : 64), kGradThreads> dq, dg;
     float next_lse = 0.f, next_delta = 0.f;
-    int32_t next_limit = 0;
     constexpr int kAcross = kOwnDelta ? kGradThreads / RB : 1, kMine = D / kAcross;
     const int stat_row = threadIdx.x / kAcross;
     u32x4v next_g[kMine / kVec<T>], next_o[kMine / kVec<T>];  // (kOwnDelta)
@@ -239,68 +242,22 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
                        (uint32_t)(r - token * group) * (uint32_t)x.head_stride;
             };
         };
-        sq.places(place(p.q), p.dk);
-        sg.places(place(p.d_o), p.dv);
-    }
-    auto fetch = [&](int32_t r0) {
-        auto row_of = [&](const T *base, const sbc_heads &x, int r) -> const T * {
-            if (r0 + r >= rows) return nullptr;
-            const int32_t token = divide(r0 + r, p.group);
-            return base + token * x.token_stride + (r0 + r - token * group) * x.head_stride;
-        };
-        if (kWhole && p.even_rows && r0 + RB <= rows) {
-            const int32_t token = divide(r0, p.group);
-            sq.load_all(qbase + token * p.q.token_stride);
-            sg.load_all(gbase + token * p.d_o.token_stride);
+        if constexpr (kDirect) {
+            dq.places(place(p.q));
+            dg.places(place(p.d_o));
         } else {
-            sq.load([&](int r) { return row_of(qbase, p.q, r); }, qbase, p.dk);
-            sg.load([&](int r) { return row_of(gbase, p.d_o, r); }, gbase, p.dv);
+            sq.places(place(p.q), p.dk);
+            sg.places(place(p.d_o), p.dv);
         }
-        if (kOwnDelta || threadIdx.x < RB) {
-            const int32_t r = r0 + stat_row;
-            // (no weight for rows that do not exist or have no keys)
-            next_lse = INFINITY;
-            next_delta = 0.f;
-            next_limit = 0;
-            const int32_t token = divide(r < rows ? r : rows - 1, p.group);
-            const int32_t head = head_k * group + (r < rows ? r - token * group : 0);
-            if (r < rows) {
-                const int64_t flat = (int64_t)(s.q0 + token) * p.heads + head;
-                next_limit = s.limit(token, p.causal);
-                if (next_limit > 0) {
-                    next_lse = p.lse_in[flat] * kLog2E;
-                    if (next_lse == -INFINITY) next_lse = INFINITY;
-                    if constexpr (!kOwnDelta && kDoK) next_delta = p.delta[flat];
-                }
-            }
-            if constexpr (kOwnDelta && kDoK) {
-                const int c0 = threadIdx.x % kAcross * kMine;
-                auto row = [&](const sbc_heads &x) {
-                    return static_cast<const T *>(x.data) + (s.q0 + token) * x.token_stride +
-                           (int64_t)head * x.head_stride;
-                };
-                const T *g = row(p.d_o), *o = row(p.o);
-#pragma unroll
-                for (int i = 0; i < kMine / kVec<T>; ++i) {
-                    next_g[i] = load_elements<T>(g, c0 + i * kVec<T>, p.dv, next_limit > 0);
-                    next_o[i] = load_elements<T>(o, c0 + i * kVec<T>, p.dv, next_limit > 0);
-                }
-            }
-        }
-    };
-    const LaneAt32<D> places;
-    const int half = lane >> 5;
-    floatx16 dk[D / 32], dv[D / 32];
-    clear(dk);
-    clear(dv);
-    int32_t r0 = from + part * RB;
-    if (r0 < rows) fetch(r0);
-    for (; r0 < rows; r0 += step) {
-        __syncthreads();
+    }
+    auto put_tile = [&](bf16_t *buffer) {
         sq.settle();
         sg.settle();
-        sq.store(qt);
-        sg.store(gt);
+        sq.store(buffer);
+        sg.store(buffer + NP * kPlane);
+    };
+    // what the rows' weights need, to place `slot`
+    auto put_stats = [&](int slot) {
         if constexpr (kOwnDelta && kDoK) {
             next_delta = 0.f;
 #pragma unroll
@@ -314,17 +271,111 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
             next_delta = group_sum<kAcross>(next_delta);
         }
         if (threadIdx.x % kAcross == 0 && (kOwnDelta || threadIdx.x < RB)) {
-            lses[stat_row] = next_lse;
-            deltas[stat_row] = next_delta;
-            limits[stat_row] = next_limit;
+            lds.lses[slot * RB + stat_row] = next_lse;
+            lds.deltas[slot * RB + stat_row] = next_delta;
         }
-        __syncthreads();
-        if (r0 + step < rows) fetch(r0 + step);
+    };
+    // a tile into registers, or (kDirect) to LDS
+    auto fetch = [&](int32_t r0, int slot) {
+        auto row_of = [&](const T *base, const sbc_heads &x, int r) -> const T * {
+            if (r0 + r >= rows) return nullptr;
+            const int32_t token = divide(r0 + r, p.group);
+            return base + token * x.token_stride + (r0 + r - token * group) * x.head_stride;
+        };
+        // (no weight for rows that do not exist)
+        const int32_t r = r0 + stat_row;
+        if constexpr (kOwnDelta) {
+            next_lse = INFINITY;
+            const int32_t token = divide(r < rows ? r : rows - 1, p.group);
+            const int32_t head = head_k * group + (r < rows ? r - token * group : 0);
+            if (r < rows) {
+                next_lse = p.lse_in[(int64_t)(s.q0 + token) * p.heads + head] * kLog2E;
+                if (next_lse == -INFINITY) next_lse = INFINITY;
+            }
+            if constexpr (kDoK) {
+                const int c0 = threadIdx.x % kAcross * kMine;
+                auto row = [&](const sbc_heads &x) {
+                    return static_cast<const T *>(x.data) + (s.q0 + token) * x.token_stride +
+                           (int64_t)head * x.head_stride;
+                };
+                const T *g = row(p.d_o), *o = row(p.o);
+#pragma unroll
+                for (int i = 0; i < kMine / kVec<T>; ++i) {
+                    next_g[i] = load_elements<T>(g, c0 + i * kVec<T>, p.dv, r < rows);
+                    next_o[i] = load_elements<T>(o, c0 + i * kVec<T>, p.dv, r < rows);
+                }
+            }
+        } else if (threadIdx.x < RB && !(kDirect && r0 + RB <= rows)) {
+            next_lse = INFINITY;
+            next_delta = 0.f;
+            if (r < rows) {
+                next_lse = p.row_lse[packed_row(p, head_k, s.q0, r)];
+                next_delta = p.row_delta[packed_row(p, head_k, s.q0, r)];
+            }
+        }
+        if (kWhole && p.even_rows && r0 + RB <= rows) {
+            const int32_t token = divide(r0, p.group);
+            const T *const q0 = qbase + token * p.q.token_stride, *const g0 = gbase + token * p.d_o.token_stride;
+            if constexpr (kDirect) {
+                bf16_t *const buffer = lds.tiles + slot * 2 * kPlane;
+                dq.load(q0, buffer);
+                dg.load(g0, buffer + kPlane);
+                // (each wave one of them, so that all have as many loads on their way)
+                const int64_t at = packed_row(p, head_k, s.q0, r0);
+                if (wave & 1)
+                    direct_floats(p.row_delta + at, lds.deltas + slot * RB, RB);
+                else
+                    direct_floats(p.row_lse + at, lds.lses + slot * RB, RB);
+            } else {
+                sq.load_all(q0);
+                sg.load_all(g0);
+            }
+        } else {
+            sq.load([&](int r) { return row_of(qbase, p.q, r); }, qbase, p.dk);
+            sg.load([&](int r) { return row_of(gbase, p.d_o, r); }, gbase, p.dv);
+            if constexpr (kDirect) {
+                put_tile(lds.tiles + slot * 2 * kPlane);
+                put_stats(slot);
+            }
+        }
+    };
+    const LaneAt32<D> places;
+    const int half = lane >> 5;
+    floatx16 dk[D / 32], dv[D / 32];
+    clear(dk);
+    clear(dv);
+    constexpr int kBuffer = 2 * NP * kPlane;
+    int32_t r0 = from + part * RB;
+    int slot = 0;
+    if (r0 < rows) fetch(r0, 0);
+    if (kDirect && r0 + step < rows) fetch(r0 + step, 1);
+    for (; r0 < rows; r0 += step) {
+        if constexpr (kDirect) {
+            // this tile's loads are done where none but the next one's are left
+            if (r0 + step + RB <= rows)
+                wait_direct<2 * decltype(dq)::kSteps + 1>();
+            else
+                wait_direct<0>();
+            __syncthreads();  // (and the tile before has been read)
+            if (r0 + 2 * step < rows) fetch(r0 + 2 * step, slot == 0 ? 2 : slot - 1);
+        } else {
+            __syncthreads();
+            put_tile(lds.tiles);
+            put_stats(0);
+            __syncthreads();
+            if (r0 + step < rows) fetch(r0 + step, 0);
+        }
+        const bf16_t *const qt = lds.tiles + slot * kBuffer, *const gt = qt + NP * kPlane;
+        const float *const lses = lds.lses + slot * RB, *const deltas = lds.deltas + slot * RB;
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
             const LaneAt32<D> at(places);
-            // (limits do not fall along the rows that there are; the others' sums are infinite)
-            const int32_t first = __builtin_amdgcn_readfirstlane(limits[32 * u]);
+            // (limits do not fall along the rows that there are; the others see nothing, also not by
+            // a product of their zeros with an infinity)
+            auto limit_of = [&](int32_t r) {
+                return r < rows ? s.limit(divide(r, p.group), p.causal) : 0;
+            };
+            const int32_t first = __builtin_amdgcn_readfirstlane(limit_of(r0 + 32 * u));
             floatx16 w[kDoK ? 2 : 1];  // scores, and dO v
             clear(w);
             row_products<T, D, (kDoK ? 2 : 1), (NP == 1 && !kDoK ? 4 : 2)>(
@@ -335,7 +386,7 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
             ColumnProducts<T, D, 32, (NP == 3 ? 1 : 2)> grads, queries;
             if constexpr (kDoV) grads.read(gt, kPlane, 32 * u, at);
             else queries.read(qt, kPlane, 32 * u, at);
-            const bool masked = first < wave_key + 32;
+            const bool masked = first < wave_key + 32 || r0 + 32 * u + 32 > rows;
             floatx16 e[1], ds[1];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -354,7 +405,7 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const bool ok = key < limits[32 * u + 8 * j + 4 * half + i];
+                        const bool ok = key < limit_of(r0 + 32 * u + 8 * j + 4 * half + i);
                         if constexpr (kDoV) e[0][4 * j + i] = ok ? e[0][4 * j + i] : 0.f;
                         if constexpr (kDoK) ds[0][4 * j + i] = ok ? ds[0][4 * j + i] : 0.f;
                     }
@@ -365,6 +416,7 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
                 queries.add(ds, qt, kPlane, 32 * u, at, dk);
             }
         }
+        if constexpr (kDirect) slot = slot == 2 ? 0 : slot + 1;
     }
     if (!there) return;
     const int64_t place = s.k0 + key;
@@ -391,17 +443,17 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
     if constexpr (kDoV) put(dv, 1.f, p.part_dv, p.dv_out, p.dv);
 }
 
-template <typename T, int D, bool kWhole>
+template <typename T, int D, bool kWhole, bool kDirect>
 __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_dkv_kernel(SoftmaxArgs p) {
-    __shared__ KeyGradShared<T, D> lds;
+    __shared__ KeyGradShared<T, D, (kDirect ? 3 : 1)> lds;
     if constexpr (kGradsApart<T, D>) {
         const int32_t half = gridDim.x / 2;  // (dk first: it takes longer)
         if ((int32_t)blockIdx.x < half)
-            key_grads<T, D, kWhole, kDk, false>(p, blockIdx.x, lds);
+            key_grads<T, D, kWhole, kDk, false, kDirect>(p, blockIdx.x, lds);
         else
-            key_grads<T, D, kWhole, kDv, false>(p, blockIdx.x - half, lds);
+            key_grads<T, D, kWhole, kDv, false, kDirect>(p, blockIdx.x - half, lds);
     } else {
-        key_grads<T, D, kWhole, kDk | kDv, false>(p, blockIdx.x, lds);
+        key_grads<T, D, kWhole, kDk | kDv, false, kDirect>(p, blockIdx.x, lds);
     }
 }
 
