@@ -437,6 +437,28 @@ template <int D, int kRows, int kThreads> struct DirectTile {
                          : "memory");
         }
     }
+    // Values of the tile, which has landed, as TileLoad::put_bad_apart has them
+    __device__ __forceinline__ static void put_bad_apart(bf16_t *tile, int32_t first,
+                                                         int32_t *first_bad) {
+        for (int s = 0; s < kSteps; ++s) {
+            const int piece = s * kThreads + threadIdx.x, row = piece / kPerRow;
+            u32x4v w = *reinterpret_cast<const u32x4v *>(tile + piece * 8);
+            if (finite_bits(w[0], true) && finite_bits(w[1], true) && finite_bits(w[2], true) &&
+                finite_bits(w[3], true))
+                continue;
+            const int col = TileAt<D>::at(row, piece % kPerRow * 8) - row * D;
+            bf16_t e[8];
+            __builtin_memcpy(e, &w, 16);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((e[i] & 0x7F80u) == 0x7F80u) {
+                    e[i] = 0;
+                    atomicMin(first_bad + col + i, first + row);
+                }
+            __builtin_memcpy(&w, e, 16);
+            *reinterpret_cast<u32x4v *>(tile + piece * 8) = w;
+        }
+    }
 };
 // `count` float32 values (64 at most) behind each other to LDS
 __device__ __forceinline__ void direct_floats(const float *base, const float *to, int count) {

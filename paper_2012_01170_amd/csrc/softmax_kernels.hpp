@@ -29,11 +29,13 @@ __device__ __forceinline__ int32_t part_keys(int32_t lk, int32_t parts) {
 // ---------------------------------------------------------------- many rows
 // A workgroup has 128 rows, 32 a wave, and goes through the keys that they see in tiles,
 // which its waves share in LDS; the next tile is on its way into registers meanwhile.
-template <typename T, int D, bool kWhole, bool kPaged>
+template <typename T, int D, bool kWhole, bool kPaged, bool kDirect = false>
 __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_tile_kernel(SoftmaxArgs p) {
-    constexpr int NP = kParts<T>, KB = kTileKeys<T, D>, kPlane = KB * D;
+    constexpr int NP = kParts<T>, KB = kDirect && D > 64 ? 32 : kTileKeys<T, D>, kPlane = KB * D;
     constexpr int kSub = KB < 32 * kTogether<T, D> ? 1 : kTogether<T, D>;
-    __shared__ __attribute__((aligned(16))) bf16_t kt[NP * kPlane], vt[NP * kPlane];
+    constexpr int kBuffer = 2 * NP * kPlane;  // keys, then values
+    __shared__ __attribute__((aligned(16))) bf16_t lds[(kDirect ? 3 : 1) * kBuffer];
+    static_assert(!kDirect || (NP == 1 && kWhole && !kPaged), "direct");
     __shared__ int32_t first_bad[D];  // (TileLoad::put_bad_apart)
     const int32_t head_k = blockIdx.x % p.kv_heads;
     const int32_t part = blockIdx.x / p.kv_heads % p.parts;
@@ -83,9 +85,18 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     }
     constexpr uint64_t kAll = KB == 64 ? ~0ull : 0xFFFFFFFFull;
     TileLoad<T, D, KB, kSoftmaxThreads, kWhole> sk, sv;
+    DirectTile<(kDirect ? D : 64), (kDirect ? KB : 64), kSoftmaxThreads> dk, dv;
     KeyPlaces where;  // of the tile that is fetched next
     uint64_t known = kAll, next_known = kAll;
-    auto fetch = [&](int32_t k0) {
+    auto put_tile = [&](int32_t k0, bf16_t *buffer) {
+        sk.settle();
+        sv.settle();
+        if (k0 + KB > least) sv.put_bad_apart(k0, first_bad);
+        sk.store(buffer);
+        sv.store(buffer + NP * kPlane);
+    };
+    // a tile into registers, or (kDirect) to LDS
+    auto fetch = [&](int32_t k0, bf16_t *buffer) {
         if constexpr (kPaged) {
             where.template settle<KB>(p);
             sk.load([&](int r) { return where.row<T>(p.pages.k, head_k, r); }, kbase, p.dk);
@@ -94,17 +105,27 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
             where.template look<KB>(p, s, k0 + KB, s.lk);
         } else {
             if (kWhole && k0 + KB <= s.lk) {
-                sk.load_all(kbase + k0 * p.k.token_stride);
-                sv.load_all(vbase + k0 * p.v.token_stride);
+                const T *const k = kbase + k0 * p.k.token_stride, *const v = vbase + k0 * p.v.token_stride;
+                if constexpr (kDirect) {
+                    dk.load(k, buffer);
+                    dv.load(v, buffer + kPlane);
+                } else {
+                    sk.load_all(k);
+                    sv.load_all(v);
+                }
                 return;
             }
             sk.load([&](int r) { return k0 + r < s.lk ? kbase + (k0 + r) * p.k.token_stride : nullptr; },
                     kbase, p.dk);
             sv.load([&](int r) { return k0 + r < s.lk ? vbase + (k0 + r) * p.v.token_stride : nullptr; },
                     vbase, p.dv);
+            if constexpr (kDirect) put_tile(k0, buffer);
         }
     };
-    if (kWhole && !kPaged) {
+    if constexpr (kDirect) {
+        dk.places([&](int r) { return (uint32_t)r * (uint32_t)p.k.token_stride; });
+        dv.places([&](int r) { return (uint32_t)r * (uint32_t)p.v.token_stride; });
+    } else if (kWhole && !kPaged) {
         sk.places(p.k.token_stride, p.dk);
         sv.places(p.v.token_stride, p.dv);
     }
@@ -114,18 +135,31 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     __syncthreads();
     if (first < end) {
         if constexpr (kPaged) where.template look<KB>(p, s, first, s.lk);
-        fetch(first);
+        fetch(first, lds);
+        if (kDirect && first + KB < end) fetch(first + KB, lds + kBuffer);
     }
+    int slot = 0;
     for (int32_t k0 = first; k0 < end; k0 += KB) {
-        __syncthreads();  // the last tile has been read
-        sk.settle();
-        sv.settle();
-        if (k0 + KB > least) sv.put_bad_apart(k0, first_bad);
-        sk.store(kt);
-        sv.store(vt);
-        known = next_known;
-        __syncthreads();
-        if (k0 + KB < end) fetch(k0 + KB);
+        if constexpr (kDirect) {
+            // this tile's loads are done where none but the next one's are left
+            if (k0 + KB < end && k0 + 2 * KB <= s.lk)
+                wait_direct<2 * decltype(dk)::kSteps>();
+            else
+                wait_direct<0>();
+            __syncthreads();  // (and the tile before has been read)
+            if (k0 + KB > least) {
+                decltype(dv)::put_bad_apart(lds + slot * kBuffer + kPlane, k0, first_bad);
+                __syncthreads();
+            }
+            if (k0 + 2 * KB < end) fetch(k0 + 2 * KB, lds + (slot == 0 ? 2 : slot - 1) * kBuffer);
+        } else {
+            __syncthreads();  // the last tile has been read
+            put_tile(k0, lds);
+            known = next_known;
+            __syncthreads();
+            if (k0 + KB < end) fetch(k0 + KB, lds);
+        }
+        const bf16_t *const kt = lds + slot * kBuffer, *const vt = kt + NP * kPlane;
         // (tiles that hold nothing for this wave, behind the diagonal, are gone through as well: with a
         // branch around them the sums were copied from registers to registers in every tile)
 #pragma unroll
@@ -149,6 +183,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
             softmax_weights<D, kSub>(x, p.scale2, sums);
             values.add(x, vt, kPlane, 32 * u0, at, sums.o);
         }
+        if constexpr (kDirect) slot = slot == 2 ? 0 : slot + 1;
     }
     if (!there) return;
     const float l = halves_sum(sums.l);
