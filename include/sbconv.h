@@ -732,15 +732,15 @@ sbc_status sbc_qk_norm_rotary_backward(const sbc_rotary_plan *plan, const sbc_he
  *              float32 or bf16 (dtype), 1 <= dk, dv <= 128, heads <= 65535,
  *              n heads and m kv_heads below 2^31
  *   lse        [n, heads] float32, or NULL: not wanted
- *   scale      > 0 and finite
+ *   scale      > 0 and below 2e38
  * Scores, maxima and sums are float32.  Products are taken on the matrix cores, of float32
  * inputs with operands split into three bf16 parts (products up to 2^-22 of the whole left
  * out); of bf16 inputs, the weights are rounded to bf16 (2^-8 each) on their way to the
  * product with v, as are the terms of the gradients' products.
  * A NaN or infinity reaches no other sequence and no row that does not see it; an infinity
- * may come out as NaN.  (The gradients: no other sequence; within one, rows and keys of the
- * same 128 may share it.)
- * No output may overlap an input.  Results do not depend on anything but the inputs.
+ * may come out as NaN.  (The gradients: no other sequence; within one, tokens up to 256 before
+ * and behind may share it.)
+ * No output may overlap an input.  The same call gives the same results, bit by bit.
  * ------------------------------------------------------------------------ */
 typedef struct {
     int32_t n, m, n_batch, heads, kv_heads, dk, dv;

@@ -72,7 +72,7 @@ sbc_status backward(SoftmaxArgs p, const sbc_softmax_attention *a, hipStream_t s
             trace_before("softmax_dkv", stream);
             const dim3 grid((unsigned)(dkv_blocks * dkv_kinds)), block(kGradThreads);
             constexpr bool kCan = sizeof(T) == 2 && D % 64 == 0 && kWhole;
-            if (kCan && p.even_rows && a->dk == D && a->dv == D)
+            if (kCan && p.even_rows && a->dk == D && softmax_direct(a, {&p.q, &p.d_o}))
                 hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole, kCan>), grid, block, 0, stream, p);
             else
                 hipLaunchKernelGGL((softmax_dkv_kernel<T, D, kWhole, false>), grid, block, 0, stream, p);

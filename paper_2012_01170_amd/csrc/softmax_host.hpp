@@ -16,8 +16,8 @@ inline sbc_status check_softmax(const sbc_softmax_attention *a) {
     if (a->heads % a->kv_heads)
         return fail(SBC_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
     if (!known_dtype(a->dtype)) return fail(SBC_ERR_INVALID_ARG, "unknown dtype");
-    if (!(a->scale > 0.f) || !std::isfinite(a->scale))
-        return fail(SBC_ERR_INVALID_ARG, "scale must be > 0 and finite");
+    if (!(a->scale > 0.f) || !(a->scale < 2e38f))  // (times log2 e it is finite)
+        return fail(SBC_ERR_INVALID_ARG, "scale must be > 0 and below 2e38");
     if (a->dk > 128 || a->dv > 128)
         return fail(SBC_ERR_UNSUPPORTED, "dk and dv must be <= 128");
     if (a->heads > 65535) return fail(SBC_ERR_UNSUPPORTED, "heads must be <= 65535");
@@ -49,6 +49,15 @@ inline bool softmax_whole(const sbc_softmax_attention *a,
     if (a->dk % v || a->dv % v) return false;
     for (const sbc_heads *x : arrays)
         if (x->token_stride >= 1 << 22) return false;
+    return true;
+}
+
+// Rows that DirectTile can load: these loads are taken at addresses of whole pieces alone
+inline bool softmax_direct(const sbc_softmax_attention *a,
+                           std::initializer_list<const sbc_heads *> arrays) {
+    if (a->dtype != SBC_BF16 || a->dk != a->dv) return false;
+    for (const sbc_heads *x : arrays)
+        if ((uintptr_t)x->data % 16 || x->token_stride % 8 || x->head_stride % 8) return false;
     return true;
 }
 

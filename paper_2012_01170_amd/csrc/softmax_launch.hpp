@@ -28,7 +28,7 @@ sbc_status softmax_forward(SoftmaxArgs p, const sbc_softmax_attention *a, const 
         else if (plan.few)
             hipLaunchKernelGGL((softmax_rows_kernel<T, D, false, kPaged>), grid, block, 0, stream, p);
         else if (constexpr bool kCan = sizeof(T) == 2 && D % 64 == 0 && !kPaged;
-                 kCan && whole && a->dk == D && a->dv == D)
+                 kCan && whole && a->dk == D && softmax_direct(a, {&p.k, &p.v}))
             hipLaunchKernelGGL((softmax_tile_kernel<T, D, true, kPaged, kCan>), grid, block, 0, stream,
                                p);
         else if (whole)

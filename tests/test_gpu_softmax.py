@@ -176,6 +176,41 @@ def test_views(dtype, heads, n):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,n", [((8, 4), 40), ((24, 8), 1300)])
+def test_layouts(dtype, d, heads, n):
+    """Heads before tokens, parts of a projection on and off 16 bytes, tokens in every second
+    row: as contiguous ones, bit by bit."""
+    rng = np.random.default_rng(14)
+    hq, hk = heads
+    c = [_rand(rng, (n, h, d), dtype) for h in (hq, hk, hk, hq)]
+
+    def passes(q, k, v, do):
+        o, lse = sbc.softmax_attention_forward(q, k, v, causal=True)
+        return (o, lse, *sbc.softmax_attention_backward(do, q, k, v, o, lse, causal=True))
+
+    want = passes(*c)
+    heads_first = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in c]
+    spread = []
+    for x in c:
+        y = torch.full((n, 2, x.shape[1], d), math.nan, dtype=dtype, device=DEV)
+        y[:, 1] = x
+        spread.append(y[:, 1])
+    layouts = [heads_first, spread]
+    for off in (8, 1):
+        wide = torch.full((n, 2 * hq + 2 * hk, d + 16), math.nan, dtype=dtype, device=DEV)
+        at, part = 0, []
+        for x in c:
+            part.append(wide[:, at:at + x.shape[1], off:off + d])
+            part[-1].copy_(x)
+            at += x.shape[1]
+        layouts.append(part)
+    for x in layouts:
+        got = passes(*x)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf, 3e38])
 @pytest.mark.parametrize("heads,n", [((2, 1), 100), ((32, 16), 600)])
 def test_hidden_values_reach_no_row(dtype, value, heads, n):

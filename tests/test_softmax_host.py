@@ -142,7 +142,7 @@ def _soft_bwd(lib, at, wsb=1 << 24, **kw):
     (dict(n_batch=0), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID),
     (dict(kv_heads=3), INVALID), (dict(dk=0), INVALID), (dict(dv=0), INVALID),
     (dict(dtype=9), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
-    (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(dk=129), UNSUPPORTED), (dict(dv=129), UNSUPPORTED), (dict(splits=None), INVALID),
     (dict(k_splits=None), INVALID), (dict(heads=65536), UNSUPPORTED),
     (dict(n=1 << 30), UNSUPPORTED), (dict(m=1 << 30), UNSUPPORTED), (dict(wsb=8, n=4000, m=4000), WORKSPACE),
