@@ -736,11 +736,12 @@ sbc_status sbc_qk_norm_rotary_backward(const sbc_rotary_plan *plan, const sbc_he
  * Scores, maxima and sums are float32.  Products are taken on the matrix cores, of float32
  * inputs with operands split into three bf16 parts (products up to 2^-22 of the whole left
  * out); of bf16 inputs, the weights are rounded to bf16 (2^-8 each) on their way to the
- * product with v, as are the terms of the gradients' products.
+ * products that give o and dv, and dS has two parts (2^-17).
  * A NaN or infinity reaches no other sequence and no row that does not see it; an infinity
  * may come out as NaN.  (The gradients: no other sequence; within one, tokens up to 256 before
  * and behind may share it.)
  * No output may overlap an input.  The same call gives the same results, bit by bit.
+ * A workspace of 0 bytes may be NULL.
  * ------------------------------------------------------------------------ */
 typedef struct {
     int32_t n, m, n_batch, heads, kv_heads, dk, dv;

@@ -216,12 +216,11 @@ __device__ __forceinline__ void frag_col32(const bf16_t *tile, int plane, int s,
         out[i] = __builtin_bit_cast(bf16x8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     }
 }
-// Registers 8 h .. + 7 of a product as an operand of the next: keys 16 h + 4 g .. + 3 and
-// 16 h + 8 + 4 g .. + 3 of its 32.  A bf16 call's weights are rounded to bf16 here (2^-8 of
-// each, independent ones, beside the output's own 2^-8).
-template <typename T>
-__device__ __forceinline__ void frag_regs(const floatx16 &x, int h, bf16x8 (&out)[kParts<T>]) {
-    if constexpr (sizeof(T) == 2) {
+// Registers 8 h .. + 7 of a product as an operand of the next, in N parts: keys 16 h + 4 g .. + 3
+// and 16 h + 8 + 4 g .. + 3 of its 32.
+template <int N>
+__device__ __forceinline__ void frag_regs(const floatx16 &x, int h, bf16x8 (&out)[N]) {
+    if constexpr (N == 1) {
         u32x4v w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
@@ -230,7 +229,7 @@ __device__ __forceinline__ void frag_regs(const floatx16 &x, int h, bf16x8 (&out
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[8 * h + i];
-        split8<3>(y, out);
+        split8<N>(y, out);
     }
 }
 
@@ -601,8 +600,11 @@ __device__ __forceinline__ void row_products(Read read, Operand operand, floatx1
 
 // acc[t] += columns 32 t .. + 31 of the tile, transposed, times weights by rows: k-step h takes
 // rows 16 h .. + 15.  First read(), which may lie well before, then add().
-// kBuffers: steps that are in registers at once, 2 or 1.
-template <typename T, int D, int kRows, int kBuffers = 2> struct ColumnProducts {
+// kBuffers: steps that are in registers at once, 2 or 1.  kWeights: the weights' parts.  A bf16
+// call's softmax weights have one: each is rounded by up to 2^-8, independently of the others,
+// beside the output's own rounding of as much.
+template <typename T, int D, int kRows, int kBuffers = 2, int kWeights = kParts<T>>
+struct ColumnProducts {
     static constexpr int NP = kParts<T>, kSteps = kRows / 16;
     bf16x8 f[kBuffers][D / 32][NP];
     // step h of the rows that begin `first` (a multiple of 32) into a tile
@@ -624,11 +626,11 @@ template <typename T, int D, int kRows, int kBuffers = 2> struct ColumnProducts 
 #pragma unroll
         for (int h = 0; h < kSteps; ++h) {
             if (kBuffers == 2 && h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
-            bf16x8 w[NP];
-            frag_regs<T>(x[h / 2], h % 2, w);
+            bf16x8 w[kWeights];
+            frag_regs<kWeights>(x[h / 2], h % 2, w);
             keep_order();
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) mma32<NP, NP>(f[h % kBuffers][t], w, acc[t]);
+            for (int t = 0; t < D / 32; ++t) mma32<NP, kWeights>(f[h % kBuffers][t], w, acc[t]);
             keep_order();
             if (kBuffers == 1 && h + 1 < kSteps) fetch(tile, plane, first, at, h + 1);
         }

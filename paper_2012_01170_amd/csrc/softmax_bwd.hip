@@ -2,11 +2,11 @@
 #include "softmax_grad.hpp"
 #include "softmax_host.hpp"
 
-
 namespace sbc {
 namespace {
 
-// Parts of the rows for dk and dv: as many as give every CU two workgroups
+// Parts of the rows for dk and dv: as many as give every CU three workgroups, of 128 rows or more
+// (a causal sequence's first keys are seen by all rows, its last by few)
 int32_t grad_parts(const sbc_softmax_attention *a) {
     const int64_t tiles = ((int64_t)a->m / kGradCols + a->n_batch) * a->kv_heads;
     const int64_t rows = (int64_t)a->n * (a->heads / a->kv_heads) / (a->n_batch > 0 ? a->n_batch : 1);
@@ -15,7 +15,7 @@ int32_t grad_parts(const sbc_softmax_attention *a) {
     if (parts > 16) parts = 16;
     return parts < 1 ? 1 : (int32_t)parts;
 }
-// One launch for all: while its workgroups are few
+// One launch for all: while its workgroups are all on the CUs at once
 bool grads_joint(const sbc_softmax_attention *a) {
     const int64_t rows = softmax_places(a, 128), keys = (int64_t)a->m / kGradCols + a->n_batch;
     return a->n > 0 && a->m > 0 && (rows + 2 * keys * grad_parts(a)) * a->kv_heads <= 2 * device_cus();

@@ -12,6 +12,11 @@ namespace sbc {
 
 constexpr int kGradThreads = 256;
 
+// dS' parts: of a bf16 call two (2^-17).  Its terms cancel in dq and dk, so that with one the
+// roundings, 2^-8 of each, were up to 1.5 times what the outputs' own rounding leaves (dq of drawn
+// problems: 2.6e-3 from float64 where rounding alone gives 1.8e-3).
+template <typename T> constexpr int kGradParts = sizeof(T) == 4 ? 3 : 2;
+
 // dq: a workgroup has 128 rows, 32 a wave, as softmax_tile_kernel.
 template <typename T, int D> constexpr int kGradKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
 // Waves a SIMD: the rows' operands and sums of wide heads in float32 fill its registers alone
@@ -130,7 +135,7 @@ __device__ __forceinline__ void row_grads(const SoftmaxArgs &p, int32_t block,
                     frag_row32<D, NP>(j ? vt : kt, kPlane, u, k, at, f);
                 },
                 [&](int k, int j) -> const bf16x8(&)[NP] { return j ? g[k] : q[k]; }, w);
-            ColumnProducts<T, D, 32> keys;
+            ColumnProducts<T, D, 32, 2, kGradParts<T>> keys;
             keys.read(kt, kPlane, 32 * u, at);
             const bool masked = k0 + 32 * u + 32 > wave_least;
             const uint32_t seen = masked ? seen_bits(~0ull, 0, limit - k0 - 32 * u) : ~0u;
@@ -168,8 +173,9 @@ __global__ __launch_bounds__(kGradThreads, (kGradWaves<T, D>)) void softmax_dq_k
 //
 // Where both sums and operands fit into half of a SIMD's registers, a workgroup makes both
 // (kDk | kDv); else one half of the workgroups makes dk and the other dv, scores twice: a wave alone on
-// its SIMD, without another's products to fill its waits, took longer (16384 tokens, 2 key heads
-// of 128 bf16 channels: 1760 us against GRADSPLIT).
+// its SIMD, without another's products to fill its waits, took longer (16384 tokens of 8 heads, 2
+// key heads, of 128 bf16 channels, both from registers: 1760 .. 1890 us against 1700 .. 1730;
+// with keys and values in LDS and 8 waves, 1600 .. 1670, with DirectTile apart, 1500 .. 1540).
 constexpr int kGradCols = 128;
 constexpr int kDk = 1, kDv = 2;
 template <typename T, int D> constexpr int kGradRows = D > 64 || (sizeof(T) == 4 && D > 32) ? (D == 96 ? 64 : 32) : 64;
@@ -184,7 +190,7 @@ template <typename T, int D, int kBuffers = 1> struct KeyGradShared {
 // kOwnDelta: delta is made here from o, by 256 / RB neighbouring lanes a row.
 // kDirect: whole tiles of rows go straight to LDS, two ahead, in three buffers: registers of
 // a tile on its way reach one tile ahead only, which is less than a load takes (16384 tokens, 2
-// key heads of 128 bf16 channels: DIRECTTIME).
+// key heads of 128 bf16 channels: 1720 -> 1536 us).
 template <typename T, int D, bool kWhole, int kGrads, bool kOwnDelta, bool kDirect = false>
 __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
                                           KeyGradShared<T, D, (kDirect ? 3 : 1)> &lds) {
@@ -383,7 +389,8 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
                     frag_row32<D, NP>(j ? gt : qt, kPlane, u, k, at, f);
                 },
                 [&](int k, int j) -> const bf16x8(&)[NP] { return j ? vf[k] : kf[k]; }, w);
-            ColumnProducts<T, D, 32, (NP == 3 ? 1 : 2)> grads, queries;
+            ColumnProducts<T, D, 32, (NP == 3 ? 1 : 2)> grads;
+            ColumnProducts<T, D, 32, (NP == 3 ? 1 : 2), kGradParts<T>> queries;
             if constexpr (kDoV) grads.read(gt, kPlane, 32 * u, at);
             else queries.read(qt, kPlane, 32 * u, at);
             const bool masked = first < wave_key + 32 || r0 + 32 * u + 32 > rows;
@@ -459,7 +466,7 @@ __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_d
 
 // All three in one launch, for small problems, where a launch is most of the time: dq's
 // workgroups first, each of the others making the deltas that it needs (8 tokens of 4 heads of 64
-// bf16 channels: GRADSJOINT).
+// bf16 channels: 20 us a call with two launches, 16 with one).
 template <typename T, int D, bool kWhole>
 __global__ __launch_bounds__(kGradThreads, (kKeyGradWaves<T, D>)) void softmax_grads_kernel(
     SoftmaxArgs p, int32_t dq_blocks, int32_t dkv_blocks) {

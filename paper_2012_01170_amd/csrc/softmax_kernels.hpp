@@ -28,7 +28,15 @@ __device__ __forceinline__ int32_t part_keys(int32_t lk, int32_t parts) {
 
 // ---------------------------------------------------------------- many rows
 // A workgroup has 128 rows, 32 a wave, and goes through the keys that they see in tiles,
-// which its waves share in LDS; the next tile is on its way into registers meanwhile.
+// which its waves share in LDS.  The next tile is on its way into registers meanwhile; or
+// (kDirect, whole bf16 pieces) two tiles straight to LDS, in three buffers: 32768 events of 4 heads
+// of 64 channels 655 -> 630 us, 32 prompts of some 1024 tokens, 8 heads of 128, 125 -> 121.
+//
+// The vector ALU bounds it with the matrix cores: a tile of 64 keys of 64 channels takes a wave 512
+// cycles of products and some 800 of exponentials (8 cycles each), sums and conversions.  A SIMD
+// overlaps those of different waves only as they happen to meet (39 % and 62 % of its time at two
+// and three waves); making the next tile's scores between this one's exponentials, in one wave,
+// took more registers than it gave (746 us), as did four waves of 32 keys at once (710).
 template <typename T, int D, bool kWhole, bool kPaged, bool kDirect = false>
 __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_tile_kernel(SoftmaxArgs p) {
     constexpr int NP = kParts<T>, KB = kDirect && D > 64 ? 32 : kTileKeys<T, D>, kPlane = KB * D;

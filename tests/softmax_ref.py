@@ -97,11 +97,12 @@ def attention(q, k, v, splits, k_splits, scale, causal, u=0.0):
 
 def attention_grad(do, q, k, v, o, lse, splits, k_splits, scale, causal, u=0.0):
     """((dq, dk, dv), their tolerances) from the given o and lse; tolerances as above, dO v and
-    dO o off by 2^-18 of their terms' magnitudes, and both operands (weights, and their
-    gradients) rounded to u."""
+    dO o off by 2^-18 of their terms' magnitudes; weights rounded to u, and their gradients, in
+    two parts where those are, to 2^-16."""
     do, q, k, v, o, lse = (x.astype(np.float64) for x in (do, q, k, v, o, lse))
     H = q.shape[1]
     group = H // k.shape[1]
+    us = 2.0 ** -16 if u else 0.0
     out = [np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)]
     tol = [np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)]
     for a, b, c, d in zip(splits, splits[1:], k_splits, k_splits[1:]):
@@ -119,7 +120,7 @@ def attention_grad(do, q, k, v, o, lse, splits, k_splits, scale, causal, u=0.0):
             mag = p * (np.abs(G) @ np.abs(V).T + np.abs(G * O).sum(1, keepdims=True))
             rel = 2.0 ** -18 * size + 2.0 ** -20 * (1 + np.abs(np.where(seen, s, 0.0)) + np.abs(ls))
             full = seen * (np.abs(G) @ np.abs(V).T + np.abs(G * O).sum(1, keepdims=True) + 1)
-            err = np.abs(ds) * (rel + u) + mag * (2.0 ** -18 + rel * u) + TINY * full
+            err = np.abs(ds) * (rel + us) + mag * (2.0 ** -18 + rel * us) + TINY * full
             out[0][a:b, h] += scale * ds @ K
             out[1][c:d, g] += scale * ds.T @ Q
             out[2][c:d, g] += p.T @ G
