@@ -13,6 +13,11 @@ int32_t grad_parts(const sbc_softmax_attention *a) {
     int64_t parts = ((int64_t)3 * device_cus() + tiles - 1) / (tiles > 0 ? tiles : 1);
     if (parts > rows / 128) parts = rows / 128;
     if (parts > 16) parts = 16;
+    // so many that each of the 8 XCDs has key heads and parts, and their rows, of its own
+    int32_t even = 8;
+    while (even > 1 && a->kv_heads % (8 / even * 2) == 0) even /= 2;
+    const int64_t up = (parts + even - 1) / even * even;
+    if (parts > 1 && up <= 2 * parts && up <= 16) parts = up;
     return parts < 1 ? 1 : (int32_t)parts;
 }
 // One launch for all: while its workgroups are all on the CUs at once
