@@ -730,7 +730,7 @@ sbc_status sbc_qk_norm_rotary_backward(const sbc_rotary_plan *plan, const sbc_he
  *              sequence are left as they were
  *   q [n, heads, dk], k [m, kv_heads, dk], v [m, kv_heads, dv], o [n, heads, dv]:
  *              float32 or bf16 (dtype), 1 <= dk, dv <= 128, heads <= 65535,
- *              n heads and m kv_heads below 2^31
+ *              n heads and m kv_heads at most 2^31 - 1024
  *   lse        [n, heads] float32, or NULL: not wanted
  *   scale      > 0 and below 2e38
  * Scores, maxima and sums are float32.  Products are taken on the matrix cores, of float32
@@ -778,7 +778,7 @@ sbc_status sbc_softmax_attention_backward(const sbc_softmax_attention *a, const 
  * sbc_softmax_attention_paged: section 15's attention, causal, of n new tokens over the
  * streams' kept tokens, the new ones among them (m, k_splits and causal are not read).
  *   table      [n_batch, width] int32, lengths [n_batch] int32: tokens that a stream has,
- *              with the new ones (taken as 0 .. width * page)
+ *              with the new ones (taken as 0 .. width * page, and 2^31 - 1024 at most)
  *   splits     of the new tokens; NULL: one for each stream (n = n_batch)
  * Keys on a page outside 0 .. n_pages-1 are left out.
  *

@@ -46,6 +46,9 @@ __device__ __forceinline__ int32_t divide(int32_t n, const Divisor &by) {
 }
 
 // ---------------------------------------------------------------- arguments
+// Rows and keys are counted in 32 bits, up to a few tiles past the last
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1024;
+
 struct SoftmaxPages {  // a paged cache, in place of k, v and k_splits
     sbc_pages k, v;
     int32_t n_pages, width;
@@ -117,7 +120,7 @@ struct Sequence {
     int32_t b, q0, lq, k0, lk;
     // keys that the token sees: causal, the last token sees the last key
     __device__ __forceinline__ int32_t limit(int32_t token, int32_t causal) const {
-        return causal ? clamp_i(token + lk - lq + 1, 0, lk) : lk;
+        return causal ? clamp_i(token - lq + lk + 1, 0, lk) : lk;
     }
 };
 template <bool kPaged>
@@ -130,7 +133,7 @@ __device__ __forceinline__ Sequence sequence_at(const SoftmaxArgs &p, int32_t b)
     if constexpr (kPaged) {
         const int64_t room = (int64_t)p.pages.width * p.pages.page.d;
         s.k0 = 0;
-        s.lk = clamp_i(p.pages.lengths[b], 0, room > INT32_MAX ? INT32_MAX : (int32_t)room);
+        s.lk = clamp_i(p.pages.lengths[b], 0, room > kMostRows ? (int32_t)kMostRows : (int32_t)room);
     } else {
         s.k0 = k_split(p, b);
         s.lk = k_split(p, b + 1) - s.k0;

@@ -21,9 +21,8 @@ inline sbc_status check_softmax(const sbc_softmax_attention *a) {
     if (a->dk > 128 || a->dv > 128)
         return fail(SBC_ERR_UNSUPPORTED, "dk and dv must be <= 128");
     if (a->heads > 65535) return fail(SBC_ERR_UNSUPPORTED, "heads must be <= 65535");
-    if ((int64_t)a->n * a->heads >= (int64_t)1 << 31 ||
-        (int64_t)a->m * a->kv_heads >= (int64_t)1 << 31)
-        return fail(SBC_ERR_UNSUPPORTED, "n * heads and m * kv_heads must be below 2^31");
+    if ((int64_t)a->n * a->heads > kMostRows || (int64_t)a->m * a->kv_heads > kMostRows)
+        return fail(SBC_ERR_UNSUPPORTED, "n * heads and m * kv_heads must be <= 2^31 - 1024");
     return SBC_OK;
 }
 // Sequences of keys that lie in one array

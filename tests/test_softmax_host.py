@@ -145,7 +145,9 @@ def _soft_bwd(lib, at, wsb=1 << 24, **kw):
     (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(dk=129), UNSUPPORTED), (dict(dv=129), UNSUPPORTED), (dict(splits=None), INVALID),
     (dict(k_splits=None), INVALID), (dict(heads=65536), UNSUPPORTED),
-    (dict(n=1 << 30), UNSUPPORTED), (dict(m=1 << 30), UNSUPPORTED), (dict(wsb=8, n=4000, m=4000), WORKSPACE),
+    (dict(n=1 << 30), UNSUPPORTED), (dict(m=1 << 30), UNSUPPORTED),
+    (dict(heads=1, kv_heads=1, n=2 ** 31 - 1000), UNSUPPORTED),
+    (dict(heads=1, kv_heads=1, m=2 ** 31 - 1), UNSUPPORTED), (dict(wsb=8, n=4000, m=4000), WORKSPACE),
 ])
 def test_attention_refusals(lib, call, kw, status):
     assert call(lib, _soft_at(), **kw) == status and lib.sbc_last_error() != b""
