@@ -119,8 +119,8 @@ __device__ __forceinline__ void row_grads(const SoftmaxArgs &p, int32_t block,
     if (most > 0) fetch(0);
     for (int32_t k0 = 0; k0 < most; k0 += KB) {
         __syncthreads();
-        sk.settle();
-        sv.settle();
+        sk.settle(p.dk);
+        sv.settle(p.dv);
         sk.store(kt);
         sv.store(vt);
         __syncthreads();
@@ -260,8 +260,8 @@ __device__ __forceinline__ void key_grads(const SoftmaxArgs &p, int32_t block,
         }
     }
     auto put_tile = [&](bf16_t *buffer) {
-        sq.settle();
-        sg.settle();
+        sq.settle(p.dk);
+        sg.settle(p.dv);
         sq.store(buffer);
         sg.store(buffer + NP * kPlane);
     };

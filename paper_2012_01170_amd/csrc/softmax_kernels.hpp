@@ -97,8 +97,8 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     KeyPlaces where;  // of the tile that is fetched next
     uint64_t known = kAll, next_known = kAll;
     auto put_tile = [&](int32_t k0, bf16_t *buffer) {
-        sk.settle();
-        sv.settle();
+        sk.settle(p.dk);
+        sv.settle(p.dv);
         if (k0 + KB > least) sv.put_bad_apart(k0, first_bad);
         sk.store(buffer);
         sv.store(buffer + NP * kPlane);
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)
             raw_parts<T>(kraw[k], f);
             mma32<NP, NP>(f, q[k], w[0]);
         }
-        sv.settle();
+        sv.settle(p.dv);
         if (k0 + 32 > least) sv.put_bad_apart(k0, first_bad);
         sv.store(vt);
         known = next_known;
