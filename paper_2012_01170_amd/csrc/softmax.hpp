@@ -99,20 +99,30 @@ __device__ __forceinline__ int32_t k_split(const SoftmaxArgs &p, int32_t b) {
 // no sum over the sequences' tiles is needed to launch or to find them.  The last b in
 // [0, n_batch) whose places begin at or before x, -1 if none; 64 lanes look at 64 places
 // of the range at once.
-template <typename F>
-__device__ __forceinline__ int32_t sequence_of(int32_t n_batch, int32_t x, F begin) {
+//
+// begins(lo, step, hi): a bit for each b = lo + lane * step below hi that begins at or before x.
+// The range goes on behind the last bit of those that hold from the first on, so that the
+// result is a b that was seen to begin there, also where splits are not in order.  (By the
+// number of bits it could be one that begins behind x, and a tile's rows negative.)
+template <typename F> constexpr int32_t last_beginning(int32_t n_batch, F begins) {
     int32_t lo = 0, hi = n_batch;
     while (lo < hi) {
         const int32_t step = (hi - lo + 63) / 64;
-        const int64_t b = lo + (int64_t)(threadIdx.x & 63) * step;
-        const bool before = b < hi && begin((int32_t)b) <= x;
-        const int32_t c = __popcll(__ballot(before));
+        const uint64_t bits = begins(lo, step, hi);
+        const int32_t c = bits == ~0ull ? 64 : __builtin_ctzll(~bits);
         if (c == 0) break;
         const int64_t up = lo + (int64_t)c * step;
         lo += (c - 1) * step + 1;
         hi = up < hi ? (int32_t)up : hi;
     }
     return lo - 1;
+}
+template <typename F>
+__device__ __forceinline__ int32_t sequence_of(int32_t n_batch, int32_t x, F begin) {
+    return last_beginning(n_batch, [&](int32_t lo, int32_t step, int32_t hi) -> uint64_t {
+        const int64_t b = lo + (int64_t)(threadIdx.x & 63) * step;
+        return __ballot(b < hi && begin((int32_t)b) <= x);
+    });
 }
 
 // One sequence's tokens and keys

@@ -1,0 +1,57 @@
+"""Softmax attention on the GPU where its arithmetic can go wrong: splits out of order, sizes next
+to 2^31, values next to the largest, and the paths that only larger batches take."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2012_01170_amd import _lib as L
+from tests.test_gpu_softmax import BF16, DEV, F32, _ints, _rand
+
+pytestmark = pytest.mark.gpu
+
+
+def _heads(x):
+    return ctypes.byref(L.SbcHeads(x.data_ptr(), x.stride(0), x.stride(1)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,splits", [((2, 1), [0, 640, 0, 0, 0, 1000]),
+                                          ((16, 8), [0, 900, 3, 0, 1000, 0, 700, 1000]),
+                                          ((2, 2), [1000, 0, 2000, -5, 500])])
+def test_splits_out_of_order(heads, splits, dtype):
+    """Whatever the splits hold, no row in front of or behind the arrays is written."""
+    print(f"[splits] {heads} {splits} {dtype}", flush=True)
+    rng = np.random.default_rng(20)
+    (hq, hk), n, d, edge = heads, 1000, 64, 300
+
+    def guarded(h):
+        return torch.full((n + 2 * edge, h, d), 5.0, dtype=dtype, device=DEV)
+
+    q, do, k, v = (_rand(rng, (n, h, d), dtype) for h in (hq, hq, hk, hk))
+    outs = [guarded(h) for h in (hq, hq, hk, hk)]
+    o, dq, dk, dv = (x[edge:edge + n] for x in outs)
+    lse_all = torch.full((n + 2 * edge, hq), 5.0, device=DEV)
+    lse = lse_all[edge:edge + n]
+    lib = L.lib()
+    at = _ints(splits)
+    for causal in (0, 1):
+        a = L.SbcSoftmaxAttention(n, n, len(splits) - 1, hq, hk, d, d,
+                                  L.SBC_F32 if dtype == F32 else L.SBC_BF16, 0.2, causal,
+                                  at.data_ptr(), None)
+        ref = ctypes.byref(a)
+        size = max(lib.sbc_softmax_attention_workspace_size(ref),
+                   lib.sbc_softmax_attention_backward_workspace_size(ref))
+        # (rows that lie in no sequence leave their places in the workspace unwritten)
+        ws = torch.zeros(size + 512, dtype=torch.uint8, device=DEV)
+        stream = torch.cuda.current_stream().cuda_stream
+        L.check(lib.sbc_softmax_attention_forward(ref, _heads(q), _heads(k), _heads(v), _heads(o),
+                                                  lse.data_ptr(), ws.data_ptr(), size, stream))
+        L.check(lib.sbc_softmax_attention_backward(
+            ref, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), lse.data_ptr(), _heads(dq),
+            _heads(dk), _heads(dv), ws.data_ptr(), size, stream))
+        torch.cuda.synchronize()
+        for x in (*outs, lse_all):
+            assert bool((x[:edge] == 5).all()) and bool((x[edge + n:] == 5).all())
+        assert not bool(ws[size:].any())

@@ -1,0 +1,79 @@
+"""Softmax attention's index arithmetic that the compiler can check without a GPU: the headers
+are compiled for the host with static assertions (in a constant expression an overflow of int32
+is an error)."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+
+
+def host_compile(tmp_path, body):
+    src = tmp_path / "check.hip"
+    src.write_text('#include "paper_2012_01170_amd/csrc/softmax_kernels.hpp"\nusing namespace sbc;\n'
+                   + body)
+    return subprocess.run([HIPCC, "-std=c++17", f"-I{ROOT}", "--offload-arch=gfx950",
+                           "--cuda-host-only", "-fsyntax-only", str(src)],
+                          capture_output=True, text=True, timeout=300)
+
+
+needs_hipcc = pytest.mark.skipif(not (os.path.exists(HIPCC) or shutil.which(HIPCC)),
+                                 reason="hipcc is not installed")
+
+
+@needs_hipcc
+def test_search_over_splits(tmp_path):
+    """The sequence that a place belongs to: the last that begins at or before it where splits
+    are in order, and where they fall one that does, so that no tile begins before its rows."""
+    r = host_compile(tmp_path, """
+constexpr int32_t kN = 300;  // sequences, in up to two rounds of 64 lanes
+struct Splits { int32_t at[kN + 1]; };
+constexpr int32_t begin(const Splits &s, int32_t group, int32_t b) {
+    return (int32_t)((int64_t)s.at[b] * group / 128) + b;
+}
+constexpr int32_t find(const Splits &s, int32_t group, int32_t n, int32_t x) {
+    return last_beginning(n, [&](int32_t lo, int32_t step, int32_t hi) {
+        uint64_t bits = 0;
+        for (int lane = 0; lane < 64; ++lane) {
+            const int64_t b = lo + (int64_t)lane * step;
+            if (b < hi && begin(s, group, (int32_t)b) <= x) bits |= (uint64_t)1 << lane;
+        }
+        return bits;
+    });
+}
+// whether every place's sequence begins at or before it, or is the last such one (`last`)
+constexpr bool holds(const Splits &s, int32_t group, int32_t n, int32_t places, bool last) {
+    for (int32_t x = 0; x < places; ++x) {
+        const int32_t b = find(s, group, n, x);
+        if (b < -1 || b >= n || (b >= 0 && begin(s, group, b) > x)) return false;
+        if (!last) continue;
+        int32_t want = -1;
+        for (int32_t i = 0; i < n && begin(s, group, i) <= x; ++i) want = i;
+        if (b != want) return false;
+    }
+    return true;
+}
+constexpr Splits kFall{{0, 12800, 0, 0, 0, 20000}};
+static_assert(holds(kFall, 2, 5, 330, false), "splits that fall, 5 sequences");
+static_assert(find(kFall, 2, 5, 2) == 0, "place 2 of them");
+constexpr Splits mixed() {
+    Splits s{};
+    uint32_t r = 1;
+    for (int i = 0; i <= kN; ++i) s.at[i] = (r = r * 1664525u + 1013904223u) >> 18;
+    return s;
+}
+static_assert(holds(mixed(), 3, kN, 90, false), "splits in no order, 300 sequences");
+constexpr Splits rising() {
+    Splits s{};
+    for (int i = 1; i <= kN; ++i) s.at[i] = s.at[i - 1] + (i % 7 == 0 ? 0 : i % 5 * 9);
+    return s;
+}
+static_assert(holds(rising(), 2, kN, 90, true) && holds(rising(), 5, kN, 120, true) &&
+              holds(rising(), 1, 64, 70, true) && holds(rising(), 1, 65, 70, true) &&
+              holds(rising(), 1, 1, 9, true), "splits in order");
+static_assert(find(rising(), 2, 0, 3) == -1, "no sequence");
+""")
+    assert r.returncode == 0, r.stderr
