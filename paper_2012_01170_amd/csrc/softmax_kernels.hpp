@@ -22,8 +22,13 @@ constexpr int kFewRows = 32;    // of softmax_rows_kernel
 
 // A sequence's keys in p.parts parts: as even ones as multiples of 128 keys (a round of the
 // four waves of softmax_rows_kernel) allow
-__device__ __forceinline__ int32_t part_keys(int32_t lk, int32_t parts) {
+constexpr int32_t part_keys(int32_t lk, int32_t parts) {
     return (int32_t)(((int64_t)lk + parts - 1) / parts + 127) / 128 * 128;
+}
+// Where the keys of a part that begins at `first` end, of those up to `limit` (the last part's
+// first + size may lie past 2^31)
+constexpr int32_t part_end(int32_t first, int32_t size, int32_t limit) {
+    return limit - first > size ? first + size : limit;
 }
 
 // ---------------------------------------------------------------- many rows
@@ -73,7 +78,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
     // the part's keys
     const int32_t size = p.parts > 1 ? part_keys(s.lk, p.parts) : s.lk;
     const int32_t first = part * size;
-    const int32_t end = p.parts > 1 && most > first + size ? first + size : most;
+    const int32_t end = p.parts > 1 ? part_end(first, size, most) : most;
     if (part > 0 && first >= most) return;  // (softmax_join_kernel knows)
     const int32_t wave_least = __builtin_amdgcn_readfirstlane(limit_of(wave_row));
 
@@ -263,7 +268,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)
     const int32_t most = __builtin_amdgcn_readfirstlane(limit_of(r0 + kFewRows - 1));
     const int32_t size = p.parts > 1 ? part_keys(s.lk, p.parts) : s.lk;
     const int32_t first = part * size;
-    const int32_t end = p.parts > 1 && most > first + size ? first + size : most;
+    const int32_t end = p.parts > 1 ? part_end(first, size, most) : most;
     if (part > 0 && first >= most) return;  // (softmax_join_kernel knows)
 
     bf16x8 q[D / 16][NP];

@@ -2,10 +2,13 @@
 to 2^31, values next to the largest, and the paths that only larger batches take."""
 import ctypes
 
+import math
+
 import numpy as np
 import pytest
 import torch
 
+import paper_2012_01170_amd as sbc
 from paper_2012_01170_amd import _lib as L
 from tests.test_gpu_softmax import BF16, DEV, F32, _ints, _rand
 
@@ -55,3 +58,20 @@ def test_splits_out_of_order(heads, splits, dtype):
         for x in (*outs, lse_all):
             assert bool((x[:edge] == 5).all()) and bool((x[edge + n:] == 5).all())
         assert not bool(ws[size:].any())
+
+
+MOST = 2 ** 31 - 1024  # keys that a call takes
+
+
+@pytest.mark.parametrize("m", [MOST])
+def test_most_keys(m):
+    """The same key and value over and over (stride 0): one row's lse counts them all.  A lane's
+    sum is below 2^24 ones, and exact."""
+    print(f"[most keys] {m}", flush=True)
+    q = torch.full((1, 1, 16), 0.5, device=DEV, dtype=BF16)
+    k = torch.full((1, 1, 16), 0.25, device=DEV, dtype=BF16).expand(m, 1, 16)
+    v = torch.linspace(-1, 1, 17, device=DEV)[1:].to(BF16)[None, None].expand(m, 1, 16)
+    o, lse = sbc.softmax_attention_forward(q, k, v, scale=1.0)
+    want = 16 * 0.5 * 0.25 + math.log(m)
+    # (float32's half unit of lse and of its parts, in units of log 2: 2^-19 each)
+    assert abs(float(lse[0, 0]) - want) < 2.0 ** -17

@@ -77,3 +77,40 @@ static_assert(holds(rising(), 2, kN, 90, true) && holds(rising(), 5, kN, 120, tr
 static_assert(find(rising(), 2, 0, 3) == -1, "no sequence");
 """)
     assert r.returncode == 0, r.stderr
+
+
+# lengths next to the most keys that a call takes, and whether the parts of `lk` keys cover those up
+# to `limit` once each
+PARTS = """
+constexpr int32_t kMost = (int32_t)kMostRows;
+static_assert(kMostRows == 2147482624, "keys that a call takes");
+constexpr bool covers(int32_t lk, int32_t parts, int32_t limit) {
+    const int32_t size = part_keys(lk, parts);
+    int32_t next = 0;
+    for (int32_t part = 0; part < parts; ++part) {
+        const int32_t first = part * size;
+        if (part > 0 && first >= limit) break;
+        const int32_t end = part_end(first, size, limit);
+        if (first != next || end < first) return false;
+        next = end;
+    }
+    return next == limit;
+}
+constexpr int32_t kNear[] = {0, 1, 127, 128, 129, 5000, 1440000000, 2120000000, kMost - 8192, kMost - 8191,
+                             kMost - 129, kMost - 128, kMost - 1, kMost};
+"""
+
+
+@needs_hipcc
+def test_parts_cover_the_keys(tmp_path):
+    r = host_compile(tmp_path, PARTS + """
+constexpr bool all() {
+    for (int32_t parts = 2; parts <= 64; ++parts)
+        for (int32_t lk : kNear)
+            for (int32_t limit : kNear)
+                if (limit <= lk && !covers(lk, parts, limit)) return false;
+    return true;
+}
+static_assert(all(), "each key is in one part");
+""")
+    assert r.returncode == 0, r.stderr
