@@ -30,6 +30,10 @@ constexpr int32_t part_keys(int32_t lk, int32_t parts) {
 constexpr int32_t part_end(int32_t first, int32_t size, int32_t limit) {
     return limit - first > size ? first + size : limit;
 }
+// Parts that hold keys below `limit`
+constexpr int32_t parts_below(int32_t limit, int32_t size) {
+    return limit > 0 ? (limit - 1) / size + 1 : 0;
+}
 
 // ---------------------------------------------------------------- many rows
 // A workgroup has 128 rows, 32 a wave, and goes through the keys that they see in tiles,
@@ -446,7 +450,7 @@ __global__ __launch_bounds__(256) void softmax_join_kernel(SoftmaxArgs p) {
     for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
     const float w = lse2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lse2 - top);
     const float total = group_sum<64>(w);
-    const int32_t parts = size > 0 ? (limit + size - 1) / size : 0;
+    const int32_t parts = parts_below(limit, size);
     float y[2] = {0.f, 0.f};
     const int c = 2 * lane;
 #pragma unroll 8

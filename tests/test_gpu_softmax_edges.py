@@ -75,3 +75,29 @@ def test_most_keys(m):
     want = 16 * 0.5 * 0.25 + math.log(m)
     # (float32's half unit of lse and of its parts, in units of log 2: 2^-19 each)
     assert abs(float(lse[0, 0]) - want) < 2.0 ** -17
+
+
+@pytest.mark.parametrize("m", [1_500_000_000, 2_120_000_000, MOST])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_most_keys_values(m, dtype):
+    """Their mean is the value itself: of each wave's sums (exact, of ones times a value of 8 bits)
+    and their joins a few roundings are left, of 2^-24, and the output's."""
+    print(f"[most keys, values] {m} {dtype}", flush=True)
+    one = torch.full((1, 1, 16), 0.25, device=DEV, dtype=dtype)
+    v = torch.linspace(-1, 1, 17, device=DEV)[1:].to(dtype)[None, None].expand(m, 1, 16)
+    o, lse = sbc.softmax_attention_forward(2 * one, one.expand(m, 1, 16), v, scale=1.0)
+    assert bool(((o - v[:1]).float().abs() <= 2.0 ** -20 * v[:1].float().abs()).all())
+    assert abs(float(lse[0, 0]) - 2 - math.log(m)) < 2.0 ** -17
+
+
+def test_most_kept_tokens():
+    """A stream whose table names one page over and over"""
+    page, width = 1 << 20, 1 << 11
+    print(f"[most kept] {page} {width}", flush=True)
+    k = torch.full((1, 1, 1, 16), 0.25, device=DEV, dtype=BF16).expand(1, page, 1, 16)
+    v = torch.linspace(-1, 1, 17, device=DEV)[1:].to(BF16)[None, None, None].expand(1, page, 1, 16)
+    q = torch.full((1, 1, 16), 0.5, device=DEV, dtype=BF16)
+    table = torch.zeros((1, width), dtype=torch.int32, device=DEV)
+    for n in (2_120_000_000, MOST, 2 ** 31 - 1):
+        o = sbc.softmax_attention_paged(q, k, v, table, _ints([n]), scale=1.0)
+        assert torch.equal(o, v[0, :1])

@@ -114,3 +114,24 @@ constexpr bool all() {
 static_assert(all(), "each key is in one part");
 """)
     assert r.returncode == 0, r.stderr
+
+
+@needs_hipcc
+def test_parts_are_counted(tmp_path):
+    """The parts that are joined: those that begin below a row's limit."""
+    r = host_compile(tmp_path, PARTS + """
+constexpr bool all() {
+    for (int32_t parts = 2; parts <= 64; ++parts)
+        for (int32_t lk : kNear)
+            for (int32_t limit : kNear) {
+                if (limit > lk) continue;
+                const int32_t size = part_keys(lk, parts);
+                int32_t want = 0;
+                while (want < parts && (int64_t)want * size < limit) ++want;
+                if (parts_below(limit, size) != want) return false;
+            }
+    return true;
+}
+static_assert(all(), "the parts that begin below the limit");
+""")
+    assert r.returncode == 0, r.stderr
