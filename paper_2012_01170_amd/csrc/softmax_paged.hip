@@ -4,8 +4,15 @@
 namespace sbc {
 namespace {
 
-sbc_status check_paged(const sbc_softmax_attention *a, int32_t n_pages, int32_t page,
-                       int32_t width) {
+// Fields that the call does not read are taken as 0 from here on
+sbc_status check_paged(const sbc_softmax_attention *&a, sbc_softmax_attention *read, int32_t n_pages,
+                       int32_t page, int32_t width) {
+    if (a) {
+        *read = *a;
+        read->m = read->causal = 0;
+        read->k_splits = nullptr;
+        a = read;
+    }
     SBC_TRY(check_softmax(a));
     if (!a->splits && a->n != a->n_batch)
         return fail(SBC_ERR_INVALID_ARG, "without splits every sequence has one new token (n = n_batch)");
@@ -27,7 +34,8 @@ using namespace sbc;
 
 extern "C" size_t sbc_softmax_attention_paged_workspace_size(const sbc_softmax_attention *a,
                                                              int32_t page, int32_t width) {
-    if (check_paged(a, 0, page, width) != SBC_OK) return 0;
+    sbc_softmax_attention read;
+    if (check_paged(a, &read, 0, page, width) != SBC_OK) return 0;
     return softmax_workspace(a, softmax_plan(a, most_keys(page, width)));
 }
 
@@ -39,7 +47,8 @@ extern "C" sbc_status sbc_softmax_attention_paged(const sbc_softmax_attention *a
                                                   float *lse, void *workspace,
                                                   size_t workspace_bytes, hipStream_t stream) {
     clear_error();
-    SBC_TRY(check_paged(a, n_pages, page, width));
+    sbc_softmax_attention read;
+    SBC_TRY(check_paged(a, &read, n_pages, page, width));
     const int32_t n = a->n, H = a->heads, G = a->kv_heads;
     const sbc_dtype dt = a->dtype;
     SBC_TRY(check_heads(q, H, n, a->dk, dt, "q"));

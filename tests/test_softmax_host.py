@@ -233,6 +233,18 @@ def test_paged_arrays(lib, case):
     assert _paged(lib, _cache_at(case)) == INVALID
 
 
+@pytest.mark.parametrize("m", [-7, 2 ** 31 - 1])
+def test_paged_reads_no_fields_of_packed_keys(lib, m):
+    """m, causal and k_splits may hold anything, in the call and in its size query."""
+    at = _cache_at()
+    odd = dict(m=m, causal=m, k_splits=at["q"] + 1)
+    assert _paged(lib, at, n=0, **odd) == 0
+    assert _paged(lib, at, wsb=8, width=1000, **odd) == WORKSPACE  # past the checks
+    f = lib.sbc_softmax_attention_paged_workspace_size
+    size = f(_soft(at, n=1, n_batch=1, m=0, causal=0, k_splits=None), 16, 10_000)
+    assert size > 0 and f(_soft(at, n=1, n_batch=1, **odd), 16, 10_000) == size
+
+
 SLOTS = ("lengths", "splits", "table", "free", "out", "slots", "after", "needed", "ws")
 
 
