@@ -797,7 +797,8 @@ sbc_status sbc_softmax_attention_backward(const sbc_softmax_attention *a, const 
  *
  * sbc_cache_append: rows of k [n, kv_heads, dk] and v [n, kv_heads, dv] to their slots;
  * slots outside 0 .. n_pages * page - 1 are left out, the others must be distinct.  Either
- * of k and v may be NULL with its pages.
+ * of k and v may be NULL with its pages.  Both may lie in one pool, halves of each page, token
+ * or head.
  * ------------------------------------------------------------------------ */
 typedef struct {
     void *data;

@@ -266,8 +266,11 @@ extern "C" sbc_status sbc_cache_append(const sbc_heads *k, const sbc_heads *v, i
         rows[w] = region_heads(x, kv_heads, n, d, dtype);
         pages[w] = region_pages(to, n_pages, page, kv_heads, d, dtype);
     }
-    SBC_TRY(check_apart({pages[0], pages[1]}, {rows[0], rows[1], region(slots, n, 8)}));
+    for (const Region &to : pages)
+        SBC_TRY(check_apart({to}, {rows[0], rows[1], region(slots, n, 8)}));
     if (n_pages == 0) return SBC_OK;
+    if (k && v && meet_pages(k_pages, dk, v_pages, dv, n_pages, page, kv_heads, dtype))
+        return fail(SBC_ERR_INVALID_ARG, "two outputs overlap");
     if ((units[0] + units[1]) * n >= (int64_t)1 << 31)
         return fail(SBC_ERR_UNSUPPORTED, "the rows must be fewer than 2^31 pieces of 16 bytes");
     a.n = n;

@@ -209,5 +209,35 @@ inline Region region_pages(const sbc_pages *x, int32_t n_pages, int32_t page, in
     if (n_pages > 1 && stride < span) return {x->data, stride * (n_pages - 1) + span, 0, 1};
     return {x->data, span, stride, n_pages};
 }
+// The same by another of its strides, `step` elements (> 0): blocks that far apart, each with what
+// lies within a step.  That holds all of it if wider strides are multiples of the step; else,
+// and where blocks run into each other, no blocks are given.
+inline Region region_pages_by(const sbc_pages *x, int32_t n_pages, int32_t page, int32_t heads,
+                              int32_t d, sbc_dtype dt, int64_t step) {
+    const int64_t e = (int64_t)dtype_bytes(dt);
+    int64_t within = d, last = 0;  // of a block; the last block's first element
+    const int64_t dims[3][2] = {{n_pages, x->page_stride}, {page, x->token_stride}, {heads, x->head_stride}};
+    for (const auto &dim : dims) {
+        if (dim[0] <= 1) continue;
+        if (dim[1] < step) within += dim[1] * (dim[0] - 1);
+        else if (dim[1] % step == 0) last += dim[1] * (dim[0] - 1);
+        else return {nullptr, 0, 0, 0};
+    }
+    if (within > step) return {nullptr, 0, 0, 0};
+    return {x->data, within * e, step * e, last / step + 1};
+}
+// Whether two caches share memory.  They may lie in the gaps of each other's pages, tokens or heads.
+inline bool meet_pages(const sbc_pages *x, int32_t dx, const sbc_pages *y, int32_t dy, int32_t n_pages,
+                       int32_t page, int32_t heads, sbc_dtype dt) {
+    if (!meet(region_pages(x, n_pages, page, heads, dx, dt), region_pages(y, n_pages, page, heads, dy, dt)))
+        return false;
+    for (const int64_t step : {x->page_stride, x->token_stride, x->head_stride}) {
+        if (step <= 0) continue;
+        const Region a = region_pages_by(x, n_pages, page, heads, dx, dt, step),
+                     b = region_pages_by(y, n_pages, page, heads, dy, dt, step);
+        if (a.data && b.data && !meet(a, b)) return false;
+    }
+    return true;
+}
 
 }  // namespace sbc

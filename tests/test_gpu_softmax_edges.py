@@ -101,3 +101,32 @@ def test_most_kept_tokens():
     for n in (2_120_000_000, MOST, 2 ** 31 - 1):
         o = sbc.softmax_attention_paged(q, k, v, table, _ints([n]), scale=1.0)
         assert torch.equal(o, v[0, :1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", ["page", "token", "head", "heads first"])
+def test_keys_and_values_in_one_pool(layout, dtype):
+    """Appended to, and read, as caches of their own, bit by bit; other places keep what they held."""
+    rng = np.random.default_rng(21)
+    n_pages, page, g, d, lengths = 9, 16, 2, 64, [70, 37]
+    shape = {"page": (n_pages, 2, page, g, d), "token": (n_pages, page, 2, g, d),
+             "head": (n_pages, page, g, 2, d), "heads first": (n_pages, 2, g, page, d)}[layout]
+    pool = torch.full((2, *shape), 5.0, dtype=dtype, device=DEV)
+    kv = pool[0].unbind(shape.index(2))
+    if layout == "heads first":
+        kv = [x.transpose(1, 2) for x in kv]
+    own = [torch.full((n_pages, page, g, d), 5.0, dtype=dtype, device=DEV) for _ in range(2)]
+    table = torch.full((2, 5), -1, dtype=torch.int32, device=DEV)
+    free = torch.randperm(n_pages, device=DEV).to(torch.int32)
+    splits = _ints([0, *np.cumsum(lengths)])
+    k, v = (_rand(rng, (sum(lengths), g, d), dtype) for _ in range(2))
+    table, slots, after, _ = sbc.cache_slots(_ints([0, 0]), table, free, page, splits=splits,
+                                             n=sum(lengths))
+    for pages in (kv, own):
+        sbc.cache_append(k, v, *pages, slots)
+    for x, y in zip(kv, own):
+        assert torch.equal(x, y)
+    assert bool((pool[1] == 5).all())
+    q = _rand(rng, (2, 4, d), dtype)
+    assert torch.equal(sbc.softmax_attention_paged(q, *kv, table, after),
+                       sbc.softmax_attention_paged(q, *own, table, after))

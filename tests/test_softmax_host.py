@@ -317,6 +317,76 @@ def test_cache_append_layouts(lib):
     assert call(ctypes.byref(L.SbcPages(at["vp"] - 4, both, HK * DV, DV))) == INVALID
 
 
+def _elements(base, strides, dims, d):
+    """Of a cache: the places of all its elements"""
+    at = np.full(1, base)
+    for n, s in (*zip(dims, strides), (d, 1)):
+        at = (at[:, None] + s * np.arange(n)).ravel()
+    return at
+
+
+def _append_places(lib, k, v, dims, dk, dv, dt):
+    """The status of caches at elements and strides k and v, past their checks of overlaps
+    UNSUPPORTED, by the number of rows"""
+    e = 4 if dt == 0 else 2
+    n_pages, page, heads = dims
+    pages = [ctypes.byref(L.SbcPages(A + e * at, *strides)) for at, strides in (k, v)]
+    rows = lambda x, d: _heads((x, heads * d, d))  # noqa: E731
+    return lib.sbc_cache_append(rows(8 * A, dk), rows(9 * A, dv), 2 ** 31 - 1, heads, dk, dv, dt,
+                                10 * A, *pages, n_pages, page, None)
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("dims", [(5, 4, 3), (1, 4, 3), (5, 1, 3), (5, 4, 1), (1, 1, 2), (2, 1, 1)])
+@pytest.mark.parametrize("dk,dv", [(16, 16), (16, 8), (9, 7)])
+def test_cache_append_one_pool(lib, dims, dk, dv, dt):
+    """Keys and values beside each other in a page, a token, a head's channels, heads before or
+    behind tokens: taken; one element into each other: refused."""
+    pages, page, G = dims
+    both = G * (dk + dv)
+    layouts = [
+        ((0, (page * both, G * dk, dk)), (page * G * dk, (page * both, G * dv, dv))),  # of a page
+        ((0, (page * both, both, dk)), (G * dk, (page * both, both, dv))),             # of a token
+        ((0, (page * both, both, dk + dv)), (dk, (page * both, both, dk + dv))),       # of a head
+        ((0, (page * both, dk, page * dk)),
+         (page * G * dk, (page * both, dv, page * dv))),                               # heads first
+        ((0, (page * both, dk + dv, page * (dk + dv))),
+         (dk, (page * both, dk + dv, page * (dk + dv)))),                              # and of a head
+        ((0, (page * G * dk, G * dk, dk)),
+         (pages * page * G * dk, (page * G * dv, G * dv, dv))),                        # apart
+        ((0, (both, pages * both, dk)), (G * dk, (both, pages * both, dv))),           # pages inside
+    ]
+    for k, v in layouts:
+        assert _append_places(lib, k, v, dims, dk, dv, dt) == UNSUPPORTED, (k, v)
+        assert _append_places(lib, v, k, dims, dv, dk, dt) == UNSUPPORTED, (k, v)
+        assert _append_places(lib, k, (v[0] - 1, v[1]), dims, dk, dv, dt) == INVALID, (k, v)
+
+
+def test_cache_append_overlaps_are_found(lib):
+    """No two caches of any strides are taken that share an element."""
+    rng = np.random.default_rng(5)
+    kinds = {True: set(), False: set()}
+    for _ in range(4000):
+        dims, dk, dv = rng.integers(1, 4, 3), int(rng.integers(1, 7)), int(rng.integers(1, 7))
+        two = []
+        for d in (dk, dv):
+            order, step, strides = rng.permutation(3), d + int(rng.integers(0, 7)), [0, 0, 0]
+            for axis in order:
+                strides[axis] = step
+                step = step * (dims[axis] + int(rng.integers(0, 2))) + int(rng.integers(0, 2)) * 3
+            two.append(strides)
+        if rng.random() < 0.7:
+            two[1] = list(two[0])
+        off = int(rng.integers(0, 60))
+        places = [_elements(at, st, dims, d) for at, st, d in ((0, two[0], dk), (off, two[1], dv))]
+        if any(len(np.unique(x)) < len(x) for x in places):
+            continue  # (refused by itself)
+        share = len(np.intersect1d(*places)) > 0
+        status = _append_places(lib, (0, two[0]), (off, two[1]), tuple(int(x) for x in dims), dk, dv, 0)
+        kinds[share].add(status)
+    assert kinds[True] == {INVALID} and UNSUPPORTED in kinds[False]
+
+
 # ---------------------------------------------------------------- the reference
 def _numeric(f, x, d, eps=1e-5):
     return (f(x + eps * d) - f(x - eps * d)) / (2 * eps)
