@@ -487,7 +487,7 @@ template <int D, int kRows, int kThreads> struct DirectTile {
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                          :
                          : "s"(m0), "v"(off[s]), "s"(base)
-                         : "memory");
+                         : "memory", "m0");
         }
     }
     // Values of the tile, which has landed, as TileLoad::put_bad_apart has them
@@ -522,7 +522,7 @@ __device__ __forceinline__ void direct_floats(const float *base, const float *to
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
                      :
                      : "s"(m0), "v"((uint32_t)lane * 4u), "s"(base)
-                     : "memory");
+                     : "memory", "m0");
 }
 // until at most kLeft of this wave's loads are on their way
 template <int kLeft> __device__ __forceinline__ void wait_direct() {

@@ -1,7 +1,9 @@
 """Softmax attention's index arithmetic that the compiler can check without a GPU: the headers
 are compiled for the host with static assertions (in a constant expression an overflow of int32
 is an error)."""
+import glob
 import os
+import re
 import shutil
 import subprocess
 
@@ -135,3 +137,14 @@ constexpr bool all() {
 static_assert(all(), "the parts that begin below the limit");
 """)
     assert r.returncode == 0, r.stderr
+
+
+def test_assembly_names_what_it_overwrites():
+    """Each piece of assembly that sets m0 names it to the compiler, which may keep a value there."""
+    found = 0
+    for path in glob.glob(os.path.join(ROOT, "paper_2012_01170_amd", "csrc", "*.h*")):
+        for text in re.findall(r"asm\b.*?;", open(path).read(), re.S):
+            if re.search(r"\bm0\s*,\s*%", text):
+                found += 1
+                assert '"m0"' in text.rsplit(":", 1)[1], (path, text)
+    assert found > 0
