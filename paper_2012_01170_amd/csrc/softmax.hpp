@@ -591,7 +591,11 @@ __device__ __forceinline__ uint32_t seen_bits(uint64_t there, int u, int32_t vis
 
 // Scores x of kSub x 32 keys -> their weights, in place; the sums follow the maximum.  The
 // maximum that weights refer to moves only where a score lies 2^8 above it (a weight then is
-// at most 2^8, and rounded as a smaller one is), so that most tiles leave the sums alone.
+// at most 2^8, and rounded as a smaller one is), so that most tiles leave the sums alone.  Sums of
+// products with values up to 2^119 / keys stay in range.  (To take larger ones, all weights could lie
+// below 1 / keys: exponents that far from zero are rounded by 2^-20, and o and lse of float32
+// inputs with them.  Or a workgroup whose sums are not finite could go through its keys again like
+// that: 20 to 50 registers more in every instance, a wave a SIMD less of 64 bf16 channels.)
 template <int D, int kSub>
 __device__ __forceinline__ void softmax_weights(floatx16 (&x)[kSub], float scale2, RowSums<D> &s) {
     float top = fmaxf(x[0][0], x[kSub - 1][15]);

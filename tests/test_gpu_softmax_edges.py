@@ -10,7 +10,8 @@ import torch
 
 import paper_2012_01170_amd as sbc
 from paper_2012_01170_amd import _lib as L
-from tests.test_gpu_softmax import BF16, DEV, F32, _ints, _rand
+from tests import softmax_ref as S
+from tests.test_gpu_softmax import BF16, DEV, F32, U, _close, _ints, _np, _rand
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +131,33 @@ def test_keys_and_values_in_one_pool(layout, dtype):
     q = _rand(rng, (2, 4, d), dtype)
     assert torch.equal(sbc.softmax_attention_paged(q, *kv, table, after),
                        sbc.softmax_attention_paged(q, *own, table, after))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,n,paged", [((2, 1), 100, False), ((1, 1), 3000, False),
+                                           ((32, 16), 600, False), ((2, 1), 300, True),
+                                           ((32, 16), 600, True)])
+def test_large_values(heads, n, paged, dtype):
+    """Values up to the stated bound, 2^119 / keys, that rows see behind a tile of lower scores, whose
+    maximum the weights refer to: a score 5.5 above it is a weight of 2^7.9."""
+    print(f"[large values] {heads} {n} {paged} {dtype}", flush=True)
+    rng = np.random.default_rng(22)
+    (hq, hk), d = heads, 64
+    new = n if hq > 2 else 3
+    q = torch.zeros(new, hq, d, dtype=dtype, device=DEV)
+    k = torch.zeros(n, hk, d, dtype=dtype, device=DEV)
+    q[:, :, 0], k[64:, :, 0] = 1.0, 5.5
+    v = (1 - 0.5 * torch.rand(n, hk, d, device=DEV)) * (2.0 ** 119 / n)
+    v = (v * torch.where(_rand(rng, (1, hk, d)) > 0.5, -1.0, 1.0)).to(dtype)  # (nothing cancels)
+    if paged:
+        page = 32
+        pages = [torch.zeros(-(-n // page), page, hk, d, dtype=dtype, device=DEV) for _ in range(2)]
+        for x, y in zip((k, v), pages):
+            y.view(-1, hk, d)[:n] = x
+        table = torch.arange(len(pages[0]), dtype=torch.int32, device=DEV)[None].contiguous()
+        o = sbc.softmax_attention_paged(q, *pages, table, _ints([n]), splits=_ints([0, new]), scale=1.0)
+    else:
+        o, _ = sbc.softmax_attention_forward(q, k, v, scale=1.0, causal=True)
+    u = U[dtype] if dtype == BF16 else 0.0
+    ro, _, to, _ = S.attention(_np(q), _np(k), _np(v), [0, new], [0, n], 1.0, True, u)
+    _close(o, ro, to + U[dtype] * np.abs(ro), "o")
