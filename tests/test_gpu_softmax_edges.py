@@ -11,7 +11,9 @@ import torch
 import paper_2012_01170_amd as sbc
 from paper_2012_01170_amd import _lib as L
 from tests import softmax_ref as S
-from tests.test_gpu_softmax import BF16, DEV, F32, U, _close, _ints, _np, _rand
+from tests.test_gpu_softmax import (BF16, DEV, F32, U, _check, _close, _inputs, _ints, _np, _rand,
+                                     _splits)
+from tests.test_gpu_softmax_cache import _check as _check_paged
 
 pytestmark = pytest.mark.gpu
 
@@ -161,3 +163,112 @@ def test_large_values(heads, n, paged, dtype):
     u = U[dtype] if dtype == BF16 else 0.0
     ro, _, to, _ = S.attention(_np(q), _np(k), _np(v), [0, new], [0, n], 1.0, True, u)
     _close(o, ro, to + U[dtype] * np.abs(ro), "o")
+
+
+# ---------------------------------------------------------------- batches that fill the card
+# (Keys are in one part there: outputs are stored by the kernels that make the sums.)
+FULL = 64  # sequences
+
+
+def _lengths(rng, empty):
+    lens = rng.integers(100, 230, FULL)
+    lens[empty], lens[empty + 1] = 0, 1
+    return lens
+
+
+def _full_call(lq, heads, dk, dv, dtype, causal, lk=None):
+    n = int(sum(lq))
+    m = n if lk is None else int(sum(lk))
+    return L.SbcSoftmaxAttention(n, m, FULL, *heads, dk, dv, L.SBC_F32 if dtype == F32 else L.SBC_BF16,
+                                 dk ** -0.5, int(causal), 256, None if lk is None else 256)
+
+
+def _one_part(a):
+    """Whether the size queries tell of one part: no sums for the forward pass, and the backward's
+    two numbers of each row alone, which it has where it takes more than one launch"""
+    lib, rows = L.lib(), 4 * a.n * a.heads
+    size = lib.sbc_softmax_attention_backward_workspace_size(ctypes.byref(a))
+    return (lib.sbc_softmax_attention_workspace_size(ctypes.byref(a)) == 0
+            and 2 * rows <= size <= 2 * rows + 1024)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,dk,dv", [((8, 8), 33, 33), ((8, 8), 40, 40), ((16, 8), 64, 64),
+                                         ((8, 8), 96, 96), ((16, 8), 128, 128), ((8, 8), 128, 64),
+                                         ((24, 8), 20, 24)])
+def test_full_batches(heads, dk, dv, causal, dtype):
+    print(f"[full] {heads} {dk} {dv} {causal} {dtype}", flush=True)
+    rng = np.random.default_rng(dk + dv + causal)
+    lq = _lengths(rng, 5)
+    lk = None if causal else _lengths(rng, 30)
+    assert _one_part(_full_call(lq, heads, dk, dv, dtype, causal, lk))
+    n, m = int(sum(lq)), int(sum(lq if lk is None else lk))
+    _check(*_inputs(rng, n, m, *heads, dk, dv, dtype), lq, lk, causal)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_full_batches_of_views(d, dtype):
+    """Rows off 16 bytes, with NaN between them: as contiguous ones, bit by bit"""
+    rng = np.random.default_rng(d)
+    lq = _lengths(rng, 0)
+    n, splits = int(sum(lq)), _ints(_splits(lq))
+    assert _one_part(_full_call(lq, (8, 8), d, d, dtype, True))
+    wide = torch.full((n, 32, d + 3), math.nan, dtype=dtype, device=DEV)
+    views = [wide[:, 8 * i:8 * i + 8, 1:1 + d] for i in range(4)]
+    for x in views:
+        x.copy_(_rand(rng, x.shape, dtype))
+
+    def passes(q, k, v, do):
+        o, lse = sbc.softmax_attention_forward(q, k, v, splits=splits, causal=True)
+        return (o, lse, *sbc.softmax_attention_backward(do, q, k, v, o, lse, splits=splits, causal=True))
+
+    for a, b in zip(passes(*views), passes(*(x.contiguous() for x in views))):
+        assert torch.equal(a, b) and bool(torch.isfinite(a.float()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_full_batches_leave_other_rows(dtype):
+    rng = np.random.default_rng(23)
+    lq, h, d = _lengths(rng, 9), 8, 64
+    n = 7 + int(sum(lq)) + 30
+    splits = _ints(7 + _splits(lq))
+    a = _full_call(lq, (h, h), d, d, dtype, True)
+    a.n, a.m, a.splits = n, n, splits.data_ptr()
+    assert _one_part(a)
+    q, k, v, do = _inputs(rng, n, n, h, h, d, d, dtype)
+    o, dq, dk, dv = (torch.full_like(q, 5.0) for _ in range(4))
+    lse = torch.full((n, h), 5.0, device=DEV)
+    lib, ref = L.lib(), ctypes.byref(a)
+    size = lib.sbc_softmax_attention_backward_workspace_size(ref)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    L.check(lib.sbc_softmax_attention_forward(ref, _heads(q), _heads(k), _heads(v), _heads(o),
+                                              lse.data_ptr(), None, 0, stream))
+    L.check(lib.sbc_softmax_attention_backward(
+        ref, _heads(do), _heads(q), _heads(k), _heads(v), _heads(o), lse.data_ptr(), _heads(dq),
+        _heads(dk), _heads(dv), ws.data_ptr(), size, stream))
+    torch.cuda.synchronize()
+    own = slice(7, n - 30)
+    ro, rl = sbc.softmax_attention_forward(q[own], k[own], v[own], splits=_ints(_splits(lq)), causal=True)
+    grads = sbc.softmax_attention_backward(do[own], q[own], k[own], v[own], ro, rl,
+                                           splits=_ints(_splits(lq)), causal=True)
+    for x, r in zip((o, lse, dq, dk, dv), (ro, rl, *grads)):
+        assert bool((x[:7] == 5).all()) and bool((x[n - 30:] == 5).all())
+        assert torch.equal(x[own], r)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d,layout", [(33, 0), (40, 1), (64, 0), (64, 2), (96, 0), (128, 0), (128, 1)])
+def test_full_batches_in_pages(d, layout, dtype):
+    print(f"[full, paged] {d} {layout} {dtype}", flush=True)
+    rng = np.random.default_rng(d + layout)
+    new = _lengths(rng, 3)
+    lengths = new + rng.integers(0, 90, FULL)
+    page, heads = 48, (8, 8)
+    a = _full_call(new, heads, d, d, dtype, True)
+    width = int(-(-lengths.max() // page)) + 1
+    assert L.lib().sbc_softmax_attention_paged_workspace_size(ctypes.byref(a), page, width) == 0
+    assert a.n > 64 * FULL  # (workgroups of 128 rows)
+    _check_paged(rng, lengths, new, page, *heads, d, d, dtype, layout)
