@@ -736,7 +736,8 @@ sbc_status sbc_qk_norm_rotary_backward(const sbc_rotary_plan *plan, const sbc_he
  * Scores, maxima and sums are float32.  Products are taken on the matrix cores, of float32
  * inputs with operands split into three bf16 parts (products up to 2^-22 of the whole left
  * out); of bf16 inputs, the weights are rounded to bf16 (2^-8 each) on their way to the
- * products that give o and dv, and dS has two parts (2^-17).
+ * products that give o and dv, and dS has two parts (2^-17; the weights as well in section 16's
+ * calls of few rows: new tokens times heads of a key head, up to 64 a sequence on average).
  * Sums of products with v are divided by those of the weights at the end, and a weight before
  * that is up to 2^8: o is finite where |v| is below 2^119 / keys (2e31 for 32768 of a sequence);
  * of larger values, up to the type's largest, it may come out as infinite or NaN.

@@ -659,8 +659,8 @@ __device__ __forceinline__ void row_products(Read read, Operand operand, floatx1
 // acc[t] += columns 32 t .. + 31 of the tile, transposed, times weights by rows: k-step h takes
 // rows 16 h .. + 15.  First read(), which may lie well before, then add().
 // kBuffers: steps that are in registers at once, 2 or 1.  kWeights: the weights' parts.  A bf16
-// call's softmax weights have one: each is rounded by up to 2^-8, independently of the others,
-// beside the output's own rounding of as much.
+// call's softmax weights have one (over a cache of few rows two, kFewWeights): each is rounded by
+// up to 2^-8, independently of the others, beside the output's own rounding of as much.
 template <typename T, int D, int kRows, int kBuffers = 2, int kWeights = kParts<T>>
 struct ColumnProducts {
     static constexpr int NP = kParts<T>, kSteps = kRows / 16;

@@ -235,6 +235,15 @@ __global__ __launch_bounds__(kSoftmaxThreads, (kTileWaves<T, D>)) void softmax_t
 }
 
 // ---------------------------------------------------------------- few rows
+// The parts of a weight where it meets v (kWeights of ColumnProducts).  Over a cache, which memory
+// bounds, a bf16 call's have two (2^-17): o is as near as with float32 weights, and one part was
+// 1e-3 .. 1.8e-3 away from that (a token each over 1 x 4095 and 64 x 8000: 14.5 and 121 us with
+// either; 64 streams of 16 tokens, 8 heads of 128: 111 us, 113; 32 of 64 tokens, 8 of 64: 32, 34).
+// One where it costs more: packed keys of 128 channels lack the registers (32 sequences of 64
+// tokens over 2000 keys: 78 us, 92), and workgroups of 128 rows are bound by products (32768 events
+// 615 us, 838; 32 prompts 124, 146; chunks over a cache 58, 65; dv in the gradients 2595, 2750).
+template <typename T, bool kPaged> constexpr int kFewWeights = sizeof(T) == 4 ? 3 : kPaged ? 2 : 1;
+
 // A workgroup has 32 rows and one part of the keys; each wave takes every fourth 32 of
 // these keys by itself (keys from memory to registers, values through LDS of its own),
 // and the waves' sums are joined at the end.  Memory bounds it where a row or few meet a long cache:
@@ -347,7 +356,7 @@ __global__ __launch_bounds__(kSoftmaxThreads, (sizeof(T) == 4 && D > 32 ? 1 : 2)
         softmax_weights<D, 1>(w, p.scale2, sums);
         // (the wave's own LDS, which it reads in the order of its writes)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        ColumnProducts<T, D, 32> values;
+        ColumnProducts<T, D, 32, 2, kFewWeights<T, kPaged>> values;
         values.read(vt, kPlane, 0, at);
         values.add(w, vt, kPlane, 0, at, sums.o);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -13,7 +13,7 @@ from paper_2012_01170_amd import _lib as L
 from tests import softmax_ref as S
 from tests.test_gpu_softmax import (BF16, DEV, F32, U, _check, _close, _inputs, _ints, _np, _rand,
                                      _splits)
-from tests.test_gpu_softmax_cache import _check as _check_paged
+from tests.test_gpu_softmax_cache import _cache, _check as _check_paged
 
 pytestmark = pytest.mark.gpu
 
@@ -163,6 +163,24 @@ def test_large_values(heads, n, paged, dtype):
     u = U[dtype] if dtype == BF16 else 0.0
     ro, _, to, _ = S.attention(_np(q), _np(k), _np(v), [0, new], [0, n], 1.0, True, u)
     _close(o, ro, to + U[dtype] * np.abs(ro), "o")
+
+
+@pytest.mark.parametrize("lengths,new,page,heads,dk,dv", [
+    ([1000, 5, 64, 0], [1, 1, 1, 1], 16, (8, 2), 128, 128), ([4095], [1], 48, (4, 4), 64, 64),
+    ([300, 77], [16, 3], 5, (2, 1), 33, 31), ([40, 700], [8, 8], 64, (16, 2), 96, 40)])
+def test_tokens_over_a_cache_are_rounded_once(lengths, new, page, heads, dk, dv):
+    """bf16: weights have two parts of 8 bits there (2^-17), so o is as far from its exact value as
+    float32 sums and its own rounding allow."""
+    print(f"[rounded once] {lengths} {new} {heads} {dk} {dv}", flush=True)
+    rng = np.random.default_rng(24)
+    (kp, vp), table, _ = _cache(rng, lengths, page, heads[1], dk, dv, BF16)
+    splits = _splits(new)
+    q = _rand(rng, (int(splits[-1]), heads[0], dk), BF16, 1.5)
+    o = sbc.softmax_attention_paged(q, kp, vp, _ints(table), _ints(lengths), splits=_ints(splits))
+    K, ks = S.gather_pages(_np(kp), table, np.asarray(lengths))
+    V, _ = S.gather_pages(_np(vp), table, np.asarray(lengths))
+    ro, _, to, _ = S.attention(_np(q), K, V, splits, ks, dk ** -0.5, True, 2.0 ** -17)
+    _close(o, ro, to + U[BF16] * np.abs(ro), "o")
 
 
 # ---------------------------------------------------------------- batches that fill the card
