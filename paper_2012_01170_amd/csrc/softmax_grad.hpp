@@ -19,7 +19,10 @@ template <typename T> constexpr int kGradParts = sizeof(T) == 4 ? 3 : 2;
 
 // dq: a workgroup has 128 rows, 32 a wave, as softmax_tile_kernel.
 template <typename T, int D> constexpr int kGradKeys = sizeof(T) == 4 && D > 64 ? 32 : 64;
-// Waves a SIMD: the rows' operands and sums of wide heads in float32 fill its registers alone
+// Waves a SIMD: the rows' operands and sums of wide heads in float32 fill its registers alone.  At
+// two, heads of 64 float32 channels do not fit whole: 40 registers go to scratch in dq, 20 in dk and
+// dv, 97 where all are made in one launch (the offsets of a tile's pieces; bf16 heads: none in dq, up to
+// 14 in dk and dv, up to 82 in one launch).
 template <typename T, int D> constexpr int kGradWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
 template <typename T, int D> constexpr int kKeyGradWaves = sizeof(T) == 4 && D > 64 ? 1 : 2;
 

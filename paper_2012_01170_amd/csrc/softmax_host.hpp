@@ -86,12 +86,14 @@ inline SoftmaxArgs softmax_args(const sbc_softmax_attention *a) {
 // in one part, 68 of 32 rows, 57 of 128 rows in 4 parts).  Few are 64 rows a sequence on average, which
 // a workgroup of 128 would leave half empty, and problems too small for it to fill the CUs even in
 // parts; there a second launch pays past 512 keys (256 points, float32: 11 us in one part, 15 in two).
+// The lengths of packed sequences lie on the GPU, so that their plan takes all keys as one
+// sequence's: a batch of many short ones may get parts that are empty, and a join.
 struct SoftmaxPlan {
     bool few;
     int32_t parts;
     int64_t blocks;
 };
-// most_keys: of one sequence
+// most_keys: that one sequence can have
 inline SoftmaxPlan softmax_plan(const sbc_softmax_attention *a, int64_t most_keys) {
     const int64_t rows = (int64_t)a->n * (a->heads / a->kv_heads);
     const int cus = device_cus();
